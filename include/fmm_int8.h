@@ -1,0 +1,131 @@
+/*
+ * fmm_int8.h - the 8-bit integer layer of the B200 (sm_100a) library of fmm.h: activations and weights in 8-bit
+ * integers with fp32 scales, their product, the root-mean-square norm in front of it, and the gradients of both from
+ * what is held in 8 bits.
+ *
+ * 8-bit form of a matrix X (rows x cols): codes (int8) and scales (fp32), one scale per row (block == 0) or per block
+ * of `block` (32 or 128) consecutive columns of a row, the last block of a row being as short as it comes.  An element
+ * stands for code * scale.  With a = max(max |x| over the block, 1e-12):
+ *     FMM_INT8_SCALE_AMAX_DIV_127   scale = fl(a / 127),                      code = round(fl(x * fl(127 / a)))
+ *     FMM_INT8_SCALE_POW2           scale = 2^e, e = ceil(log2(fl(a / 127))), code = round(x * 2^-e)
+ * all in fp32, round() to the nearest integer, ties to even; |code| <= 127.  Values of power-of-two scales are exact in
+ * bf16.  A block that holds an infinity or a NaN gets NaN as its scale.
+ *
+ * General rules
+ *   - Status codes, "dev" pointers and streams as in fmm.h: nothing throws, aborts or traps the device, nothing is
+ *     allocated or synchronised, work is only enqueued on `cuda_stream`, on the current device.  Calls may be captured
+ *     into CUDA graphs.  Results do not depend on the run: no floating-point atomics, every sum in a fixed order.
+ *   - Matrices are row-major; `ld*` is the distance between rows in elements, at least the number of columns.  Any
+ *     alignment that their type allows is accepted where nothing else is said (16-byte aligned rows are read and
+ *     written fastest).  Elements behind the last column of a row are neither read nor written.
+ *   - Rows and columns may be 0: then nothing is read, and what an empty sum gives is written.
+ *   - An output may not overlap an input or another output, except where it is said.
+ *   - workspace: dev, 256-byte aligned, caller-owned; calls that share one must be stream-ordered.
+ */
+#ifndef FMM_INT8_H
+#define FMM_INT8_H
+
+#include "fmm.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum { FMM_INT8_SCALE_AMAX_DIV_127 = 0, FMM_INT8_SCALE_POW2 = 1 } fmm_int8_scale_t;
+typedef enum { FMM_TYPE_F32 = 0, FMM_TYPE_BF16 = 1, FMM_TYPE_F16 = 2 } fmm_type_t;
+
+/* 8-bit form of X (dev, rows x cols of `type`): codes (dev, rows x cols) and scales (dev, rows if block == 0, else
+ * rows x ceil(cols / block), dense). */
+fmm_status_t fmm_int8_quantize(const void* X, fmm_type_t type, int64_t ldx, int64_t rows, int64_t cols, int block,
+                               fmm_int8_scale_t scale_mode, int8_t* codes, int64_t ldc, float* scales, void* cuda_stream);
+
+/* X = code * scale, taken in fp32 and rounded once to `type` (dev, rows x cols).  Rows of codes may lie in any order
+ * that `ldc` gives. */
+fmm_status_t fmm_int8_dequantize(const int8_t* codes, int64_t ldc, const float* scales, int64_t rows, int64_t cols,
+                                 int block, void* X, fmm_type_t type, int64_t ldx, void* cuda_stream);
+
+/* Residual's addition, root-mean-square norm and 8-bit output, row by row:
+ *     h = fl(x + residual)  (x itself where residual is NULL);  rstd = fl32(1 / sqrt(sum h^2 / cols + eps)), in fp64;
+ *     codes, scales (one per row) = 8-bit form of fl(fl(h * rstd) * gain);
+ *     checkpoint, checkpoint_scales = 8-bit form of h in blocks of checkpoint_block, FMM_INT8_SCALE_AMAX_DIV_127.
+ *   x, residual, gain (cols), hidden: of `type`.  residual == NULL: no addition; hidden is then not written and may be
+ *   NULL.  hidden receives h rounded to `type`; it may be the same matrix as x or as residual (same pointer and
+ *   distance between rows).  rstd (rows) may be NULL.  checkpoint_block 0: no checkpoint, checkpoint and
+ *   checkpoint_scales are not used.  eps finite, >= 0. */
+typedef struct {
+    fmm_type_t type;
+    fmm_int8_scale_t scale_mode;
+    int checkpoint_block;
+    int64_t rows, cols;
+    double eps;
+    const void* x;        int64_t ldx;
+    const void* residual; int64_t ldr;
+    const void* gain;
+    void* hidden;         int64_t ldh;
+    int8_t* codes;        int64_t ldc;
+    float* scales;
+    float* rstd;
+    int8_t* checkpoint;   int64_t ldk;
+    float* checkpoint_scales;
+} fmm_int8_rms_norm_t;
+fmm_status_t fmm_int8_rms_norm(const fmm_int8_rms_norm_t* p, void* cuda_stream);
+
+/* Gradients of that norm, the rounding to 8 bits counting as the identity (straight through).  With
+ * xhat = checkpoint value * rstd and c = mean over the row of (dy * gain * xhat):
+ *     dx = rstd * (dy * gain - xhat * c) + dresidual;     dgain = sum over the rows of dy * xhat   (fp32)
+ *   dy, gain, dresidual (NULL: none), dx: of `type`.  dx, the gradient of x and of residual alike, may be the same
+ *   matrix as dy or as dresidual.  block: 32 or 128, or 0 for one checkpoint scale per row. */
+typedef struct {
+    fmm_type_t type;
+    int block;
+    int64_t rows, cols;
+    const void* dy;        int64_t ldy;
+    const int8_t* checkpoint; int64_t ldk;
+    const float* checkpoint_scales;
+    const float* rstd;
+    const void* gain;
+    const void* dresidual; int64_t ldr;
+    void* dx;              int64_t ldx;
+    float* dgain;
+} fmm_int8_rms_norm_backward_t;
+fmm_status_t fmm_int8_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
+fmm_status_t fmm_int8_rms_norm_backward(const fmm_int8_rms_norm_backward_t* p, void* workspace, size_t workspace_bytes,
+                                        void* cuda_stream);
+
+/* C = (A B^T) scaled by row and column, plus a bias: C[i][j] = acc * a_scales[i] * b_scales[j] + bias[j], the sum acc of
+ * the products of codes being exact, the rest in fp32, rounded once to `type`.
+ *   A dev, M x K codes (tokens); B dev, N x K codes (a weight, one row per output channel); C dev, M x N; bias dev, N of
+ *   `type`, or NULL.  A and B 16-byte aligned, lda and ldb multiples of 16 (FMM_ERR_INVALID_ARG; the codes that
+ *   fmm_int8_quantize and fmm_int8_rms_norm write may have any such ld); K <= 131071, so that no sum leaves 32 bits, and
+ *   M, N < 2^31 - 512 (FMM_ERR_SHAPE). */
+fmm_status_t fmm_int8_matmul(const int8_t* A, int64_t lda, const float* a_scales, const int8_t* B, int64_t ldb,
+                             const float* b_scales, const void* bias, int64_t M, int64_t N, int64_t K, void* C,
+                             fmm_type_t type, int64_t ldc, void* cuda_stream);
+
+/* Gradients of that product for dY (dev, M x N of `type`, FMM_TYPE_BF16 or FMM_TYPE_F16), from what is held in 8 bits.
+ * The 8-bit values code * scale are restored in dY's type (exactly, for bf16 and power-of-two scales; otherwise rounded
+ * once), products are summed in fp32.
+ *     fmm_int8_grad_weight: dW[j][k] (+)= sum_i dY[i][j] * (X[i][k] * x_scales[i])
+ *         X dev, M x K codes; dW dev, N x K of out_type: FMM_TYPE_F32 or dY's type.  accumulate != 0 adds to dW.
+ *     fmm_int8_grad_input:  dX[i][k] = sum_j dY[i][j] * (W[j][k] * w_scales[j])
+ *         W dev, N x K codes; dX dev, M x K of out_type: FMM_TYPE_F32 or dY's type.
+ *   M, N, K < 2^31 - 512 (FMM_ERR_SHAPE).  The workspace holds the restored operand and, where its rows are not 16-byte
+ *   aligned, a copy of dY; its size depends on dY's alignment (dy_aligned: dY and ldy * 2 are multiples of 16). */
+fmm_status_t fmm_int8_grad_workspace_bytes(int64_t code_rows, int64_t K, int64_t M, int64_t N, int dy_aligned, size_t* bytes);
+fmm_status_t fmm_int8_grad_weight(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* X, int64_t ldx,
+                                  const float* x_scales, int64_t M, int64_t N, int64_t K, void* dW, fmm_type_t out_type,
+                                  int64_t ldw, int accumulate, void* workspace, size_t workspace_bytes, void* cuda_stream);
+fmm_status_t fmm_int8_grad_input(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* W, int64_t ldw,
+                                 const float* w_scales, int64_t M, int64_t N, int64_t K, void* dX, fmm_type_t out_type,
+                                 int64_t ldx, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Status of the product kernels on the current device, read after cudaDeviceSynchronize: *code == 0, or the location of
+ * the first bounded device-side wait that gave up (FMM_ERR_DEVICE_TIMEOUT; the results of that call are invalid).
+ * Debug build (fmm_debug_build): also the first store outside the ranges that a launch was given. */
+fmm_status_t fmm_int8_status(int* code);
+fmm_status_t fmm_int8_status_clear(void);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* FMM_INT8_H */

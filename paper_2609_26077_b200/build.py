@@ -8,8 +8,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libfmm_b200.so")
 SOURCES = ["fmm_api.cu", "fmm_encode.cu", "fmm_gemm.cu", "fmm_keep.cu", "fmm_split.cu", "fmm_stats.cu"]
+INT8_SOURCES = ["int8_rows.cu", "int8_product.cu"]          # the 8-bit integer layer (include/fmm_int8.h), in the same library
 HEADERS = [os.path.join(CSRC, h) for h in sorted(os.listdir(CSRC)) if h.endswith((".h", ".cuh"))] + [
-    os.path.join(HERE, "..", "include", "fmm.h")]
+    os.path.join(HERE, "..", "include", h) for h in ("fmm.h", "fmm_int8.h")]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC", "-cudart", "static"]
@@ -22,7 +23,7 @@ def _stale(out):
     if not os.path.exists(out):
         return True
     t = os.path.getmtime(out)
-    deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
+    deps = [os.path.join(CSRC, s) for s in SOURCES + INT8_SOURCES] + HEADERS
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -32,7 +33,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
         return out
     objs = []
     procs = []
-    for s in SOURCES:
+    for s in SOURCES + INT8_SOURCES:
         o = os.path.join(CSRC, s.replace(".cu", ".dbg.o" if debug else ".o"))
         cmd = ([NVCC] + FLAGS + (["-DFMM_DEBUG"] if debug else []) + (["-Xptxas", "-v"] if verbose else []) +
                ["-c", os.path.join(CSRC, s), "-o", o])

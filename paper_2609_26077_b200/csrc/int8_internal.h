@@ -1,0 +1,63 @@
+// Internal declarations of the 8-bit integer layer (not part of the C ABI).
+#pragma once
+#include <cuda_runtime.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+#include "../../include/fmm_int8.h"
+#include "fmm_internal.h"
+
+// Store ranges of a launch, checked in the FMM_DEBUG build only (as FmmGuard, for launches with more than two outputs).
+struct Int8Ranges {
+#ifdef FMM_DEBUG
+    const char* lo[6];
+    const char* hi[6];
+    int count;
+#endif
+};
+static inline void int8_add_range(Int8Ranges& r, const void* p, int64_t rows, int64_t cols, int64_t ld, int64_t element)
+{
+#ifdef FMM_DEBUG
+    if (!p || rows <= 0 || cols <= 0) return;
+    r.lo[r.count] = static_cast<const char*>(p);
+    r.hi[r.count++] = static_cast<const char*>(p) + ((rows - 1) * ld + cols) * element;
+#else
+    (void)r; (void)p; (void)rows; (void)cols; (void)ld; (void)element;
+#endif
+}
+#if defined(FMM_DEBUG) && defined(__CUDACC__)
+__device__ __forceinline__ bool int8_store_ok(const Int8Ranges& r, const void* ptr, size_t bytes, int code, int* word)
+{
+    const char* c = static_cast<const char*>(ptr);
+    for (int i = 0; i < r.count; ++i) if (c >= r.lo[i] && c + bytes <= r.hi[i]) return true;
+    atomicCAS(word, 0, code);
+    return false;
+}
+#define INT8_STORE_OK(r, ptr, bytes, code, word) int8_store_ok(r, ptr, bytes, code, word)
+#else
+#define INT8_STORE_OK(r, ptr, bytes, code, word) true
+#endif
+
+static inline int int8_type_bytes(fmm_type_t t) { return t == FMM_TYPE_F32 ? 4 : 2; }
+static inline bool int8_type_ok(fmm_type_t t) { return t == FMM_TYPE_F32 || t == FMM_TYPE_BF16 || t == FMM_TYPE_F16; }
+static inline bool int8_aligned(const void* p, int64_t ld_bytes, unsigned a) { return (((uintptr_t)p | (uintptr_t)ld_bytes) & (a - 1)) == 0; }
+// Rows and columns that 32-bit indexes hold with room for a tile behind them
+constexpr int64_t INT8_MAX_DIM = ((int64_t)1 << 31) - 512;
+
+#ifdef __CUDACC__
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+template <typename T> __device__ __forceinline__ uint32_t pack_two(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack_two<__nv_bfloat16>(float a, float b)
+{ __nv_bfloat162 v = __floats2bfloat162_rn(a, b); return *reinterpret_cast<uint32_t*>(&v); }
+template <> __device__ __forceinline__ uint32_t pack_two<__half>(float a, float b)
+{ __half2 v = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&v); }
+#endif
+
+// int8_rows.cu: the status word of its store checks (FMM_DEBUG build; 0 otherwise)
+fmm_status_t int8_rows_guard_read(int* code, bool clear);

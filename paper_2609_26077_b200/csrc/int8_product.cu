@@ -1,0 +1,690 @@
+// Products of the 8-bit integer layer on the tensor cores:
+//
+//   INT8    C[i][j]  = (sum_k A[i][k] B[j][k]) a_scales[i] b_scales[j] + bias[j]     codes x codes, kind::i8, exact 32-bit sums
+//   GRAD_W  dW[j][k] = sum_i dY[i][j] X[i][k]                                        16-bit operands, kind::f16, fp32 sums
+//   GRAD_X  dX[i][k] = sum_j dY[i][j] W[j][k]
+//
+// The tile's rows (TMEM lanes) run along the output's contiguous axis - output channels j of C, input channels k of the gradients - and
+// its columns along the other one, so that 32 lanes store 32 neighbouring elements straight from registers, and a product of
+// few tokens is a tile of few columns: the weight streams through the side with 128 rows whatever the number of tokens.
+//
+//               rows operand ("R")                  columns operand ("S")
+//   INT8        B (N x K), K-major                  A (M x K), K-major
+//   GRAD_W      X restored (M x K), row-major       dY (M x N), row-major     contraction over the rows of both
+//   GRAD_X      W restored (N x K), row-major       dY (M x N), K-major
+//
+// An operand whose contraction runs over its rows is loaded as it lies, in boxes of 64 rows x 128 bytes, and handed to the tensor
+// cores as MN-major; nothing is transposed in memory.  One pipeline stage is 128 bytes of contraction on both sides (128 codes, 64
+// 16-bit numbers), four MMAs.
+//
+// The 8-bit operand of a gradient is restored to 16 bits by fmm_int8_dequantize into the workspace before the product: 3 bytes a code
+// once, against 2 M N K operations.  Restoring it tile by tile on the way into the tensor cores would take two more passes
+// through shared memory per tile (codes in, 16-bit values out), which the product's own operand traffic already fills.
+#include <algorithm>
+#include "fmm_gemm_common.cuh"
+#include "int8_internal.h"
+
+namespace {
+
+enum Kind { INT8 = 0, GRAD_W = 1, GRAD_X = 2 };
+
+// [0] first bounded wait that gave up, [1] store outside its range (FMM_DEBUG build)
+__device__ int g_int8_product_status[2];
+
+__device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t cta)
+{ uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(cta)); return r; }
+__device__ __forceinline__ uint4 ld_cluster128u(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts32u(uint32_t addr, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+
+// warp-collective, as the MMAs of fmm_ptx.cuh
+template <int KIND, int NCTA>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+#define INT8_MMA(group, kind) \
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|q, 0xffffffff;\n\t" \
+                 "@q tcgen05.mma.cta_group::" group ".kind::" kind " [%0], %1, %2, %3, p;\n\t}" \
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory")
+    if (KIND == INT8) { if (NCTA == 1) INT8_MMA("1", "i8"); else INT8_MMA("2", "i8"); }
+    else { if (NCTA == 1) INT8_MMA("1", "f16"); else INT8_MMA("2", "f16"); }
+#undef INT8_MMA
+}
+// MN-major operand tile of 16-bit numbers, 128-byte swizzle: boxes of 64 k rows x 64 elements (8 KB), 8-row groups 1024 bytes apart
+constexpr int MN_BOX = 64 * 128;
+__device__ __forceinline__ uint64_t make_mnmajor_sw128_desc(uint32_t saddr)
+{
+    return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)(MN_BOX >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+template <bool MN> __device__ __forceinline__ uint64_t make_desc(uint32_t saddr) { return MN ? make_mnmajor_sw128_desc(saddr) : make_kmajor_sw128_desc(saddr); }
+
+struct ProductParams {
+    int rows, cols;                 // of the output: contiguous axis, other axis
+    int kstages;                    // 128-byte stages of the contraction
+    int tiles_r, tiles_c;
+    int k_shares;                   // cluster kernel
+    uint32_t idesc;                 // without the tile's dimensions
+    const float* r_scales; const float* c_scales; const void* bias;      // INT8
+    void* out; long long ldo;
+    int out_type, accumulate;
+    Int8Ranges ranges;
+};
+
+// contraction elements per stage
+template <int KIND> constexpr int STAGE_ELEMENTS = KIND == INT8 ? 128 : 64;
+template <int KIND> constexpr bool R_MN = KIND != INT8;
+template <int KIND> constexpr bool S_MN = KIND == GRAD_W;
+
+// Operand loads of one stage: `n` rows (K-major) or elements (MN-major) from `first`, stage ks of the contraction.
+template <bool MN, int ELEMENTS, int N, int NCTA>
+__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* tm, int first, int ks, uint32_t bar)
+{
+    if constexpr (MN) {
+        static_assert(N % 64 == 0, "whole boxes");
+#pragma unroll
+        for (int b = 0; b < N / 64; ++b) tma_load_2d<NCTA>(dst + b * MN_BOX, tm, first + 64 * b, ks * ELEMENTS, bar);
+    } else tma_load_2d<NCTA>(dst, tm, ks * ELEMENTS, first, bar);
+}
+// the four MMAs of a stage
+template <int KIND, int NCTA>
+__device__ __forceinline__ void mma_stage(uint32_t d, uint32_t r_addr, uint32_t s_addr, uint32_t idesc, bool first)
+{
+    const uint64_t rd = make_desc<R_MN<KIND>>(r_addr), sd = make_desc<S_MN<KIND>>(s_addr);
+    constexpr int RSTEP = R_MN<KIND> ? 2048 >> 4 : 32 >> 4, SSTEP = S_MN<KIND> ? 2048 >> 4 : 32 >> 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mma<KIND, NCTA>(d, rd + RSTEP * j, sd + SSTEP * j, idesc, (!first || j > 0) ? 1u : 0u);
+}
+
+// What becomes of a sum.  INT8: acc * lo * hi with the smaller scale first, so that nothing overflows on the way to a result that does
+// not (a comparison with NaN keeps both); then the bias.
+__device__ __forceinline__ float scaled(uint32_t acc, float a, float b)
+{
+    const bool first = a <= b;
+    return __int2float_rn((int)acc) * (first ? a : b) * (first ? b : a);
+}
+template <typename T> __device__ __forceinline__ void put_one(const ProductParams& p, long long at, float v)
+{
+    T* q = static_cast<T*>(p.out) + at;
+    if (!INT8_STORE_OK(p.ranges, q, sizeof(T), 2201, &g_int8_product_status[1])) return;
+    if (p.accumulate) v += to_float(*q);
+    *q = from_float<T>(v);
+}
+__device__ __forceinline__ float load_bias(const ProductParams& p, int row)
+{
+    if (!p.bias) return 0.0f;
+    if (p.out_type == FMM_TYPE_F32) return static_cast<const float*>(p.bias)[row];
+    if (p.out_type == FMM_TYPE_BF16) return to_float(static_cast<const __nv_bfloat16*>(p.bias)[row]);
+    return to_float(static_cast<const __half*>(p.bias)[row]);
+}
+// N columns from col0 of one row of the output, from a thread's registers.  c_scale: shared address of column col0's scale
+template <int KIND, int N>
+__device__ __forceinline__ void put_columns(const ProductParams& p, const uint32_t (&v)[N], int row, int col0, float r_scale, float bias, uint32_t c_scale)
+{
+    if (row >= p.rows) return;
+    auto each = [&](auto type) {
+        using T = decltype(type);
+        long long at = (long long)col0 * p.ldo + row;
+#pragma unroll
+        for (int j = 0; j < N; ++j, at += p.ldo) {
+            if (col0 + j >= p.cols) break;
+            float x;
+            if constexpr (KIND == INT8) x = scaled(v[j], r_scale, lds32f(c_scale + 4 * j)) + bias;
+            else x = __uint_as_float(v[j]);
+            put_one<T>(p, at, x);
+        }
+    };
+    if (p.out_type == FMM_TYPE_F32) each(float{});
+    else if (p.out_type == FMM_TYPE_BF16) each(__nv_bfloat16{});
+    else each(__half{});
+}
+
+// ------------------------------------------------------------------------------------------------ cluster kernel
+// One tile of 128 rows x TC columns per cluster of k_shares CTAs, each of which sums a share of the contraction; the shares meet in
+// distributed shared memory and are added in ascending order.  For products of few tiles: latency (a launch, the first load, the
+// exchange) and, with few columns, the weight's way from memory bound it, so the contraction is cut until the device is full.
+// Two CTAs fit an SM: one exchanges or waits for its first operands while the other multiplies.
+//   warps 0..3  drain TMEM, exchange, output (a TMEM lane quadrant each);  warp 4  TMA producer;  warp 5  MMA issuer
+template <int KIND, int TC>
+struct ClusterCfg {
+    static constexpr int R_BYTES = 128 * 128, S_BYTES = TC * 128, STAGE_BYTES = R_BYTES + S_BYTES;
+    static constexpr int STAGES = 98304 / STAGE_BYTES;                  // 5, 4, 4, 3 for 16, 32, 64, 128 columns
+    static constexpr int OFF_SCALES = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALES + TC * 4, NUM_BARS = 2 * STAGES + 1;
+    static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;
+    static constexpr int TMEM_COLS = TC < 32 ? 32 : TC;
+    static_assert(SMEM_BYTES + 1024 <= 233472 / 2, "two CTAs per SM");
+    static_assert(TC * 512 <= OFF_SCALES, "the exchange tile lies inside the operand ring");
+};
+
+template <int KIND, int TC>
+__global__ void __launch_bounds__(192, 2)
+int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmS, const ProductParams p)
+{
+    using C = ClusterCfg<KIND, TC>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t base = (raw_addr + 1023u) & ~1023u;       // the same offset in every CTA of the cluster
+    uint8_t* base_ptr = smem_raw + (base - raw_addr);
+    const uint32_t bar0 = base + C::OFF_BAR;
+    auto bar_full = [&](int s) { return bar0 + 8u * s; };
+    auto bar_empty = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+    const uint32_t bar_done = bar0 + 8u * (2 * C::STAGES);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + C::OFF_BAR + C::NUM_BARS * 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const Ctl ctl{abort_flag, g_int8_product_status};
+
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+        mbar_init(bar_done, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 5) {
+        tmem_alloc<1>(smem_u32(tmem_slot), C::TMEM_COLS);
+        tmem_relinquish<1>();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = warp_uniform(*tmem_slot);
+
+    const int shares = p.k_shares, rank = shares > 1 ? (int)warp_uniform(cluster_ctarank()) : 0;
+    const int tile = (int)(blockIdx.x / (unsigned)shares), tr = tile % p.tiles_r, tc = tile / p.tiles_r;
+    const int ks0 = (int)((long long)p.kstages * rank / shares), ks1 = (int)((long long)p.kstages * (rank + 1) / shares);
+    const int row0 = tr * 128, col0 = tc * TC;
+
+    if (warp == 4) {
+        int stage = 0; uint32_t phase = 0;
+        griddep_wait();
+        for (int ks = ks0; ks < ks1; ++ks) {
+            if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2301)) break;
+            if (elect_one()) {
+                const uint32_t s = base + stage * C::STAGE_BYTES;
+                mbar_expect_tx(bar_full(stage), C::STAGE_BYTES);
+                load_operand<R_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 1>(s, &tmR, row0, ks, bar_full(stage));
+                load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, TC, 1>(s + C::R_BYTES, &tmS, col0, ks, bar_full(stage));
+            }
+            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+    } else if (warp == 5) {
+        int stage = 0; uint32_t phase = 0;
+        const uint32_t idesc = p.idesc | ((uint32_t)(TC >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+        bool ok = true;
+        for (int ks = ks0; ks < ks1; ++ks) {
+            if (!mbar_wait_warp(bar_full(stage), phase, ctl, 2302)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t s = base + stage * C::STAGE_BYTES;
+            mma_stage<KIND, 1>(tmem_base, s, s + C::R_BYTES, idesc, ks == ks0);
+            tc_commit<1>(bar_empty(stage));
+            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) tc_commit<1>(bar_done);
+    } else {
+        griddep_wait();
+        const uint32_t scales = base + C::OFF_SCALES;
+        if constexpr (KIND == INT8) {
+            for (int i = threadIdx.x; i < TC; i += 128) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+        }
+        const bool ok = mbar_wait_warp(bar_done, 0, ctl, 2303);
+        tc_fence_after();
+        const uint32_t lane_taddr = tmem_base + ((uint32_t)(warp * 32) << 16);
+        constexpr int CH = TC < 32 ? TC : 32;
+        const int valid = min(TC, p.cols - col0);
+        if (shares == 1) {
+            const int row = row0 + warp * 32 + lane;
+            float r_scale = 0.0f, bias = 0.0f;
+            if constexpr (KIND == INT8) if (row < p.rows) { r_scale = p.r_scales[row]; bias = load_bias(p, row); }
+#pragma unroll 1
+            for (int c = 0; c < valid; c += CH) {
+                uint32_t v[CH];
+                if constexpr (CH == 32) tmem_ld32(lane_taddr + c, v); else tmem_ld16(lane_taddr + c, v);
+                tmem_ld_wait();
+                if (ok) put_columns<KIND, CH>(p, v, row, col0 + c, r_scale, bias, scales + 4 * c);
+            }
+        } else {
+            // column-major tile of 128 x 4 bytes a column, over the operand ring: every MMA of this CTA has read its operands
+#pragma unroll 1
+            for (int c = 0; c < valid; c += CH) {
+                uint32_t v[CH];
+                if constexpr (CH == 32) tmem_ld32(lane_taddr + c, v); else tmem_ld16(lane_taddr + c, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < CH; ++j) sts32u(base + (c + j) * 512 + (warp * 32 + lane) * 4, v[j]);
+            }
+        }
+    }
+    if (shares > 1) {
+        cluster_sync();                                      // every share is in its CTA's shared memory
+        if (warp < 4 && !*abort_flag) {
+            const int valid = min(TC, p.cols - col0), row = row0 + 4 * lane;
+            const uint32_t scales = base + C::OFF_SCALES;
+            float r_scale[4] = {}, bias[4] = {};
+            if constexpr (KIND == INT8) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (row + i < p.rows) { r_scale[i] = p.r_scales[row + i]; bias[i] = load_bias(p, row + i); }
+            }
+            // the tile's columns are dealt out to the cluster's 4 * shares warps
+            for (int c = rank * 4 + warp; c < valid; c += 4 * shares) {
+                uint4 x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) if (j < shares) x[j] = ld_cluster128u(map_to_cta(base + c * 512 + lane * 16, j));
+                uint32_t sum[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
+#pragma unroll
+                for (int j = 1; j < 8; ++j)
+                    if (j < shares) {
+                        const uint32_t y[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            sum[i] = KIND == INT8 ? sum[i] + y[i] : __float_as_uint(__uint_as_float(sum[i]) + __uint_as_float(y[i]));
+                    }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t one[1] = {sum[i]};
+                    put_columns<KIND, 1>(p, one, row + i, col0 + c, r_scale[i], bias[i], scales + 4 * c);
+                }
+            }
+        }
+    }
+    // ---------------------------------------------------------------------- teardown
+    if (*abort_flag) {
+        // let copies that are still in flight towards this CTA's shared memory land
+        const uint64_t t0 = global_timer();
+        while (global_timer() - t0 < 200000ull) __nanosleep(1000);
+    }
+    tc_fence_before();
+    if (shares > 1) cluster_sync_relaxed();                  // the peers no longer read this CTA's shared memory
+    else __syncthreads();
+    if (warp == 5) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc<1>(tmem_base, C::TMEM_COLS);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ persistent kernel
+// CTA pairs (cta_group::2) walk tiles of 256 x 256: each CTA loads its 128 rows and half of the columns, so that an operand byte
+// from L2 serves 256 multiply-accumulates.  Two TMEM accumulators: a tile is written out while the next one is multiplied.
+template <int KIND>
+struct PairCfg {
+    static constexpr int TC = 256, R_BYTES = 128 * 128, S_BYTES = 128 * 128, STAGE_BYTES = R_BYTES + S_BYTES, STAGES = 6;
+    static constexpr int OFF_SCALES = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALES + 2 * TC * 4, NUM_BARS = 2 * STAGES + 4;
+    static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;
+    static_assert(SMEM_BYTES <= 232448, "shared memory of a block");
+};
+
+template <int KIND>
+__global__ void __launch_bounds__(192, 1)
+int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmS, const ProductParams p)
+{
+    using C = PairCfg<KIND>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t base = (raw_addr + 1023u) & ~1023u;
+    uint8_t* base_ptr = smem_raw + (base - raw_addr);
+    const uint32_t bar0 = base + C::OFF_BAR;
+    auto bar_full = [&](int s) { return bar0 + 8u * s; };
+    auto bar_empty = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+    auto bar_tfull = [&](int b) { return bar0 + 8u * (2 * C::STAGES + b); };
+    auto bar_tempty = [&](int b) { return bar0 + 8u * (2 * C::STAGES + 2 + b); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + C::OFF_BAR + C::NUM_BARS * 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const Ctl ctl{abort_flag, g_int8_product_status};
+
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int rank = (int)warp_uniform(cluster_ctarank());
+    const bool leader = rank == 0;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(bar_tfull(b), 1); mbar_init(bar_tempty(b), 2 * 4); }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 5) {
+        tmem_alloc<2>(smem_u32(tmem_slot), 512);
+        tmem_relinquish<2>();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                                          // the peer's barriers are initialised before anyone signals them
+    tc_fence_after();
+    const uint32_t tmem_base = warp_uniform(*tmem_slot);
+
+    const int units = gridDim.x / 2, unit = blockIdx.x / 2;
+    const long long tiles = (long long)p.tiles_r * p.tiles_c;
+    // groups of eight tiles of rows, all columns of a group before the next: the tiles in flight share operands in L2
+    auto place = [&](long long w, int& tr, int& tc) {
+        const long long per = 8ll * p.tiles_c;
+        const int g = (int)(w / per), first = 8 * g, rows = min(8, p.tiles_r - first), in = (int)(w - g * per);
+        tr = first + in % rows;
+        tc = in / rows;
+    };
+
+    if (warp == 4) {
+        int stage = 0; uint32_t phase = 0;
+        bool ok = true;
+        griddep_wait();
+        for (long long w = unit; w < tiles && ok; w += units) {
+            int tr, tc;
+            place(w, tr, tc);
+            for (int ks = 0; ks < p.kstages; ++ks) {
+                if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2311)) { ok = false; break; }
+                // completion is counted on the even CTA's barrier; only that CTA arms it
+                const uint32_t fb = bar_full(stage) & PEER_BIT_MASK;
+                if (elect_one()) {
+                    const uint32_t s = base + stage * C::STAGE_BYTES;
+                    if (leader) mbar_expect_tx(bar_full(stage), 2 * C::STAGE_BYTES);
+                    load_operand<R_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 2>(s, &tmR, (2 * tr + rank) * 128, ks, fb);
+                    load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 2>(s + C::R_BYTES, &tmS, (2 * tc + rank) * 128, ks, fb);
+                }
+                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 5) {
+        if (leader) {
+            int stage = 0, buf = 0; uint32_t phase = 0, bphase = 0;
+            const uint32_t idesc = p.idesc | ((uint32_t)(C::TC >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
+            bool ok = true;
+            for (long long w = unit; w < tiles && ok; w += units) {
+                if (!mbar_wait_warp(bar_tempty(buf), bphase ^ 1u, ctl, 2312)) break;
+                tc_fence_after();
+                for (int ks = 0; ks < p.kstages; ++ks) {
+                    if (!mbar_wait_warp(bar_full(stage), phase, ctl, 2313)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t s = base + stage * C::STAGE_BYTES;
+                    mma_stage<KIND, 2>(tmem_base + buf * C::TC, s, s + C::R_BYTES, idesc, ks == 0);
+                    tc_commit<2>(bar_empty(stage));
+                    if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                }
+                if (!ok) break;
+                tc_commit<2>(bar_tfull(buf));
+                if (++buf == 2) { buf = 0; bphase ^= 1u; }
+            }
+        }
+    } else {
+        int buf = 0; uint32_t bphase = 0;
+        griddep_wait();
+        for (long long w = unit; w < tiles; w += units) {
+            int tr, tc;
+            place(w, tr, tc);
+            const int row = (2 * tr + rank) * 128 + warp * 32 + lane, col0 = tc * C::TC;
+            const uint32_t scales = base + C::OFF_SCALES + buf * C::TC * 4;
+            float r_scale = 0.0f, bias = 0.0f;
+            if constexpr (KIND == INT8) {
+                // (a warp is at most one tile behind the others, and the scales of two tiles are kept)
+                for (int i = threadIdx.x; i < C::TC; i += 128) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                if (row < p.rows) { r_scale = p.r_scales[row]; bias = load_bias(p, row); }
+            }
+            if (!mbar_wait_warp(bar_tfull(buf), bphase, ctl, 2314)) break;
+            tc_fence_after();
+            const uint32_t taddr = tmem_base + buf * C::TC + ((uint32_t)(warp * 32) << 16);
+            const int valid = min(C::TC, p.cols - col0);
+#pragma unroll 1
+            for (int c = 0; c < valid; c += 32) {
+                uint32_t v[32];
+                tmem_ld32(taddr + c, v);
+                tmem_ld_wait();
+                put_columns<KIND, 32>(p, v, row, col0 + c, r_scale, bias, scales + 4 * c);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(bar_tempty(buf) & PEER_BIT_MASK);
+            if (++buf == 2) { buf = 0; bphase ^= 1u; }
+        }
+    }
+    // ---------------------------------------------------------------------- teardown
+    if (*abort_flag) {
+        const uint64_t t0 = global_timer();
+        while (global_timer() - t0 < 200000ull) __nanosleep(1000);
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                                          // the peer no longer signals this CTA's barriers
+    if (warp == 5) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc<2>(tmem_base, 512);
+    }
+}
+
+// An empty contraction: C = bias, or 0
+__global__ void __launch_bounds__(256) empty_sum_kernel(const ProductParams p)
+{
+    const long long n = (long long)p.rows * p.cols;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const int col = (int)(i / p.rows), row = (int)(i - (long long)col * p.rows);
+        const float v = load_bias(p, row);
+        const long long at = (long long)col * p.ldo + row;
+        if (p.out_type == FMM_TYPE_F32) put_one<float>(p, at, v);
+        else if (p.out_type == FMM_TYPE_BF16) put_one<__nv_bfloat16>(p, at, v);
+        else put_one<__half>(p, at, v);
+    }
+}
+
+// 16-bit rows of any alignment, copied to rows that a tensor map can read
+__global__ void __launch_bounds__(256) realign_kernel(const uint16_t* x, long long ldx, uint16_t* y, long long ldy, int rows, int cols)
+{
+    for (long long row = blockIdx.x; row < rows; row += gridDim.x)
+        for (int c = threadIdx.x; c < cols; c += 256) y[row * ldy + c] = x[row * ldx + c];
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+struct Operand { const void* p; int64_t rows, cols, ld; };        // row-major, cols contiguous; ld in elements
+
+template <int KIND, bool MN>
+bool make_operand_map(CUtensorMap* tm, const Operand& o, int n)
+{
+    const CUtensorMapDataType dt = KIND == INT8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
+    const int e = KIND == INT8 ? 1 : 2;
+    return make_map_2d(tm, dt, e, o.p, (uint64_t)o.cols, (uint64_t)o.rows, MN ? 64 : 128 / e, MN ? 64 : n, CU_TENSOR_MAP_SWIZZLE_128B, (uint64_t)o.ld);
+}
+
+// The kernel's shared memory limit, raised once per device.
+template <typename K> bool raise_smem(K kernel, int bytes, std::atomic<bool>* done)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return false; }
+    if (dev < 64 && done[dev].load(std::memory_order_acquire)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) { cudaGetLastError(); return false; }
+    if (dev < 64) done[dev].store(true, std::memory_order_release);
+    return true;
+}
+
+template <typename K>
+fmm_status_t launch_kernel(K kernel, unsigned grid, int smem, unsigned cluster, const CUtensorMap& r, const CUtensorMap& s, const ProductParams& p, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(192); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, r, s, p) != cudaSuccess) { cudaGetLastError(); return FMM_ERR_CUDA; }
+    return FMM_OK;
+}
+
+template <int KIND, int TC>
+fmm_status_t launch_cluster(ProductParams p, const Operand& r, const Operand& s, int shares, cudaStream_t st)
+{
+    using C = ClusterCfg<KIND, TC>;
+    static std::atomic<bool> done[64];
+    CUtensorMap tmR, tmS;
+    if (!make_operand_map<KIND, R_MN<KIND>>(&tmR, r, 128) || !make_operand_map<KIND, S_MN<KIND>>(&tmS, s, TC) ||
+        !raise_smem(int8_cluster_kernel<KIND, TC>, C::SMEM_BYTES, done)) return FMM_ERR_CUDA;
+    p.tiles_r = (p.rows + 127) / 128; p.tiles_c = (p.cols + TC - 1) / TC; p.k_shares = shares;
+    const int64_t grid = (int64_t)p.tiles_r * p.tiles_c * shares;
+    if (grid > 0x7FFFFFFF) return FMM_ERR_SHAPE;
+    return launch_kernel(int8_cluster_kernel<KIND, TC>, (unsigned)grid, C::SMEM_BYTES, (unsigned)shares, tmR, tmS, p, st);
+}
+
+template <int KIND>
+fmm_status_t launch_pair(ProductParams p, const Operand& r, const Operand& s, cudaStream_t st)
+{
+    using C = PairCfg<KIND>;
+    static std::atomic<bool> done[64];
+    CUtensorMap tmR, tmS;
+    if (!make_operand_map<KIND, R_MN<KIND>>(&tmR, r, 128) || !make_operand_map<KIND, S_MN<KIND>>(&tmS, s, 128) ||
+        !raise_smem(int8_pair_kernel<KIND>, C::SMEM_BYTES, done)) return FMM_ERR_CUDA;
+    p.tiles_r = (p.rows + 255) / 256; p.tiles_c = (p.cols + 255) / 256; p.k_shares = 1;
+    // as few pairs as finish in the same number of waves
+    const int64_t tiles = (int64_t)p.tiles_r * p.tiles_c, most = std::max(1, fmm_sm_count() / 2), waves = (tiles + most - 1) / most;
+    return launch_kernel(int8_pair_kernel<KIND>, (unsigned)((tiles + waves - 1) / waves * 2), C::SMEM_BYTES, 2, tmR, tmS, p, st);
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+template <int KIND>
+fmm_status_t launch_product(const ProductParams& p, const Operand& r, const Operand& s, cudaStream_t st)
+{
+    const int sms = fmm_sm_count();
+    const int64_t pairs = ceil_div(p.rows, 256) * ceil_div(p.cols, 256);
+    if (pairs >= sms / 4) return launch_pair<KIND>(p, r, s, st);
+    int tc = 128;
+    if (KIND == INT8) { if (p.cols <= 16) tc = 16; else if (p.cols <= 32) tc = 32; }
+    if (tc == 128 && (p.cols <= 64 || ceil_div(p.rows, 128) * ceil_div(p.cols, 128) < sms)) tc = 64;
+    const int64_t tiles = ceil_div(p.rows, 128) * ceil_div(p.cols, tc);
+    int shares = 1;
+    while (shares < 8 && tiles * shares * 2 <= 2 * sms && p.kstages >= 4 * shares) shares *= 2;
+    if constexpr (KIND == INT8) {
+        if (tc == 16) return launch_cluster<KIND, 16>(p, r, s, shares, st);
+        if (tc == 32) return launch_cluster<KIND, 32>(p, r, s, shares, st);
+    }
+    return tc == 64 ? launch_cluster<KIND, 64>(p, r, s, shares, st) : launch_cluster<KIND, 128>(p, r, s, shares, st);
+}
+
+fmm_status_t launch_empty(const ProductParams& p, cudaStream_t st)
+{
+    empty_sum_kernel<<<(unsigned)fmm_sm_count() * 8, 256, 0, st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? FMM_OK : FMM_ERR_CUDA;
+}
+
+bool dim_ok(int64_t n) { return n >= 0 && n < INT8_MAX_DIM; }
+int64_t up_to(int64_t n, int64_t a) { return ceil_div(n, a) * a; }
+
+struct GradWorkspace { int64_t ld_codes, ld_dy; size_t dy, total; };       // elements, elements, bytes, bytes
+GradWorkspace grad_workspace(int64_t code_rows, int64_t K, int64_t M, int64_t N, bool dy_aligned)
+{
+    GradWorkspace w;
+    w.ld_codes = up_to(K, 8);
+    w.ld_dy = up_to(N, 8);
+    w.dy = (size_t)up_to(code_rows * w.ld_codes * 2, 256);
+    w.total = w.dy + (dy_aligned ? 0 : (size_t)up_to(M * w.ld_dy * 2, 256));
+    return w;
+}
+
+// Both gradients: `codes` (code_rows x K) restored to `type` in the workspace, dY realigned there if it has to be, one product.
+template <int KIND>
+fmm_status_t grad(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* codes, int64_t ldc, const float* scales, int64_t M, int64_t N, int64_t K,
+                  void* out, fmm_type_t out_type, int64_t ldo, int accumulate, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (type != FMM_TYPE_BF16 && type != FMM_TYPE_F16) return FMM_ERR_INVALID_ARG;
+    if (out_type != FMM_TYPE_F32 && out_type != type) return FMM_ERR_INVALID_ARG;
+    if (!dim_ok(M) || !dim_ok(N) || !dim_ok(K)) return FMM_ERR_SHAPE;
+    const int64_t code_rows = KIND == GRAD_W ? M : N, contraction = code_rows, cols = KIND == GRAD_W ? N : M;
+    if (K == 0 || cols == 0) return FMM_OK;
+    const int eo = int8_type_bytes(out_type);
+    if (!out || ldo < K || ((uintptr_t)out & (eo - 1))) return FMM_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    ProductParams p = {};
+    p.rows = (int)K; p.cols = (int)cols;
+    p.out = out; p.ldo = ldo; p.out_type = out_type; p.accumulate = accumulate != 0;
+    int8_add_range(p.ranges, out, cols, K, ldo, eo);
+    if (contraction == 0) return accumulate ? FMM_OK : launch_empty(p, st);
+    if (!dY || ldy < N || ((uintptr_t)dY & 1) || !codes || ldc < K || !scales || ((uintptr_t)scales & 3)) return FMM_ERR_INVALID_ARG;
+    const bool dy_aligned = int8_aligned(dY, ldy * 2, 16);
+    const GradWorkspace w = grad_workspace(code_rows, K, M, N, dy_aligned);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < w.total) return FMM_ERR_WORKSPACE;
+    fmm_status_t s = fmm_int8_dequantize(codes, ldc, scales, code_rows, K, 0, workspace, type, w.ld_codes, stream);
+    if (s != FMM_OK) return s;
+    Operand dy = {dY, M, N, ldy};
+    if (!dy_aligned) {
+        uint16_t* copy = reinterpret_cast<uint16_t*>(static_cast<char*>(workspace) + w.dy);
+        realign_kernel<<<(unsigned)std::min<int64_t>(M, (int64_t)fmm_sm_count() * 8), 256, 0, st>>>(static_cast<const uint16_t*>(dY), ldy, copy, w.ld_dy, (int)M, (int)N);
+        if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;
+        dy = {copy, M, N, w.ld_dy};
+    }
+    const uint32_t format = type == FMM_TYPE_BF16 ? 1u : 0u;
+    p.kstages = (int)ceil_div(contraction, 64);
+    p.idesc = (1u << 4) | (format << 7) | (format << 10) | (1u << 15) | ((KIND == GRAD_W ? 1u : 0u) << 16);
+    return launch_product<KIND>(p, {workspace, code_rows, K, w.ld_codes}, dy, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+fmm_status_t fmm_int8_matmul(const int8_t* A, int64_t lda, const float* a_scales, const int8_t* B, int64_t ldb, const float* b_scales,
+                             const void* bias, int64_t M, int64_t N, int64_t K, void* Cm, fmm_type_t type, int64_t ldc, void* stream)
+{
+    if (!int8_type_ok(type)) return FMM_ERR_INVALID_ARG;
+    if (!dim_ok(M) || !dim_ok(N) || K < 0 || K > 131071) return FMM_ERR_SHAPE;
+    if (M == 0 || N == 0) return FMM_OK;
+    const int e = int8_type_bytes(type);
+    if (!Cm || ldc < N || ((uintptr_t)Cm & (e - 1)) || ((uintptr_t)bias & (e - 1))) return FMM_ERR_INVALID_ARG;
+    ProductParams p = {};
+    p.rows = (int)N; p.cols = (int)M;
+    p.r_scales = b_scales; p.c_scales = a_scales; p.bias = bias;
+    p.out = Cm; p.ldo = ldc; p.out_type = type;
+    int8_add_range(p.ranges, Cm, M, N, ldc, e);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (K == 0) return launch_empty(p, st);
+    if (!A || !B || !a_scales || !b_scales || (((uintptr_t)a_scales | (uintptr_t)b_scales) & 3) || lda < K || ldb < K ||
+        !int8_aligned(A, lda, 16) || !int8_aligned(B, ldb, 16)) return FMM_ERR_INVALID_ARG;
+    p.kstages = (int)ceil_div(K, 128);
+    p.idesc = (2u << 4) | (1u << 7) | (1u << 10);
+    return launch_product<INT8>(p, {B, N, K, ldb}, {A, M, K, lda}, st);
+}
+
+fmm_status_t fmm_int8_grad_workspace_bytes(int64_t code_rows, int64_t K, int64_t M, int64_t N, int dy_aligned, size_t* bytes)
+{
+    if (!bytes) return FMM_ERR_INVALID_ARG;
+    if (!dim_ok(code_rows) || !dim_ok(K) || !dim_ok(M) || !dim_ok(N)) return FMM_ERR_SHAPE;
+    *bytes = grad_workspace(code_rows, K, M, N, dy_aligned != 0).total;
+    return FMM_OK;
+}
+
+fmm_status_t fmm_int8_grad_weight(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* X, int64_t ldx, const float* x_scales, int64_t M, int64_t N,
+                                  int64_t K, void* dW, fmm_type_t out_type, int64_t ldw, int accumulate, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return grad<GRAD_W>(dY, type, ldy, X, ldx, x_scales, M, N, K, dW, out_type, ldw, accumulate, workspace, workspace_bytes, stream);
+}
+
+fmm_status_t fmm_int8_grad_input(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* W, int64_t ldw, const float* w_scales, int64_t M, int64_t N,
+                                 int64_t K, void* dX, fmm_type_t out_type, int64_t ldx, void* workspace, size_t workspace_bytes, void* stream)
+{
+    return grad<GRAD_X>(dY, type, ldy, W, ldw, w_scales, M, N, K, dX, out_type, ldx, 0, workspace, workspace_bytes, stream);
+}
+
+fmm_status_t fmm_int8_status(int* code)
+{
+    if (!code) return FMM_ERR_INVALID_ARG;
+    *code = 0;
+    int words[2] = {0, 0}, rows = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(words, g_int8_product_status, sizeof(words)) != cudaSuccess) {
+        cudaGetLastError();
+        return FMM_ERR_CUDA;
+    }
+    const fmm_status_t s = int8_rows_guard_read(&rows, false);
+    if (s != FMM_OK) return s;
+    *code = words[0] ? words[0] : words[1] ? words[1] : rows;
+    return words[0] ? FMM_ERR_DEVICE_TIMEOUT : FMM_OK;
+}
+
+fmm_status_t fmm_int8_status_clear(void)
+{
+    const int zero[2] = {0, 0};
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyToSymbol(g_int8_product_status, zero, sizeof(zero)) != cudaSuccess) {
+        cudaGetLastError();
+        return FMM_ERR_CUDA;
+    }
+    int unused = 0;
+    return int8_rows_guard_read(&unused, true);
+}
+
+}  // extern "C"
