@@ -17,7 +17,8 @@
  *     into CUDA graphs.  Results do not depend on the run: no floating-point atomics, every sum in a fixed order.
  *   - Matrices are row-major; `ld*` is the distance between rows in elements, at least the number of columns.  Any
  *     alignment that their type allows is accepted where nothing else is said (16-byte aligned rows are read and
- *     written fastest).  Elements behind the last column of a row are neither read nor written.
+ *     written fastest).  Nothing is written behind the last column of a row, and nothing read but what shares an
+ *     aligned 16-byte vector with an element of the row.
  *   - Rows and columns may be 0: then nothing is read, and what an empty sum gives is written.
  *   - An output may not overlap an input or another output, except where it is said.
  *   - workspace: dev, 256-byte aligned, caller-owned; calls that share one must be stream-ordered.

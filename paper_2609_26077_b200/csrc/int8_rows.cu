@@ -5,6 +5,7 @@
 // A thread owns groups of eight consecutive columns (16 bytes of a 16-bit type); group v of a row is thread v mod NT, so
 // that a block of 32 (128) columns is 4 (16) neighbouring lanes of one warp and its maximum takes 2 (4) shuffles.
 #include <math.h>
+#include "fmm_ptx.cuh"
 #include "int8_internal.h"
 
 namespace {
@@ -15,66 +16,107 @@ __device__ int g_int8_rows_guard;
 #define ROW_STORE_OK(ptr, bytes, code) INT8_STORE_OK(p.ranges, ptr, bytes, code, &g_int8_rows_guard)
 
 // ---------------------------------------------------------------------------------------- eight columns of a row
-template <typename T> struct Raw8 { uint32_t w[sizeof(T) * 2]; };
+// Kernels exist for rows that all start on 16-byte boundaries and have a multiple of eight columns (AL: all of a thread's eight exist,
+// or none), and for any.  In the second kind a row is read by the aligned 16-byte vectors that hold an element of it, and a thread's eight columns are shifted out of two (fp32: three) of them; it is
+// written the same way, neighbouring lanes passing on what belongs to the other's vector; so an output in an input's place holds: a
+// lane stores its neighbour's columns only with that lane's numbers, and what else a vector held of others is not used.  (1000 rows of 4095 fp16 columns through the
+// norm: 19.3 us element by element, 8.3 this way.)  The offset `m` of a row within its vector is the same for all its columns.
+template <typename T, bool AL> struct Raw8 { uint32_t w[AL ? sizeof(T) * 2 : sizeof(T) * 2 + 4]; };
 
-// columns [0, n) of p, zeros behind; n may be 0 or less.  vec: p is 16-byte aligned
-template <typename T> __device__ __forceinline__ Raw8<T> load8(const T* p, int n, bool vec)
+template <typename T> __device__ __forceinline__ int row_offset(const T* row) { return (int)(((uintptr_t)row & 15) / sizeof(T)); }
+
+// columns [col, col + 8) of a row of which n are left from col on (0 or less: none is read, zeros)
+template <typename T, bool AL> __device__ __forceinline__ Raw8<T, AL> load8(const T* row, int col, int n)
 {
-    Raw8<T> r;
-    if (vec && n >= 8) {
+    constexpr int PER = 16 / sizeof(T);
+    const int m = AL ? 0 : row_offset(row);
+    const uint4* p = reinterpret_cast<const uint4*>(row + col - m);
+    Raw8<T, AL> r;
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-            const uint4 v = reinterpret_cast<const uint4*>(p)[i];
-            r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
-        }
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r.w[i] = i < n ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
-    } else {
-        const uint16_t* s = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.w[i] = (2 * i < n ? (uint32_t)s[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)s[2 * i + 1] << 16 : 0u);
+    for (int i = 0; i < 8 / PER + (AL ? 0 : 1); ++i) {
+        const bool some = AL || i == 0 ? n > 0 : i * PER < m + 8 && n > i * PER - m;
+        const uint4 v = some ? p[i] : make_uint4(0u, 0u, 0u, 0u);
+        r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
     }
     return r;
 }
-template <typename T> __device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&f)[8])
+// w[i] = words [shift, shift + N) of w, shift in units of `T` below 16 bytes' worth
+template <typename T, int N, int M> __device__ __forceinline__ void shift_words(uint32_t (&w)[M], int shift)
 {
-    if constexpr (sizeof(T) == 4) {
+    constexpr int TWO = sizeof(T) == 4 ? 2 : 4, ONE = TWO / 2;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(r.w[i]);
-    } else {
+    for (int i = 0; i + 2 < M; ++i) w[i] = shift & TWO ? w[i + 2] : w[i];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            T a, b;
-            const uint16_t lo = (uint16_t)r.w[i], hi = (uint16_t)(r.w[i] >> 16);
-            a = *reinterpret_cast<const T*>(&lo); b = *reinterpret_cast<const T*>(&hi);
-            f[2 * i] = to_float(a); f[2 * i + 1] = to_float(b);
+    for (int i = 0; i + 1 < M; ++i) w[i] = shift & ONE ? w[i + 1] : w[i];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = shift & 1 ? __funnelshift_r(w[i], w[i + 1], 16) : w[i];
+    }
+}
+// the eight numbers, zeros for those behind the row's end.  m: row_offset
+template <typename T, bool AL> __device__ __forceinline__ void unpack8(const Raw8<T, AL>& r, int m, int n, float (&f)[8])
+{
+    constexpr int N = sizeof(T) * 2;
+    uint32_t w[AL ? N : N + 4];
+#pragma unroll
+    for (int i = 0; i < (AL ? N : N + 4); ++i) w[i] = r.w[i];
+    if constexpr (!AL) shift_words<T, N>(w, m);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) f[i] = __uint_as_float(w[i]);
+        else {
+            const uint16_t h = (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2]);
+            f[i] = to_float(*reinterpret_cast<const T*>(&h));
         }
     }
-}
-template <typename T> __device__ __forceinline__ Raw8<T> pack8(const float (&f)[8])
-{
-    Raw8<T> r;
-    if constexpr (sizeof(T) == 4) {
+    if (!AL && n < 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(f[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.w[i] = pack_two<T>(f[2 * i], f[2 * i + 1]);
+        for (int i = 0; i < 8; ++i) f[i] = i < n ? f[i] : 0.0f;
     }
-    return r;
 }
-template <typename T, typename P> __device__ __forceinline__ void store8(T* q, const float (&f)[8], int n, bool vec, const P& p, int code)
+// Columns [col, col + 8) of a row of which n are left.  Every lane of the warp calls it, lane l + 1 for the next eight columns.
+template <typename T, bool AL, typename P> __device__ __forceinline__ void store8(T* row, int col, int n, const float (&f)[8], const P& p, int code)
 {
-    if (n <= 0 || !ROW_STORE_OK(q, (n < 8 ? n : 8) * sizeof(T), code)) return;
-    if (vec && n >= 8) {
-        const Raw8<T> r = pack8<T>(f);
+    constexpr int N = sizeof(T) * 2;
+    uint32_t w[N + 4 + N];                                    // (aligned: the first N)
+    uint32_t* own = w + (AL ? 0 : N);
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-            reinterpret_cast<uint4*>(q)[i] = make_uint4(r.w[4 * i], r.w[4 * i + 1], r.w[4 * i + 2], r.w[4 * i + 3]);
+    for (int i = 0; i < N; ++i) {
+        if constexpr (sizeof(T) == 4) own[i] = __float_as_uint(f[i]);
+        else own[i] = pack_two<T>(f[2 * i], f[2 * i + 1]);
+    }
+    T* q = row + col;
+    auto store_vectors = [&](T* at) {
+        if (!ROW_STORE_OK(at, 8 * sizeof(T), code)) return;
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) reinterpret_cast<uint4*>(at)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    };
+    auto store_some = [&](int from, int to) {                 // elements [from, to) that exist, one by one
+        if (from >= min(to, n) || !ROW_STORE_OK(q + from, (min(to, n) - from) * sizeof(T), code)) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i >= from && i < to && i < n) q[i] = from_float<T>(f[i]);
+    };
+    if constexpr (AL) {
+        if (n > 0) store_vectors(q);
     } else {
+        // this lane's vectors hold the last m elements of the lane before and the first 8 - m of its own
+        const int m = row_offset(row), lane = threadIdx.x & 31;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < n) q[i] = from_float<T>(f[i]);
+        for (int i = 0; i < N; ++i) w[i] = __shfl_up_sync(0xffffffffu, own[i], 1);
+        if (m == 0 ? n >= 8 : lane > 0 && n >= 8 - m) {
+            if (m == 0) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) w[i] = own[i];
+            } else if constexpr (sizeof(T) == 4) {
+                // 8 - m words on: 4, then 4 - m
+#pragma unroll
+                for (int i = 0; i < 2 * N - 4; ++i) w[i] = w[i + 4];
+                shift_words<T, N>(w, 4 - m);
+            } else shift_words<T, N>(w, 8 - m);
+            store_vectors(q - m);
+        } else store_some(0, 8 - m);
+        // the last m elements are the next lane's to store, unless there is none or its vectors are not whole
+        if (m > 0 && (lane == 31 || n - 8 < 8 - m)) store_some(8 - m, 8);
     }
 }
 // eight codes; vec: 8-byte aligned
@@ -95,10 +137,12 @@ template <typename P> __device__ __forceinline__ void store_codes8(int8_t* q, ui
         for (int i = 0; i < 8; ++i) if (i < n) q[i] = (int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
     }
 }
+// code + 128 as the last byte of 2^23 + that, less 2^23 + 128: two instructions at full rate, a conversion has a quarter of it
 __device__ __forceinline__ void codes_to_float(uint2 c, float (&f)[8])
 {
+    const uint32_t w[2] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)(int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(__byte_perm(w[i >> 2], 0x4B000000u, 0x7540 | (i & 3))) - 8388736.0f;
 }
 
 // ---------------------------------------------------------------------------------------- quantization of a block
@@ -138,16 +182,45 @@ __device__ __forceinline__ uint2 codes8(const float (&f)[8], float inverse)
     auto four = [&](int o) { return __byte_perm(__byte_perm(b[o], b[o + 1], 0x0040), __byte_perm(b[o + 2], b[o + 3], 0x0040), 0x5410); };
     return make_uint2(four(0), four(4));
 }
-// maximum over aligned groups of `lanes` (4, 16 or 32) lanes
-__device__ __forceinline__ uint32_t group_max(uint32_t m, int lanes)
+// Maxima of N groups of eight columns to those of the blocks they lie in, a block being `lanes` (4 or 16) neighbouring lanes, and the
+// blocks' scales.  A block's lanes share the divisions out (two IEEE divisions per block and thread made the quantization of 16384 x
+// 8192 bf16 numbers take 118 us instead of 66).
+template <int N> __device__ __forceinline__ void block_scales(uint32_t (&m)[N], int lanes, bool pow2, Scale (&s)[N])
 {
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
-    m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-    if (lanes > 4) {
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 4));
-        m = max(m, __shfl_xor_sync(0xffffffffu, m, 8));
+    static_assert(N == 1 || N == 2 || N == 4, "groups of a thread");
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        m[i] = max(m[i], __shfl_xor_sync(0xffffffffu, m[i], 1));
+        m[i] = max(m[i], __shfl_xor_sync(0xffffffffu, m[i], 2));
+        if (lanes > 4) {
+            m[i] = max(m[i], __shfl_xor_sync(0xffffffffu, m[i], 4));
+            m[i] = max(m[i], __shfl_xor_sync(0xffffffffu, m[i], 8));
+        }
     }
-    return m;
+    const int lane = threadIdx.x & 31, k = lane & (lanes - 1), first = lane - k;
+    uint32_t mine = m[0];
+    if (N > 1) mine = k & 1 ? m[1] : mine;
+    if (N > 2) mine = (k & 2 ? (k & 1 ? m[N - 1] : m[N / 2]) : mine);
+    if (pow2 || lanes < 2 * N) {
+        // lane k: both numbers of group k
+        const Scale own = block_scale(mine, pow2);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[i].scale = __shfl_sync(0xffffffffu, own.scale, first + i);
+            s[i].inverse = __shfl_sync(0xffffffffu, own.inverse, first + i);
+        }
+    } else {
+        // lane k: the scale of group k, lane N + k its inverse
+        const bool inverse = k & N, finite = mine < 0x7F800000u;
+        const float a = __uint_as_float(max(mine, __float_as_uint(1e-12f)));
+        float x = __fdiv_rn(inverse ? 127.0f : a, inverse ? a : 127.0f);
+        if (!finite) x = inverse ? 0.0f : __uint_as_float(0x7FC00000u);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            s[i].scale = __shfl_sync(0xffffffffu, x, first + i);
+            s[i].inverse = __shfl_sync(0xffffffffu, x, first + N + i);
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------- sums over a row's threads
@@ -187,83 +260,94 @@ struct RowsParams {
     int64_t ldx, ldr, ldh, ldc, ldk;
     double eps;
     int rows, cols, block;                    // block: of the checkpoint, 0: none
-    bool pow2, vx, vr, vg, vh, vc, vk;        // which arrays have aligned rows
+    bool pow2, aligned, vc, vk;               // aligned: AL for x, residual, gain and hidden; vc, vk: of codes and checkpoint, to 8 bytes
     Int8Ranges ranges;
 };
 
-template <typename T> __device__ __forceinline__ void checkpoint8(const RowsParams& p, int64_t row, int col, const float (&h)[8])
+// N groups of eight columns, at col, col + step, ...
+template <int N> __device__ __forceinline__ void checkpoint8(const RowsParams& p, int64_t row, int col, int step, const float (&h)[N][8])
 {
-    const int lanes = p.block / 8, n = p.cols - col;
-    const Scale s = block_scale(group_max(abs_max8(h), lanes), false);
-    if (n <= 0) return;
-    store_codes8(p.checkpoint + row * p.ldk + col, codes8(h, s.inverse), n, p.vk, p, 2101);
-    if ((col / 8) % lanes == 0) {
-        float* q = p.checkpoint_scales + row * ((p.cols + p.block - 1) / p.block) + col / p.block;
-        if (ROW_STORE_OK(q, 4, 2102)) *q = s.scale;
+    const int shift = p.block == 32 ? 5 : 7, lanes = 1 << (shift - 3), per_row = (p.cols + p.block - 1) >> shift;
+    uint32_t m[N];
+    Scale s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) m[i] = abs_max8(h[i]);
+    block_scales(m, lanes, false, s);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int c = col + i * step, n = p.cols - c;
+        if (n <= 0) continue;
+        store_codes8(p.checkpoint + row * p.ldk + c, codes8(h[i], s[i].inverse), n, p.vk, p, 2101);
+        if ((c & (p.block - 1)) == 0) {
+            float* q = p.checkpoint_scales + row * per_row + (c >> shift);
+            if (ROW_STORE_OK(q, 4, 2102)) *q = s[i].scale;
+        }
     }
 }
 
 // A row per NT threads, held in registers: VPT groups of eight columns a thread.  The squares are summed in fp64 (they are
 // exact there), so that the reciprocal root does not depend on the order of the sum and codes are the same on every machine.
-template <typename T, bool NORM, int NT, int VPT>
+template <typename T, bool NORM, bool AL, int NT, int VPT>
 __global__ void __launch_bounds__(NT == 32 ? 128 : NT) rows_kernel(const RowsParams p)
 {
     __shared__ double red_sum[32];
     __shared__ uint32_t red_max[32];
     constexpr int RPC = NT == 32 ? 4 : 1;
     const int t = threadIdx.x;
-    int64_t row = (int64_t)blockIdx.x * RPC + threadIdx.y;
+    const int64_t row = (int64_t)blockIdx.x * RPC + threadIdx.y;
     if (RPC > 1 && row >= p.rows) return;                     // whole warps
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    const int mx = AL ? 0 : row_offset(x);
     float h[VPT][8];
-    Raw8<T> raw[VPT];
+    Raw8<T, AL> raw[VPT];
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); raw[i] = load8(x + col, p.cols - col, p.vx); }
+    for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); raw[i] = load8<T, AL>(x, col, p.cols - col); }
     if constexpr (NORM) {
         if (p.residual) {
             const T* r = static_cast<const T*>(p.residual) + row * p.ldr;
-            Raw8<T> rawr[VPT];
+            const int mr = AL ? 0 : row_offset(r);
+            Raw8<T, AL> rawr[VPT];
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); rawr[i] = load8(r + col, p.cols - col, p.vr); }
+            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); rawr[i] = load8<T, AL>(r, col, p.cols - col); }
             T* hid = static_cast<T*>(p.hidden) + row * p.ldh;
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int col = 8 * (i * NT + t);
+                const int n = p.cols - 8 * (i * NT + t);
                 float b[8];
-                unpack8(raw[i], h[i]);
-                unpack8(rawr[i], b);
+                unpack8<T, AL>(raw[i], mx, n, h[i]);
+                unpack8<T, AL>(rawr[i], mr, n, b);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[i][j] = __fadd_rn(h[i][j], b[j]);
-                store8(hid + col, h[i], p.cols - col, p.vh, p, 2103);
             }
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); store8<T, AL>(hid, col, p.cols - col, h[i], p, 2103); }
         } else {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) unpack8(raw[i], h[i]);
+            for (int i = 0; i < VPT; ++i) unpack8<T, AL>(raw[i], mx, p.cols - 8 * (i * NT + t), h[i]);
         }
+        const T* gain = static_cast<const T*>(p.gain);
+        const int mg = AL ? 0 : row_offset(gain);
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); raw[i] = load8(static_cast<const T*>(p.gain) + col, p.cols - col, p.vg); }
+        for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); raw[i] = load8<T, AL>(gain, col, p.cols - col); }
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) { const double v = (double)h[i][j]; sum = fma(v, v, sum); }
-        if (p.block) {
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) checkpoint8<T>(p, row, 8 * (i * NT + t), h[i]);
-        }
+        if (p.block) checkpoint8<VPT>(p, row, 8 * t, 8 * NT, h);
         sum = row_sum<NT>(sum, red_sum);
         const float rstd = (float)(1.0 / sqrt(sum / (double)p.cols + p.eps));
         if (t == 0 && p.rstd && ROW_STORE_OK(p.rstd + row, 4, 2104)) p.rstd[row] = rstd;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             float g[8];
-            unpack8(raw[i], g);
+            unpack8<T, AL>(raw[i], mg, p.cols - 8 * (i * NT + t), g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] = __fmul_rn(__fmul_rn(h[i][j], rstd), g[j]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) unpack8(raw[i], h[i]);
+        for (int i = 0; i < VPT; ++i) unpack8<T, AL>(raw[i], mx, p.cols - 8 * (i * NT + t), h[i]);
     }
     // behind the last column: h is 0 there, and 0 * rstd is NaN where rstd is infinite (a row of zeros with eps 0), which is what
     // the row's own zeros are as well
@@ -281,22 +365,23 @@ __global__ void __launch_bounds__(NT == 32 ? 128 : NT) rows_kernel(const RowsPar
 }
 
 // Rows that do not fit registers: read again for each pass (from L2, mostly).  hidden may be x or residual, so it is written in the
-// last pass.
-template <typename T, bool NORM>
+// last pass.  Every lane goes round as often, as lanes exchange numbers.
+template <typename T, bool NORM, bool AL>
 __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
 {
     constexpr int NT = 1024;
     __shared__ double red_sum[32];
     __shared__ uint32_t red_max[32];
     const int64_t row = blockIdx.x;
-    const int t = threadIdx.x, groups = (p.cols + 7) / 8;
+    const int t = threadIdx.x, end = (p.cols + 8 * NT - 1) / (8 * NT) * (8 * NT);
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const T* r = NORM && p.residual ? static_cast<const T*>(p.residual) + row * p.ldr : nullptr;
+    auto number8 = [&](const T* row, int col, float (&f)[8]) { unpack8<T, AL>(load8<T, AL>(row, col, p.cols - col), AL ? 0 : row_offset(row), p.cols - col, f); };
     auto hidden8 = [&](int col, float (&h)[8]) {
-        unpack8(load8(x + col, p.cols - col, p.vx), h);
+        number8(x, col, h);
         if (r) {
             float b[8];
-            unpack8(load8(r + col, p.cols - col, p.vr), b);
+            number8(r, col, b);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = __fadd_rn(h[j], b[j]);
         }
@@ -304,12 +389,12 @@ __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
     float rstd = 1.0f;
     if constexpr (NORM) {
         double sum = 0.0;
-        for (int v = t; v < (groups + NT - 1) / NT * NT; v += NT) {          // every lane goes round as often: checkpoint8 shuffles
-            float h[8];
-            hidden8(8 * v, h);
+        for (int col = 8 * t; col < end; col += 8 * NT) {
+            float h[1][8];
+            hidden8(col, h[0]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { const double d = (double)h[j]; sum = fma(d, d, sum); }
-            if (p.block) checkpoint8<T>(p, row, 8 * v, h);
+            for (int j = 0; j < 8; ++j) { const double d = (double)h[0][j]; sum = fma(d, d, sum); }
+            if (p.block) checkpoint8<1>(p, row, col, 0, h);
         }
         sum = row_sum<NT>(sum, red_sum);
         rstd = (float)(1.0 / sqrt(sum / (double)p.cols + p.eps));
@@ -318,55 +403,68 @@ __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
     auto normed8 = [&](int col, float (&h)[8]) {
         if constexpr (NORM) {
             float g[8];
-            unpack8(load8(static_cast<const T*>(p.gain) + col, p.cols - col, p.vg), g);
+            number8(static_cast<const T*>(p.gain), col, g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[j] = __fmul_rn(__fmul_rn(h[j], rstd), g[j]);
         }
     };
     uint32_t m = 0;
-    for (int v = t; v < groups; v += NT) {
+    for (int col = 8 * t; col < end; col += 8 * NT) {
         float h[8];
-        hidden8(8 * v, h);
-        normed8(8 * v, h);
+        hidden8(col, h);
+        normed8(col, h);
         m = max(m, abs_max8(h));
     }
     const Scale s = block_scale(row_max<NT>(m, red_max), p.pow2);
-    for (int v = t; v < groups; v += NT) {
+    for (int col = 8 * t; col < end; col += 8 * NT) {
         float h[8];
-        hidden8(8 * v, h);
-        if (r) store8(static_cast<T*>(p.hidden) + row * p.ldh + 8 * v, h, p.cols - 8 * v, p.vh, p, 2113);
-        normed8(8 * v, h);
-        store_codes8(p.codes + row * p.ldc + 8 * v, codes8(h, s.inverse), p.cols - 8 * v, p.vc, p, 2115);
+        hidden8(col, h);
+        if (r) store8<T, AL>(static_cast<T*>(p.hidden) + row * p.ldh, col, p.cols - col, h, p, 2113);
+        normed8(col, h);
+        store_codes8(p.codes + row * p.ldc + col, codes8(h, s.inverse), p.cols - col, p.vc, p, 2115);
     }
     if (t == 0 && ROW_STORE_OK(p.scales + row, 4, 2116)) p.scales[row] = s.scale;
 }
 
 // ---------------------------------------------------------------------------------------- quantization in blocks
+// blockDim (columns / 8 / VPT, rows): a thread takes VPT groups of eight columns at a time, all of them loaded before the first is used.
 struct BlocksParams {
     const void* x; int8_t* codes; float* scales;
     int64_t ldx, ldc;
     int rows, cols, block;
-    bool pow2, vx, vc;
+    bool pow2, vc;
     Int8Ranges ranges;
 };
-// No row is reduced: a warp takes 256 columns at a time.  blockDim (columns / 8, rows)
-template <typename T>
+constexpr int FLAT_VPT = 4;
+
+template <typename T, bool AL>
 __global__ void __launch_bounds__(256) quantize_blocks_kernel(const BlocksParams p)
 {
-    const int lanes = p.block / 8, per_row = (p.cols + p.block - 1) / p.block, rounds = (p.cols + 255) / 256 * 32;
+    constexpr int VPT = FLAT_VPT;
+    const int shift = p.block == 32 ? 5 : 7, lanes = 1 << (shift - 3), per_row = (p.cols + p.block - 1) >> shift, step = 8 * blockDim.x;
     for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < p.rows; row += (int64_t)gridDim.x * blockDim.y) {
         const T* x = static_cast<const T*>(p.x) + row * p.ldx;
-#pragma unroll 2
-        for (int v = threadIdx.x; v < rounds; v += blockDim.x) {
-            const int col = 8 * v, n = p.cols - col;
-            float f[8];
-            unpack8(load8(x + col, n, p.vx), f);
-            const Scale s = block_scale(group_max(abs_max8(f), lanes), p.pow2);
-            if (n <= 0) continue;
-            store_codes8(p.codes + row * p.ldc + col, codes8(f, s.inverse), n, p.vc, p, 2121);
-            if (v % lanes == 0) {
-                float* q = p.scales + row * per_row + v / lanes;
-                if (ROW_STORE_OK(q, 4, 2122)) *q = s.scale;
+        const int mx = AL ? 0 : row_offset(x);
+        for (int first = 0; first < p.cols; first += VPT * step) {
+            const int col = first + 8 * threadIdx.x;
+            Raw8<T, AL> raw[VPT];
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(x, col + i * step, p.cols - (col + i * step));
+            float f[VPT][8];
+            uint32_t m[VPT];
+            Scale s[VPT];
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) { unpack8<T, AL>(raw[i], mx, p.cols - (col + i * step), f[i]); m[i] = abs_max8(f[i]); }
+            block_scales(m, lanes, p.pow2, s);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int c = col + i * step, n = p.cols - c;
+                if (n <= 0) continue;
+                store_codes8(p.codes + row * p.ldc + c, codes8(f[i], s[i].inverse), n, p.vc, p, 2121);
+                if ((c & (p.block - 1)) == 0) {
+                    float* q = p.scales + row * per_row + (c >> shift);
+                    if (ROW_STORE_OK(q, 4, 2122)) *q = s[i].scale;
+                }
             }
         }
     }
@@ -377,26 +475,36 @@ struct RestoreParams {
     const int8_t* codes; const float* scales; void* x;
     int64_t ldc, ldx;
     int rows, cols, block;
-    bool vc, vx;
+    bool vc;
     Int8Ranges ranges;
 };
-template <typename T>
+template <typename T, bool AL>
 __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
 {
-    const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, groups = (p.cols + 7) / 8, shift = p.block == 32 ? 2 : 4;
+    constexpr int VPT = FLAT_VPT;
+    const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, shift = p.block == 32 ? 5 : 7, step = 8 * blockDim.x;
     for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < p.rows; row += (int64_t)gridDim.x * blockDim.y) {
         const int8_t* codes = p.codes + row * p.ldc;
         const float* scales = p.scales + row * per_row;
         T* x = static_cast<T*>(p.x) + row * p.ldx;
-#pragma unroll 4
-        for (int v = threadIdx.x; v < groups; v += blockDim.x) {
-            float f[8];
-            const uint2 c = load_codes8(codes + 8 * v, p.cols - 8 * v, p.vc);
-            const float s = scales[p.block ? v >> shift : 0];
-            codes_to_float(c, f);
+        for (int first = 0; first < p.cols; first += VPT * step) {
+            const int col = first + 8 * threadIdx.x;
+            uint2 c[VPT];
+            float s[VPT];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], s);
-            store8(x + 8 * v, f, p.cols - 8 * v, p.vx, p, 2131);
+            for (int i = 0; i < VPT; ++i) {
+                const int at = col + i * step, n = p.cols - at;
+                c[i] = load_codes8(codes + at, n, p.vc);
+                s[i] = n > 0 ? scales[p.block ? at >> shift : 0] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                float f[8];
+                codes_to_float(c[i], f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], s[i]);
+                store8<T, AL>(x, col + i * step, p.cols - (col + i * step), f, p, 2131);
+            }
         }
     }
 }
@@ -405,174 +513,203 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
 struct BackParams {
     const void* dy; const int8_t* checkpoint; const float* scales; const float* rstd; const void* gain; const void* dresidual;
     void* dx; float* dgain; float* partial;
-    int64_t ldy, ldk, ldr, ldx;
+    int64_t ldy, ldk, ldr, ldx, ldp;          // ldp: of partial, a multiple of 8
     int rows, cols, block, parts;             // parts: rows of `partial`
-    bool vy, vk, vg, vr, vx;
+    bool aligned, vk;                         // aligned: AL for dy, gain, dresidual and dx; vk: of the checkpoint, to 8 bytes
     Int8Ranges ranges;
 };
 
-// xhat of eight columns: code * scale * rstd
+constexpr int BACK_VPT = 2;
+
+// xhat of eight columns: code * (scale * rstd)
 __device__ __forceinline__ void xhat8(uint2 codes, float scale, float rstd, float (&f)[8])
 {
     codes_to_float(codes, f);
+    const float s = scale * rstd;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = f[j] * scale * rstd;
+    for (int j = 0; j < 8; ++j) f[j] *= s;
 }
 
-// What a thread holds of a row.
-template <typename T, int VPT> struct BackRow {
-    Raw8<T> dy[VPT], dresidual[VPT];
-    uint2 codes[VPT];
-    float scale[VPT], rstd;
-};
-
-// Rows are dealt out to `parts` groups of NT threads; a thread keeps its columns' sums of dy * xhat in registers over all rows of its
-// group and writes them once, as one row of `partial`; column_sum_kernel adds those rows up in a fixed order.  A row is held as it was
-// read and its numbers are formed twice, before and after the sum over the row, so that the next row's loads can be in flight
-// meanwhile (NEXT) in 128 registers: with two groups of a 16-bit type a thread.  Otherwise the gain, and dresidual behind the sum,
-// are loaded where they are used.
-template <typename T, int NT, int VPT>
-__global__ void __launch_bounds__(NT == 32 ? 128 : NT) back_kernel(const BackParams p)
+// sum over the warps of a row's threads, however many, in a fixed order
+__device__ __forceinline__ float row_sum_of(float v, float* red, int warps)
 {
-    constexpr bool NEXT = sizeof(T) == 2 && VPT <= 2;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (warps > 1) {
+        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+        __syncthreads();
+        const int lane = threadIdx.x & 31;
+        v = lane < warps ? red[lane] : 0.0f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    }
+    return v;
+}
+
+// Rows are dealt out to groups of threads, a block or (SHORT) a warp, four to a block; each thread has two groups of eight columns.
+// It keeps its columns' sums of dy * xhat in registers over all its rows and the block writes them once, as one row of `partial`;
+// column_sum_kernel adds those rows up in a fixed order.  128 registers a thread let the next row's loads be in flight while this one
+// is summed (NEXT: aligned rows of a 16-bit type; the others' loads are issued together where the row begins).  The gain, the same for
+// all rows, comes from L1 each time.
+template <typename T, bool AL, bool SHORT>
+__global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(const BackParams p)
+{
+    constexpr bool NEXT = AL && sizeof(T) == 2;
+    constexpr int RPC = SHORT ? 4 : 1, VPT = BACK_VPT;
     __shared__ float red[2][32];
-    constexpr int RPC = NT == 32 ? 4 : 1;
-    const int t = threadIdx.x, part = blockIdx.x * RPC + threadIdx.y;
-    if (RPC > 1 && part >= p.parts) return;                   // whole warps
-    const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, shift = p.block == 32 ? 2 : 4;
+    __shared__ float4 meet[RPC > 1 ? RPC * VPT * 32 * 2 : 1];
+    fmmptx::griddep_launch_dependents();
+    const int NT = SHORT ? 32 : blockDim.x, t = threadIdx.x, group = blockIdx.x * RPC + threadIdx.y, groups = gridDim.x * RPC;
+    const int shift = p.block == 32 ? 5 : 7, per_row = p.block ? (p.cols + p.block - 1) >> shift : 1;
     float sum[VPT][8];
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[i][j] = 0.0f;
-    auto load_gain = [&](int i) { const int col = 8 * (i * NT + t); return load8(static_cast<const T*>(p.gain) + col, p.cols - col, p.vg); };
-    auto load_dresidual = [&](int64_t row, int i) {
-        const int col = 8 * (i * NT + t);
-        return load8(static_cast<const T*>(p.dresidual) + row * p.ldr + col, p.cols - col, p.vr);
-    };
+    const T* gain = static_cast<const T*>(p.gain);
+    const int mg = AL ? 0 : row_offset(gain);
+    Raw8<T, AL> dy[VPT];
+    uint2 codes[VPT];
+    float scale[VPT], rstd = 0.0f;
     auto fetch = [&](int64_t row) {
-        BackRow<T, VPT> r;
-        r.rstd = p.rstd[row];
+        rstd = p.rstd[row];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int v = i * NT + t, col = 8 * v, n = p.cols - col;
-            r.dy[i] = load8(static_cast<const T*>(p.dy) + row * p.ldy + col, n, p.vy);
-            r.codes[i] = load_codes8(p.checkpoint + row * p.ldk + col, n, p.vk);
-            r.scale[i] = n > 0 ? p.scales[row * per_row + (p.block ? v >> shift : 0)] : 0.0f;
+            const int col = 8 * (i * NT + t), n = p.cols - col;
+            dy[i] = load8<T, AL>(static_cast<const T*>(p.dy) + row * p.ldy, col, n);
+            codes[i] = load_codes8(p.checkpoint + row * p.ldk + col, n, p.vk);
+            scale[i] = n > 0 ? p.scales[row * per_row + (p.block ? col >> shift : 0)] : 0.0f;
         }
-        if (NEXT && p.dresidual) {
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) r.dresidual[i] = load_dresidual(row, i);
-        }
-        return r;
     };
-    Raw8<T> g[VPT];
-    if (NEXT) {
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) g[i] = load_gain(i);
-    }
-    BackRow<T, VPT> next;
-    if (NEXT && part < p.rows) next = fetch(part);
     int parity = 0;
-    for (int64_t row = part; row < p.rows; row += p.parts, parity ^= 1) {
-        const BackRow<T, VPT> r = NEXT ? next : fetch(row);
-        if (NEXT && row + p.parts < p.rows) next = fetch(row + p.parts);
-        float c = 0.0f;
+    if (NEXT && group < p.rows) fetch(group);
+    for (int64_t row = group; row < p.rows; row += groups, parity ^= 1) {
+        if (!NEXT) fetch(row);
+        const float rs = rstd;
+        const int my = AL ? 0 : row_offset(static_cast<const T*>(p.dy) + row * p.ldy);
+        const T* dres = static_cast<const T*>(p.dresidual) + row * p.ldr;
+        Raw8<T, AL> add[VPT];
+        if (p.dresidual) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); add[i] = load8<T, AL>(dres, col, p.cols - col); }
+        }
+        float out[VPT][8], xh[VPT][8], c = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            float d[8], gg[8], xh[8];
-            unpack8(r.dy[i], d);
-            unpack8(NEXT ? g[i] : load_gain(i), gg);
-            xhat8(r.codes[i], r.scale[i], r.rstd, xh);
+            const int col = 8 * (i * NT + t), n = p.cols - col;
+            float g[8];
+            unpack8<T, AL>(load8<T, AL>(gain, col, n), mg, n, g);
+            unpack8<T, AL>(dy[i], my, n, out[i]);
+            xhat8(codes[i], scale[i], rs, xh[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                sum[i][j] = fmaf(d[j], xh[j], sum[i][j]);
-                c = fmaf(d[j] * gg[j], xh[j], c);
+                sum[i][j] = fmaf(out[i][j], xh[i][j], sum[i][j]);
+                out[i][j] *= g[j];
+                c = fmaf(out[i][j], xh[i][j], c);
             }
         }
-        c = row_sum<NT>(c, red[parity]) / (float)p.cols;
+        if (NEXT && row + groups < p.rows) fetch(row + groups);
+        c = row_sum_of(c, red[parity], NT / 32) / (float)p.cols;
         T* dx = static_cast<T*>(p.dx) + row * p.ldx;
+        const int mr = AL ? 0 : row_offset(dres);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int col = 8 * (i * NT + t);
-            float d[8], gg[8], xh[8];
-            unpack8(r.dy[i], d);
-            unpack8(NEXT ? g[i] : load_gain(i), gg);
-            xhat8(r.codes[i], r.scale[i], r.rstd, xh);
+            const int col = 8 * (i * NT + t), n = p.cols - col;
+            float b[8];
+            if (p.dresidual) unpack8<T, AL>(add[i], mr, n, b);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = r.rstd * (d[j] * gg[j] - xh[j] * c);
-            if (p.dresidual) {
-                float b[8];
-                unpack8(NEXT ? r.dresidual[i] : load_dresidual(row, i), b);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] += b[j];
+            for (int j = 0; j < 8; ++j) {
+                out[i][j] = rs * (out[i][j] - xh[i][j] * c);
+                if (p.dresidual) out[i][j] += b[j];
             }
-            store8(dx + col, d, p.cols - col, p.vx, p, 2141);
+            store8<T, AL>(dx, col, n, out[i], p, 2141);
         }
     }
-    float* q = p.partial + (int64_t)part * p.cols;
+    if constexpr (RPC > 1) {
+        // the block's groups meet, in their order
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); store8(q + col, sum[i], p.cols - col, (p.cols & 3) == 0, p, 2142); }
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                meet[((threadIdx.y * VPT + i) * 2 + h) * 32 + t] = make_float4(sum[i][4 * h], sum[i][4 * h + 1], sum[i][4 * h + 2], sum[i][4 * h + 3]);
+        __syncthreads();
+        if (threadIdx.y > 0) return;
+#pragma unroll
+        for (int y = 1; y < RPC; ++y)
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float4 v = meet[((y * VPT + i) * 2 + h) * 32 + t];
+                    sum[i][4 * h] += v.x; sum[i][4 * h + 1] += v.y; sum[i][4 * h + 2] += v.z; sum[i][4 * h + 3] += v.w;
+                }
+    }
+    float* q = p.partial + (int64_t)blockIdx.x * p.ldp;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); store8<float, true>(q, col, p.cols - col, sum[i], p, 2142); }
 }
 
 // Rows that do not fit registers: dy and the codes are read twice (the second time from L2, mostly), and the sums of a group live in
 // its row of `partial`, which no other group touches.
-template <typename T>
+template <typename T, bool AL>
 __global__ void __launch_bounds__(1024) back_long_kernel(const BackParams p)
 {
     constexpr int NT = 1024;
     __shared__ float red[2][32];
-    const int t = threadIdx.x, part = blockIdx.x, groups = (p.cols + 7) / 8;
-    const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, shift = p.block == 32 ? 2 : 4;
-    float* q = p.partial + (int64_t)part * p.cols;
-    const bool vq = (p.cols & 3) == 0;
+    fmmptx::griddep_launch_dependents();
+    const int t = threadIdx.x, part = blockIdx.x, end = (p.cols + 8 * NT - 1) / (8 * NT) * (8 * NT);
+    const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, shift = p.block == 32 ? 5 : 7;
+    float* q = p.partial + (int64_t)part * p.ldp;
+    auto number8 = [&](const void* base, int64_t ld, int64_t row, int col, float (&f)[8]) {
+        const T* r = static_cast<const T*>(base) + row * ld;
+        unpack8<T, AL>(load8<T, AL>(r, col, p.cols - col), AL ? 0 : row_offset(r), p.cols - col, f);
+    };
     int parity = 0;
-    for (int64_t row = part; row < p.rows; row += p.parts, parity ^= 1) {
+    for (int64_t row = part; row < p.rows; row += gridDim.x, parity ^= 1) {
         const float rs = p.rstd[row];
-        auto both8 = [&](int v, float (&d)[8], float (&xh)[8]) {
-            const int n = p.cols - 8 * v;
-            unpack8(load8(static_cast<const T*>(p.dy) + row * p.ldy + 8 * v, n, p.vy), d);
-            xhat8(load_codes8(p.checkpoint + row * p.ldk + 8 * v, n, p.vk), p.scales[row * per_row + (p.block ? v >> shift : 0)], rs, xh);
+        auto both8 = [&](int col, float (&d)[8], float (&xh)[8], float (&g)[8]) {
+            const int n = p.cols - col;
+            number8(p.dy, p.ldy, row, col, d);
+            number8(p.gain, 0, 0, col, g);
+            xhat8(load_codes8(p.checkpoint + row * p.ldk + col, n, p.vk), n > 0 ? p.scales[row * per_row + (p.block ? col >> shift : 0)] : 0.0f, rs, xh);
         };
-        auto gain8 = [&](int v, float (&g)[8]) { unpack8(load8(static_cast<const T*>(p.gain) + 8 * v, p.cols - 8 * v, p.vg), g); };
         float c = 0.0f;
-        for (int v = t; v < groups; v += NT) {
+        for (int col = 8 * t; col < p.cols; col += 8 * NT) {
             float d[8], xh[8], g[8], s[8];
-            both8(v, d, xh);
-            gain8(v, g);
+            both8(col, d, xh, g);
             if (row == part) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[j] = 0.0f;
-            } else unpack8(load8<float>(q + 8 * v, p.cols - 8 * v, vq), s);
+            } else unpack8<float, true>(load8<float, true>(q, col, p.cols - col), 0, p.cols - col, s);
 #pragma unroll
             for (int j = 0; j < 8; ++j) { s[j] = fmaf(d[j], xh[j], s[j]); c = fmaf(d[j] * g[j], xh[j], c); }
-            store8(q + 8 * v, s, p.cols - 8 * v, vq, p, 2152);
+            store8<float, true>(q, col, p.cols - col, s, p, 2152);
         }
         c = row_sum<NT>(c, red[parity]) / (float)p.cols;
-        for (int v = t; v < groups; v += NT) {
+        for (int col = 8 * t; col < end; col += 8 * NT) {
             float d[8], xh[8], g[8], b[8];
-            both8(v, d, xh);
-            gain8(v, g);
-            if (p.dresidual) unpack8(load8(static_cast<const T*>(p.dresidual) + row * p.ldr + 8 * v, p.cols - 8 * v, p.vr), b);
+            both8(col, d, xh, g);
+            if (p.dresidual) number8(p.dresidual, p.ldr, row, col, b);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 d[j] = rs * (d[j] * g[j] - xh[j] * c);
                 if (p.dresidual) d[j] += b[j];
             }
-            store8(static_cast<T*>(p.dx) + row * p.ldx + 8 * v, d, p.cols - 8 * v, p.vx, p, 2151);
+            store8<T, AL>(static_cast<T*>(p.dx) + row * p.ldx, col, p.cols - col, d, p, 2151);
         }
     }
 }
 
-// dgain[col] = sum of the `parts` rows of partial: 32 columns a block, 32 warps that take every 32nd row, then the warps in order
+// dgain[col] = sum of the rows of partial: 32 columns a block, 32 warps that take every 32nd row, then the warps in order
 __global__ void __launch_bounds__(1024) column_sum_kernel(const BackParams p)
 {
     __shared__ float red[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    fmmptx::griddep_wait();
     float s = 0.0f;
     if (col < p.cols) {
 #pragma unroll 4
-        for (int r = warp; r < p.parts; r += 32) s += p.partial[(int64_t)r * p.cols + col];
+        for (int r = warp; r < p.parts; r += 32) s += p.partial[(int64_t)r * p.ldp + col];
     }
     red[warp][lane] = s;
     __syncthreads();
@@ -587,48 +724,63 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const BackParams p)
 // ---------------------------------------------------------------------------------------- launches
 fmm_status_t launched() { return cudaGetLastError() == cudaSuccess ? FMM_OK : FMM_ERR_CUDA; }
 
-template <typename T, bool NORM> fmm_status_t launch_rows(const RowsParams& p, cudaStream_t st)
+template <typename T, bool NORM, bool AL> fmm_status_t launch_rows_aligned(const RowsParams& p, cudaStream_t st)
 {
     const int groups = (p.cols + 7) / 8;
     const unsigned rows = (unsigned)p.rows;
-    if (groups <= 64) rows_kernel<T, NORM, 32, 2><<<(rows + 3) / 4, dim3(32, 4), 0, st>>>(p);
-    else if (groups <= 256) rows_kernel<T, NORM, 128, 2><<<rows, 128, 0, st>>>(p);
-    else if (groups <= 512) rows_kernel<T, NORM, 256, 2><<<rows, 256, 0, st>>>(p);
-    else if (groups <= 1024) rows_kernel<T, NORM, 256, 4><<<rows, 256, 0, st>>>(p);
-    else if (groups <= 2048) rows_kernel<T, NORM, 512, 4><<<rows, 512, 0, st>>>(p);
-    else rows_long_kernel<T, NORM><<<rows, 1024, 0, st>>>(p);
+    if (groups <= 64) rows_kernel<T, NORM, AL, 32, 2><<<(rows + 3) / 4, dim3(32, 4), 0, st>>>(p);
+    else if (groups <= 256) rows_kernel<T, NORM, AL, 128, 2><<<rows, 128, 0, st>>>(p);
+    else if (groups <= 512) rows_kernel<T, NORM, AL, 256, 2><<<rows, 256, 0, st>>>(p);
+    else if (groups <= 1024) rows_kernel<T, NORM, AL, 256, 4><<<rows, 256, 0, st>>>(p);
+    else if (groups <= 2048) rows_kernel<T, NORM, AL, 512, 4><<<rows, 512, 0, st>>>(p);
+    else rows_long_kernel<T, NORM, AL><<<rows, 1024, 0, st>>>(p);
     return launched();
 }
+template <typename T, bool NORM> fmm_status_t launch_rows(const RowsParams& p, cudaStream_t st)
+{
+    return p.aligned ? launch_rows_aligned<T, NORM, true>(p, st) : launch_rows_aligned<T, NORM, false>(p, st);
+}
 
-// groups of threads among which the rows of the norm's gradients are dealt out, and threads of a group (1024: long rows)
-struct BackShape { int threads, parts; };
+// Threads among which a row of the norm's gradients is split (0: long rows), and blocks.  A group of threads has at least four rows, so that
+// what it adds to the columns' sums is worth writing out.
+struct BackShape { int threads, blocks; };
 BackShape back_shape(int64_t rows, int64_t cols)
 {
     const int64_t groups = (cols + 7) / 8;
-    const int threads = groups <= 64 ? 32 : groups <= 256 ? 128 : groups <= 512 ? 256 : groups <= 2048 ? 512 : 1024;
-    const int64_t resident = (int64_t)fmm_sm_count() * (1024 / threads);
-    const int64_t by_rows = (rows + 3) / 4;
+    const int threads = groups <= 1024 ? (int)(groups + 32 * BACK_VPT - 1) / (32 * BACK_VPT) * 32 : 0;
+    const int64_t per_sm = threads == 32 ? 4 : threads ? 512 / threads : 1, rows_at_once = threads == 32 ? 4 : 1;
+    const int64_t resident = (int64_t)fmm_sm_count() * per_sm, by_rows = (rows + 4 * rows_at_once - 1) / (4 * rows_at_once);
     return {threads, (int)(by_rows < 1 ? 1 : by_rows < resident ? by_rows : resident)};
 }
+int64_t partial_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 
+template <typename T, bool AL> void launch_back_aligned(const BackParams& p, int threads, cudaStream_t st)
+{
+    const unsigned blocks = (unsigned)p.parts;
+    if (threads == 32) back_kernel<T, AL, true><<<blocks, dim3(32, 4), 0, st>>>(p);
+    else if (threads) back_kernel<T, AL, false><<<blocks, threads, 0, st>>>(p);
+    else back_long_kernel<T, AL><<<blocks, 1024, 0, st>>>(p);
+}
 template <typename T> fmm_status_t launch_back(const BackParams& p, int threads, cudaStream_t st)
 {
-    const unsigned parts = (unsigned)p.parts, groups = (unsigned)(p.cols + 7) / 8;
-    if (threads == 32) back_kernel<T, 32, 2><<<(parts + 3) / 4, dim3(32, 4), 0, st>>>(p);
-    else if (threads == 128) back_kernel<T, 128, 2><<<parts, 128, 0, st>>>(p);
-    else if (threads == 256) back_kernel<T, 256, 2><<<parts, 256, 0, st>>>(p);
-    else if (threads == 512 && groups <= 1024) back_kernel<T, 512, 2><<<parts, 512, 0, st>>>(p);
-    else if (threads == 512) back_kernel<T, 512, 4><<<parts, 512, 0, st>>>(p);
-    else back_long_kernel<T><<<parts, 1024, 0, st>>>(p);
-    column_sum_kernel<<<(unsigned)(p.cols + 31) / 32, 1024, 0, st>>>(p);
-    return launched();
+    if (p.aligned) launch_back_aligned<T, true>(p, threads, st); else launch_back_aligned<T, false>(p, threads, st);
+    if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;
+    // set up while the rows are dealt with; it waits for them before its first load
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.cols + 31) / 32); cfg.blockDim = dim3(1024); cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, column_sum_kernel, p) != cudaSuccess) { cudaGetLastError(); return FMM_ERR_CUDA; }
+    return FMM_OK;
 }
 
-// blocks of 256 threads for row-parallel kernels without a reduction: columns / 8 along x, rows along y
+// blocks of 256 threads for row-parallel kernels without a reduction: columns / 8 / FLAT_VPT along x, rows along y
 dim3 flat_block(int cols)
 {
     unsigned x = 32;
-    while (x < 256 && 8u * x < (unsigned)cols) x *= 2;
+    while (x < 256 && 8u * FLAT_VPT * x < (unsigned)cols) x *= 2;
     return dim3(x, 256 / x);
 }
 unsigned flat_grid(int rows, dim3 block)
@@ -668,24 +820,28 @@ fmm_status_t fmm_int8_quantize(const void* X, fmm_type_t type, int64_t ldx, int6
     const int e = int8_type_bytes(type);
     if (!matrix_ok(scales, 1, 1, 4) || (cols > 0 && (!matrix_ok(X, cols, ldx, e) || !matrix_ok(codes, cols, ldc, 1)))) return FMM_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const bool vx = int8_aligned(X, ldx * e, 16), vc = int8_aligned(codes, ldc, 8), pow2 = scale_mode == FMM_INT8_SCALE_POW2;
+    const bool vx = int8_aligned(X, ldx * e, 16) && cols % 8 == 0, vc = int8_aligned(codes, ldc, 8), pow2 = scale_mode == FMM_INT8_SCALE_POW2;
     Int8Ranges ranges = {};
     int8_add_range(ranges, codes, rows, cols, ldc, 1);
     if (block) {
         const int64_t per_row = (cols + block - 1) / block;
         int8_add_range(ranges, scales, rows, per_row, per_row, 4);
-        const BlocksParams p = {X, codes, scales, ldx, ldc, (int)rows, (int)cols, block, pow2, vx, vc, ranges};
+        const BlocksParams p = {X, codes, scales, ldx, ldc, (int)rows, (int)cols, block, pow2, vc, ranges};
         const dim3 b = flat_block((int)cols);
         const unsigned grid = flat_grid((int)rows, b);
-        if (type == FMM_TYPE_F32) quantize_blocks_kernel<float><<<grid, b, 0, st>>>(p);
-        else if (type == FMM_TYPE_BF16) quantize_blocks_kernel<__nv_bfloat16><<<grid, b, 0, st>>>(p);
-        else quantize_blocks_kernel<__half><<<grid, b, 0, st>>>(p);
+        auto launch = [&](auto type) {
+            using T = decltype(type);
+            if (vx) quantize_blocks_kernel<T, true><<<grid, b, 0, st>>>(p); else quantize_blocks_kernel<T, false><<<grid, b, 0, st>>>(p);
+        };
+        if (type == FMM_TYPE_F32) launch(float{});
+        else if (type == FMM_TYPE_BF16) launch(__nv_bfloat16{});
+        else launch(__half{});
         return launched();
     }
     int8_add_range(ranges, scales, 1, rows, rows, 4);
     RowsParams p = {};
     p.x = X; p.ldx = ldx; p.codes = codes; p.ldc = ldc; p.scales = scales;
-    p.rows = (int)rows; p.cols = (int)cols; p.pow2 = pow2; p.vx = vx; p.vc = vc; p.ranges = ranges;
+    p.rows = (int)rows; p.cols = (int)cols; p.pow2 = pow2; p.aligned = vx; p.vc = vc; p.ranges = ranges;
     if (type == FMM_TYPE_F32) return launch_rows<float, false>(p, st);
     if (type == FMM_TYPE_BF16) return launch_rows<__nv_bfloat16, false>(p, st);
     return launch_rows<__half, false>(p, st);
@@ -701,13 +857,17 @@ fmm_status_t fmm_int8_dequantize(const int8_t* codes, int64_t ldc, const float* 
     if (!matrix_ok(codes, cols, ldc, 1) || !matrix_ok(scales, 1, 1, 4) || !matrix_ok(X, cols, ldx, e)) return FMM_ERR_INVALID_ARG;
     Int8Ranges ranges = {};
     int8_add_range(ranges, X, rows, cols, ldx, e);
-    const RestoreParams p = {codes, scales, X, ldc, ldx, (int)rows, (int)cols, block, int8_aligned(codes, ldc, 8), int8_aligned(X, ldx * e, 16), ranges};
+    const RestoreParams p = {codes, scales, X, ldc, ldx, (int)rows, (int)cols, block, int8_aligned(codes, ldc, 8), ranges};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const dim3 b = flat_block((int)cols);
     const unsigned grid = flat_grid((int)rows, b);
-    if (type == FMM_TYPE_F32) dequantize_kernel<float><<<grid, b, 0, st>>>(p);
-    else if (type == FMM_TYPE_BF16) dequantize_kernel<__nv_bfloat16><<<grid, b, 0, st>>>(p);
-    else dequantize_kernel<__half><<<grid, b, 0, st>>>(p);
+    auto launch = [&](auto type) {
+        using T = decltype(type);
+        if (int8_aligned(X, ldx * e, 16) && cols % 8 == 0) dequantize_kernel<T, true><<<grid, b, 0, st>>>(p); else dequantize_kernel<T, false><<<grid, b, 0, st>>>(p);
+    };
+    if (type == FMM_TYPE_F32) launch(float{});
+    else if (type == FMM_TYPE_BF16) launch(__nv_bfloat16{});
+    else launch(__half{});
     return launched();
 }
 
@@ -729,8 +889,9 @@ fmm_status_t fmm_int8_rms_norm(const fmm_int8_rms_norm_t* a, void* stream)
     p.checkpoint = a->checkpoint; p.checkpoint_scales = a->checkpoint_scales;
     p.ldx = a->ldx; p.ldr = a->ldr; p.ldh = a->ldh; p.ldc = a->ldc; p.ldk = a->ldk;
     p.eps = a->eps; p.rows = (int)rows; p.cols = (int)cols; p.block = a->checkpoint_block; p.pow2 = a->scale_mode == FMM_INT8_SCALE_POW2;
-    p.vx = int8_aligned(a->x, a->ldx * e, 16); p.vr = int8_aligned(a->residual, a->ldr * e, 16); p.vg = int8_aligned(a->gain, 0, 16);
-    p.vh = int8_aligned(a->hidden, a->ldh * e, 16); p.vc = int8_aligned(a->codes, a->ldc, 8); p.vk = int8_aligned(a->checkpoint, a->ldk, 8);
+    p.aligned = cols % 8 == 0 && int8_aligned(a->x, a->ldx * e, 16) && int8_aligned(a->gain, 0, 16) &&
+                (!a->residual || (int8_aligned(a->residual, a->ldr * e, 16) && int8_aligned(a->hidden, a->ldh * e, 16)));
+    p.vc = int8_aligned(a->codes, a->ldc, 8); p.vk = int8_aligned(a->checkpoint, a->ldk, 8);
     if (a->residual) int8_add_range(p.ranges, a->hidden, rows, cols, a->ldh, e);
     int8_add_range(p.ranges, a->codes, rows, cols, a->ldc, 1);
     int8_add_range(p.ranges, a->scales, 1, rows, rows, 4);
@@ -749,7 +910,7 @@ fmm_status_t fmm_int8_rms_norm_backward_workspace_bytes(int64_t rows, int64_t co
 {
     if (!bytes) return FMM_ERR_INVALID_ARG;
     if (!dims_ok(rows, cols)) return FMM_ERR_SHAPE;
-    *bytes = (size_t)back_shape(rows, cols).parts * (size_t)cols * 4;
+    *bytes = (size_t)back_shape(rows, cols).blocks * (size_t)partial_ld(cols) * 4;
     return FMM_OK;
 }
 
@@ -772,17 +933,19 @@ fmm_status_t fmm_int8_rms_norm_backward(const fmm_int8_rms_norm_backward_t* a, v
         (a->dresidual && !matrix_ok(a->dresidual, cols, a->ldr, e)))
         return FMM_ERR_INVALID_ARG;
     const BackShape shape = back_shape(rows, cols);
-    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < (size_t)shape.parts * (size_t)cols * 4) return FMM_ERR_WORKSPACE;
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < (size_t)shape.blocks * (size_t)partial_ld(cols) * 4) return FMM_ERR_WORKSPACE;
     BackParams p = {};
     p.dy = a->dy; p.checkpoint = a->checkpoint; p.scales = a->checkpoint_scales; p.rstd = a->rstd; p.gain = a->gain; p.dresidual = a->dresidual;
     p.dx = a->dx; p.dgain = a->dgain; p.partial = static_cast<float*>(workspace);
     p.ldy = a->ldy; p.ldk = a->ldk; p.ldr = a->ldr; p.ldx = a->ldx;
-    p.rows = (int)rows; p.cols = (int)cols; p.block = a->block; p.parts = shape.parts;
-    p.vy = int8_aligned(a->dy, a->ldy * e, 16); p.vk = int8_aligned(a->checkpoint, a->ldk, 8); p.vg = int8_aligned(a->gain, 0, 16);
-    p.vr = int8_aligned(a->dresidual, a->ldr * e, 16); p.vx = int8_aligned(a->dx, a->ldx * e, 16);
+    p.ldp = partial_ld(cols);
+    p.rows = (int)rows; p.cols = (int)cols; p.block = a->block; p.parts = shape.blocks;
+    p.aligned = cols % 8 == 0 && int8_aligned(a->dy, a->ldy * e, 16) && int8_aligned(a->gain, 0, 16) && int8_aligned(a->dx, a->ldx * e, 16) &&
+                (!a->dresidual || int8_aligned(a->dresidual, a->ldr * e, 16));
+    p.vk = int8_aligned(a->checkpoint, a->ldk, 8);
     int8_add_range(p.ranges, a->dx, rows, cols, a->ldx, e);
     int8_add_range(p.ranges, a->dgain, 1, cols, cols, 4);
-    int8_add_range(p.ranges, workspace, shape.parts, cols, cols, 4);
+    int8_add_range(p.ranges, workspace, shape.blocks, p.ldp, p.ldp, 4);
     if (a->type == FMM_TYPE_F32) return launch_back<float>(p, shape.threads, st);
     if (a->type == FMM_TYPE_BF16) return launch_back<__nv_bfloat16>(p, shape.threads, st);
     return launch_back<__half>(p, shape.threads, st);
