@@ -17,6 +17,11 @@
 // cores as MN-major; nothing is transposed in memory.  One pipeline stage is 128 bytes of contraction on both sides (128 codes, 64
 // 16-bit numbers), four MMAs.
 //
+// The tensor cores add in fp32 by cutting off what does not fit, so the sums of a gradient drift towards zero as the contraction
+// grows: 2.4e-6 of their size over 8192 terms, 6e-6 over 16384.  Where the output is fp32 they are therefore taken out of the
+// accumulator every CHUNK stages (1024 terms) and added up in registers, rounded to nearest: XXX and XXX.  An output of 16 bits has no
+// use for that.
+//
 // The 8-bit operand of a gradient is restored to 16 bits by fmm_int8_dequantize into the workspace before the product: 3 bytes a code
 // once, against 2 M N K operations.  Restoring it tile by tile on the way into the tensor cores would take two more passes
 // through shared memory per tile (codes in, 16-bit values out), which the product's own operand traffic already fills.
@@ -67,6 +72,7 @@ struct ProductParams {
     int kstages;                    // 128-byte stages of the contraction
     int tiles_r, tiles_c;
     int k_shares;                   // cluster kernel
+    int chunk;                      // gradients: stages after which the sums leave the tensor cores' accumulator (see below)
     uint32_t idesc;                 // without the tile's dimensions
     const float* r_scales; const float* c_scales; const void* bias;      // INT8
     void* out; long long ldo;
@@ -74,6 +80,7 @@ struct ProductParams {
     Int8Ranges ranges;
 };
 
+constexpr int CHUNK = 16;
 // contraction elements per stage
 template <int KIND> constexpr int STAGE_ELEMENTS = KIND == INT8 ? 128 : 64;
 template <int KIND> constexpr bool R_MN = KIND != INT8;
@@ -120,22 +127,45 @@ __device__ __forceinline__ float load_bias(const ProductParams& p, int row)
     if (p.out_type == FMM_TYPE_BF16) return to_float(static_cast<const __nv_bfloat16*>(p.bias)[row]);
     return to_float(static_cast<const __half*>(p.bias)[row]);
 }
-// N columns from col0 of one row of the output, from a thread's registers.  c_scale: shared address of column col0's scale
+// N columns from col0 of one row of the output, from a thread's registers, `valid` of which exist.  c_scale: shared address of column
+// col0's scale.  All of them are computed before the first is stored, and whole groups without a test in between: with one the
+// columns came one after the other, 75 cycles each (4096 x 4096 x 128: 47.6 us a call, XXX without).
 template <int KIND, int N>
-__device__ __forceinline__ void put_columns(const ProductParams& p, const uint32_t (&v)[N], int row, int col0, float r_scale, float bias, uint32_t c_scale)
+__device__ __forceinline__ void put_columns(const ProductParams& p, const uint32_t (&v)[N], int row, int col0, int valid, float r_scale, float bias, uint32_t c_scale)
 {
     if (row >= p.rows) return;
+    float x[N];
+    if constexpr (KIND == INT8) {
+        float s[N];
+        if constexpr (N % 4 == 0) {
+#pragma unroll
+            for (int j = 0; j < N; j += 4) { const float4 f = lds128(c_scale + 4 * j); s[j] = f.x; s[j + 1] = f.y; s[j + 2] = f.z; s[j + 3] = f.w; }
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) s[j] = lds32f(c_scale + 4 * j);
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = scaled(v[j], r_scale, s[j]) + bias;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = __uint_as_float(v[j]);
+    }
     auto each = [&](auto type) {
         using T = decltype(type);
-        long long at = (long long)col0 * p.ldo + row;
+        T* q = static_cast<T*>(p.out) + ((long long)col0 * p.ldo + row);
+#ifndef FMM_DEBUG
+        if (valid >= N) {
+            if (p.accumulate) {
 #pragma unroll
-        for (int j = 0; j < N; ++j, at += p.ldo) {
-            if (col0 + j >= p.cols) break;
-            float x;
-            if constexpr (KIND == INT8) x = scaled(v[j], r_scale, lds32f(c_scale + 4 * j)) + bias;
-            else x = __uint_as_float(v[j]);
-            put_one<T>(p, at, x);
+                for (int j = 0; j < N; ++j) x[j] += to_float(q[j * p.ldo]);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) q[j * p.ldo] = from_float<T>(x[j]);
+            return;
         }
+#endif
+#pragma unroll
+        for (int j = 0; j < N; ++j) if (j < valid) put_one<T>(p, (q - static_cast<T*>(p.out)) + j * p.ldo, x[j]);
     };
     if (p.out_type == FMM_TYPE_F32) each(float{});
     else if (p.out_type == FMM_TYPE_BF16) each(__nv_bfloat16{});
@@ -146,21 +176,26 @@ __device__ __forceinline__ void put_columns(const ProductParams& p, const uint32
 // One tile of 128 rows x TC columns per cluster of k_shares CTAs, each of which sums a share of the contraction; the shares meet in
 // distributed shared memory and are added in ascending order.  For products of few tiles: latency (a launch, the first load, the
 // exchange) and, with few columns, the weight's way from memory bound it, so the contraction is cut until the device is full.
-// Two CTAs fit an SM: one exchanges or waits for its first operands while the other multiplies.
-//   warps 0..3  drain TMEM, exchange, output (a TMEM lane quadrant each);  warp 4  TMA producer;  warp 5  MMA issuer
+// INT8: two CTAs fit an SM; one exchanges or waits for its first operands while the other multiplies.
+//   the first 4 (8) warps  drain TMEM, exchange, output: a TMEM lane quadrant (and half of the columns) each
+//   the last two           TMA producer, MMA issuer
 template <int KIND, int TC>
 struct ClusterCfg {
     static constexpr int R_BYTES = 128 * 128, S_BYTES = TC * 128, STAGE_BYTES = R_BYTES + S_BYTES;
-    static constexpr int STAGES = 98304 / STAGE_BYTES;                  // 5, 4, 4, 3 for 16, 32, 64, 128 columns
-    static constexpr int OFF_SCALES = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALES + TC * 4, NUM_BARS = 2 * STAGES + 1;
-    static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;
-    static constexpr int TMEM_COLS = TC < 32 ? 32 : TC;
-    static_assert(SMEM_BYTES + 1024 <= 233472 / 2, "two CTAs per SM");
+    static constexpr int STAGES = (KIND == INT8 ? 98304 : 196608) / STAGE_BYTES;       // INT8: 5, 4, 4, 3 for 16, 32, 64, 128 columns
+    static constexpr int OFF_SCALES = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALES + TC * 4;
+    static constexpr int BUFS = KIND == INT8 ? 1 : 2, NUM_BARS = 2 * STAGES + 2 * BUFS;         // accumulators; gradients: a chunk is drained
+    static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;                       // while the next one is multiplied
+    static constexpr int TMEM_COLS = BUFS * TC < 32 ? 32 : BUFS * TC;
+    // gradients keep a chunk's sums in registers: twice the warps, one CTA per SM
+    static constexpr int OUT_WARPS = KIND == INT8 ? 4 : 8, THREADS = (OUT_WARPS + 2) * 32, CTAS = KIND == INT8 ? 2 : 1;
+    static_assert(TMEM_COLS <= 512 / CTAS, "TMEM of an SM");
+    static_assert(SMEM_BYTES + 1024 <= 233472 / (KIND == INT8 ? 2 : 1), "shared memory of an SM");
     static_assert(TC * 512 <= OFF_SCALES, "the exchange tile lies inside the operand ring");
 };
 
 template <int KIND, int TC>
-__global__ void __launch_bounds__(192, 2)
+__global__ void __launch_bounds__(ClusterCfg<KIND, TC>::THREADS, ClusterCfg<KIND, TC>::CTAS)
 int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmS, const ProductParams p)
 {
     using C = ClusterCfg<KIND, TC>;
@@ -171,7 +206,8 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
     const uint32_t bar0 = base + C::OFF_BAR;
     auto bar_full = [&](int s) { return bar0 + 8u * s; };
     auto bar_empty = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
-    const uint32_t bar_done = bar0 + 8u * (2 * C::STAGES);
+    auto bar_tfull = [&](int b) { return bar0 + 8u * (2 * C::STAGES + b); };
+    auto bar_tempty = [&](int b) { return bar0 + 8u * (2 * C::STAGES + C::BUFS + b); };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + C::OFF_BAR + C::NUM_BARS * 8);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const Ctl ctl{abort_flag, g_int8_product_status};
@@ -179,11 +215,11 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
     const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
-        mbar_init(bar_done, 1);
+        for (int b = 0; b < C::BUFS; ++b) { mbar_init(bar_tfull(b), 1); mbar_init(bar_tempty(b), C::OUT_WARPS); }
         *abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 5) {
+    if (warp == C::OUT_WARPS + 1) {
         tmem_alloc<1>(smem_u32(tmem_slot), C::TMEM_COLS);
         tmem_relinquish<1>();
     }
@@ -197,7 +233,7 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
     const int ks0 = (int)((long long)p.kstages * rank / shares), ks1 = (int)((long long)p.kstages * (rank + 1) / shares);
     const int row0 = tr * 128, col0 = tc * TC;
 
-    if (warp == 4) {
+    if (warp == C::OUT_WARPS) {
         int stage = 0; uint32_t phase = 0;
         griddep_wait();
         for (int ks = ks0; ks < ks1; ++ks) {
@@ -210,19 +246,25 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
             }
             if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
         }
-    } else if (warp == 5) {
-        int stage = 0; uint32_t phase = 0;
+    } else if (warp == C::OUT_WARPS + 1) {
+        int stage = 0, buf = 0; uint32_t phase = 0, bphase = 0;
         const uint32_t idesc = p.idesc | ((uint32_t)(TC >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
         bool ok = true;
-        for (int ks = ks0; ks < ks1; ++ks) {
-            if (!mbar_wait_warp(bar_full(stage), phase, ctl, 2302)) { ok = false; break; }
+        for (int kc = ks0; kc < ks1 && ok; kc += p.chunk) {
+            if (!mbar_wait_warp(bar_tempty(buf), bphase ^ 1u, ctl, 2304)) break;
             tc_fence_after();
-            const uint32_t s = base + stage * C::STAGE_BYTES;
-            mma_stage<KIND, 1>(tmem_base, s, s + C::R_BYTES, idesc, ks == ks0);
-            tc_commit<1>(bar_empty(stage));
-            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            const int end = min(kc + p.chunk, ks1);
+            for (int ks = kc; ks < end; ++ks) {
+                if (!mbar_wait_warp(bar_full(stage), phase, ctl, 2302)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t s = base + stage * C::STAGE_BYTES;
+                mma_stage<KIND, 1>(tmem_base + buf * TC, s, s + C::R_BYTES, idesc, ks == kc);
+                tc_commit<1>(bar_empty(stage));
+                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            }
+            if (ok) tc_commit<1>(bar_tfull(buf));
+            if (++buf == C::BUFS) { buf = 0; bphase ^= 1u; }
         }
-        if (ok) tc_commit<1>(bar_done);
     } else {
         griddep_wait();
         const uint32_t scales = base + C::OFF_SCALES;
@@ -230,37 +272,66 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
             for (int i = threadIdx.x; i < TC; i += 128) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
             asm volatile("bar.sync 1, 128;" ::: "memory");
         }
-        const bool ok = mbar_wait_warp(bar_done, 0, ctl, 2303);
-        tc_fence_after();
-        const uint32_t lane_taddr = tmem_base + ((uint32_t)(warp * 32) << 16);
-        constexpr int CH = TC < 32 ? TC : 32;
-        const int valid = min(TC, p.cols - col0);
-        if (shares == 1) {
-            const int row = row0 + warp * 32 + lane;
+        constexpr int CH = TC < 32 ? TC : 32, COLS = TC * 4 / C::OUT_WARPS;      // columns of a warp
+        const int quadrant = warp & 3, first = (warp >> 2) * COLS;
+        const uint32_t lane_taddr = tmem_base + ((uint32_t)(quadrant * 32) << 16);
+        const int valid = min(TC, p.cols - col0), row = row0 + quadrant * 32 + lane;
+        // share 1: the output; else a column-major tile of 128 x 4 bytes a column, over the operand ring, once every MMA of this CTA has
+        // read its operands
+        auto put = [&](const uint32_t (&v)[CH], int c, float r_scale, float bias) {
+            if (shares == 1) put_columns<KIND, CH>(p, v, row, col0 + c, valid - c, r_scale, bias, scales + 4 * c);
+            else {
+#pragma unroll
+                for (int j = 0; j < CH; ++j) sts32u(base + (c + j) * 512 + (quadrant * 32 + lane) * 4, v[j]);
+            }
+        };
+        if constexpr (KIND == INT8) {
             float r_scale = 0.0f, bias = 0.0f;
-            if constexpr (KIND == INT8) if (row < p.rows) { r_scale = p.r_scales[row]; bias = load_bias(p, row); }
+            if (shares == 1 && row < p.rows) { r_scale = p.r_scales[row]; bias = load_bias(p, row); }
+            const bool ok = mbar_wait_warp(bar_tfull(0), 0, ctl, 2303);
+            tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < valid; c += CH) {
+            for (int c = 0; c < valid && ok; c += CH) {
                 uint32_t v[CH];
                 if constexpr (CH == 32) tmem_ld32(lane_taddr + c, v); else tmem_ld16(lane_taddr + c, v);
                 tmem_ld_wait();
-                if (ok) put_columns<KIND, CH>(p, v, row, col0 + c, r_scale, bias, scales + 4 * c);
+                put(v, c, r_scale, bias);
             }
         } else {
-            // column-major tile of 128 x 4 bytes a column, over the operand ring: every MMA of this CTA has read its operands
-#pragma unroll 1
-            for (int c = 0; c < valid; c += CH) {
-                uint32_t v[CH];
-                if constexpr (CH == 32) tmem_ld32(lane_taddr + c, v); else tmem_ld16(lane_taddr + c, v);
-                tmem_ld_wait();
+            float sum[COLS / CH][CH];
+            int buf = 0; uint32_t bphase = 0;
+            bool ok = true;
+            for (int kc = ks0; kc < ks1; kc += p.chunk) {
+                if (!mbar_wait_warp(bar_tfull(buf), bphase, ctl, 2303)) { ok = false; break; }
+                tc_fence_after();
 #pragma unroll
-                for (int j = 0; j < CH; ++j) sts32u(base + (c + j) * 512 + (warp * 32 + lane) * 4, v[j]);
+                for (int c = 0; c < COLS; c += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(lane_taddr + buf * TC + first + c, v);
+                    tmem_ld_wait16(v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        float& s = sum[(c + j) / CH][(c + j) % CH];
+                        s = kc == ks0 ? __uint_as_float(v[j]) : s + __uint_as_float(v[j]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_tempty(buf));
+                if (++buf == C::BUFS) { buf = 0; bphase ^= 1u; }
+            }
+#pragma unroll
+            for (int i = 0; i < COLS / CH; ++i) {
+                uint32_t v[CH];
+#pragma unroll
+                for (int j = 0; j < CH; ++j) v[j] = __float_as_uint(sum[i][j]);
+                if (ok && first + i * CH < valid) put(v, first + i * CH, 0.0f, 0.0f);
             }
         }
     }
     if (shares > 1) {
         cluster_sync();                                      // every share is in its CTA's shared memory
-        if (warp < 4 && !*abort_flag) {
+        if (warp < C::OUT_WARPS && !*abort_flag) {
             const int valid = min(TC, p.cols - col0), row = row0 + 4 * lane;
             const uint32_t scales = base + C::OFF_SCALES;
             float r_scale[4] = {}, bias[4] = {};
@@ -268,8 +339,8 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < 4; ++i) if (row + i < p.rows) { r_scale[i] = p.r_scales[row + i]; bias[i] = load_bias(p, row + i); }
             }
-            // the tile's columns are dealt out to the cluster's 4 * shares warps
-            for (int c = rank * 4 + warp; c < valid; c += 4 * shares) {
+            // the tile's columns are dealt out to the cluster's output warps
+            for (int c = rank * C::OUT_WARPS + warp; c < valid; c += C::OUT_WARPS * shares) {
                 uint4 x[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) if (j < shares) x[j] = ld_cluster128u(map_to_cta(base + c * 512 + lane * 16, j));
@@ -285,7 +356,7 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t one[1] = {sum[i]};
-                    put_columns<KIND, 1>(p, one, row + i, col0 + c, r_scale[i], bias[i], scales + 4 * c);
+                    put_columns<KIND, 1>(p, one, row + i, col0 + c, 1, r_scale[i], bias[i], scales + 4 * c);
                 }
             }
         }
@@ -299,7 +370,7 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
     tc_fence_before();
     if (shares > 1) cluster_sync_relaxed();                  // the peers no longer read this CTA's shared memory
     else __syncthreads();
-    if (warp == 5) {
+    if (warp == C::OUT_WARPS + 1) {
         __syncwarp();
         tc_fence_after();
         tmem_dealloc<1>(tmem_base, C::TMEM_COLS);
@@ -314,11 +385,16 @@ struct PairCfg {
     static constexpr int TC = 256, R_BYTES = 128 * 128, S_BYTES = 128 * 128, STAGE_BYTES = R_BYTES + S_BYTES, STAGES = 6;
     static constexpr int OFF_SCALES = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALES + 2 * TC * 4, NUM_BARS = 2 * STAGES + 4;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;
+    // warp 0 TMA producer, warp 1 MMA issuer, warps 4..11 output: a TMEM lane quadrant and half of the columns each, the gradients' sums
+    // in registers
+    static constexpr int OUT_WARPS = 8, OUT_WARP0 = 4, THREADS = (OUT_WARP0 + OUT_WARPS) * 32;
+    static constexpr int REGS_AT_LAUNCH = 168, REGS_CTRL = 56, REGS_OUT = 216;
+    static_assert(128 * REGS_CTRL + OUT_WARPS * 32 * REGS_OUT <= THREADS * REGS_AT_LAUNCH, "register pool");
     static_assert(SMEM_BYTES <= 232448, "shared memory of a block");
 };
 
 template <int KIND>
-__global__ void __launch_bounds__(192, 1)
+__global__ void __launch_bounds__(PairCfg<KIND>::THREADS, 1)
 int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant__ CUtensorMap tmS, const ProductParams p)
 {
     using C = PairCfg<KIND>;
@@ -340,11 +416,11 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
     const bool leader = rank == 0;
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(bar_tfull(b), 1); mbar_init(bar_tempty(b), 2 * 4); }
+        for (int b = 0; b < 2; ++b) { mbar_init(bar_tfull(b), 1); mbar_init(bar_tempty(b), 2 * C::OUT_WARPS); }
         *abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 5) {
+    if (warp == 1) {
         tmem_alloc<2>(smem_u32(tmem_slot), 512);
         tmem_relinquish<2>();
     }
@@ -364,7 +440,9 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
         tc = in / rows;
     };
 
-    if (warp == 4) {
+    if (warp < C::OUT_WARP0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_CTRL));
+    if (warp == 0) {
         int stage = 0; uint32_t phase = 0;
         bool ok = true;
         griddep_wait();
@@ -384,57 +462,96 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
                 if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
             }
         }
-    } else if (warp == 5) {
+    } else if (warp == 1) {
         if (leader) {
             int stage = 0, buf = 0; uint32_t phase = 0, bphase = 0;
             const uint32_t idesc = p.idesc | ((uint32_t)(C::TC >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
             bool ok = true;
-            for (long long w = unit; w < tiles && ok; w += units) {
-                if (!mbar_wait_warp(bar_tempty(buf), bphase ^ 1u, ctl, 2312)) break;
-                tc_fence_after();
-                for (int ks = 0; ks < p.kstages; ++ks) {
-                    if (!mbar_wait_warp(bar_full(stage), phase, ctl, 2313)) { ok = false; break; }
+            for (long long w = unit; w < tiles && ok; w += units)
+                for (int kc = 0; kc < p.kstages && ok; kc += p.chunk) {
+                    if (!mbar_wait_warp(bar_tempty(buf), bphase ^ 1u, ctl, 2312)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t s = base + stage * C::STAGE_BYTES;
-                    mma_stage<KIND, 2>(tmem_base + buf * C::TC, s, s + C::R_BYTES, idesc, ks == 0);
-                    tc_commit<2>(bar_empty(stage));
-                    if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                    const int end = min(kc + p.chunk, p.kstages);
+                    for (int ks = kc; ks < end; ++ks) {
+                        if (!mbar_wait_warp(bar_full(stage), phase, ctl, 2313)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t s = base + stage * C::STAGE_BYTES;
+                        mma_stage<KIND, 2>(tmem_base + buf * C::TC, s, s + C::R_BYTES, idesc, ks == kc);
+                        tc_commit<2>(bar_empty(stage));
+                        if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+                    tc_commit<2>(bar_tfull(buf));
+                    if (++buf == 2) { buf = 0; bphase ^= 1u; }
                 }
-                if (!ok) break;
-                tc_commit<2>(bar_tfull(buf));
-                if (++buf == 2) { buf = 0; bphase ^= 1u; }
-            }
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS_OUT));
+        constexpr int COLS = C::TC / 2;                      // of a warp
+        const int quadrant = warp & 3, half = (warp - C::OUT_WARP0) >> 2;
+        const uint32_t lane_taddr = tmem_base + half * COLS + ((uint32_t)(quadrant * 32) << 16);
         int buf = 0; uint32_t bphase = 0;
+        bool ok = true;
         griddep_wait();
-        for (long long w = unit; w < tiles; w += units) {
-            int tr, tc;
-            place(w, tr, tc);
-            const int row = (2 * tr + rank) * 128 + warp * 32 + lane, col0 = tc * C::TC;
-            const uint32_t scales = base + C::OFF_SCALES + buf * C::TC * 4;
-            float r_scale = 0.0f, bias = 0.0f;
-            if constexpr (KIND == INT8) {
-                // (a warp is at most one tile behind the others, and the scales of two tiles are kept)
-                for (int i = threadIdx.x; i < C::TC; i += 128) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-                if (row < p.rows) { r_scale = p.r_scales[row]; bias = load_bias(p, row); }
-            }
-            if (!mbar_wait_warp(bar_tfull(buf), bphase, ctl, 2314)) break;
-            tc_fence_after();
-            const uint32_t taddr = tmem_base + buf * C::TC + ((uint32_t)(warp * 32) << 16);
-            const int valid = min(C::TC, p.cols - col0);
-#pragma unroll 1
-            for (int c = 0; c < valid; c += 32) {
-                uint32_t v[32];
-                tmem_ld32(taddr + c, v);
-                tmem_ld_wait();
-                put_columns<KIND, 32>(p, v, row, col0 + c, r_scale, bias, scales + 4 * c);
-            }
+        auto release = [&] {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(bar_tempty(buf) & PEER_BIT_MASK);
             if (++buf == 2) { buf = 0; bphase ^= 1u; }
+        };
+        for (long long w = unit; w < tiles && ok; w += units) {
+            int tr, tc;
+            place(w, tr, tc);
+            const int row = (2 * tr + rank) * 128 + quadrant * 32 + lane, col0 = tc * C::TC + half * COLS;
+            const int valid = min(COLS, p.cols - col0);
+            if constexpr (KIND == INT8) {
+                // (a warp is at most one tile behind the others, and the scales of two tiles are kept)
+                const uint32_t tile_scales = base + C::OFF_SCALES + buf * C::TC * 4, scales = tile_scales + half * COLS * 4;
+                for (int i = threadIdx.x - C::OUT_WARP0 * 32; i < C::TC; i += C::OUT_WARPS * 32) {
+                    const int col = tc * C::TC + i;
+                    sts32u(tile_scales + 4 * i, col < p.cols ? __float_as_uint(p.c_scales[col]) : 0u);
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(C::OUT_WARPS * 32) : "memory");
+                float r_scale = 0.0f, bias = 0.0f;
+                if (row < p.rows) { r_scale = p.r_scales[row]; bias = load_bias(p, row); }
+                if (!mbar_wait_warp(bar_tfull(buf), bphase, ctl, 2314)) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < valid; c += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(lane_taddr + buf * C::TC + c, v);
+                    tmem_ld_wait();
+                    put_columns<KIND, 32>(p, v, row, col0 + c, valid - c, r_scale, bias, scales + 4 * c);
+                }
+                release();
+            } else {
+                float sum[COLS / 32][32];
+                for (int kc = 0; kc < p.kstages; kc += p.chunk) {
+                    if (!mbar_wait_warp(bar_tfull(buf), bphase, ctl, 2314)) { ok = false; break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 0; c < COLS; c += 16) {
+                        uint32_t v[16];
+                        tmem_ld16(lane_taddr + buf * C::TC + c, v);
+                        tmem_ld_wait16(v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            float& s = sum[c / 32][c % 32 + j];
+                            s = kc == 0 ? __uint_as_float(v[j]) : s + __uint_as_float(v[j]);
+                        }
+                    }
+                    release();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < COLS / 32; ++i) {
+                    uint32_t v[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[i][j]);
+                    if (32 * i < valid) put_columns<KIND, 32>(p, v, row, col0 + 32 * i, valid - 32 * i, 0.0f, 0.0f, 0);
+                }
+            }
         }
     }
     // ---------------------------------------------------------------------- teardown
@@ -445,7 +562,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     cluster_sync();                                          // the peer no longer signals this CTA's barriers
-    if (warp == 5) {
+    if (warp == 1) {
         __syncwarp();
         tc_fence_after();
         tmem_dealloc<2>(tmem_base, 512);
@@ -496,11 +613,11 @@ template <typename K> bool raise_smem(K kernel, int bytes, std::atomic<bool>* do
 }
 
 template <typename K>
-fmm_status_t launch_kernel(K kernel, unsigned grid, int smem, unsigned cluster, const CUtensorMap& r, const CUtensorMap& s, const ProductParams& p, cudaStream_t st)
+fmm_status_t launch_kernel(K kernel, unsigned grid, unsigned threads, int smem, unsigned cluster, const CUtensorMap& r, const CUtensorMap& s, const ProductParams& p, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(192); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -520,7 +637,7 @@ fmm_status_t launch_cluster(ProductParams p, const Operand& r, const Operand& s,
     p.tiles_r = (p.rows + 127) / 128; p.tiles_c = (p.cols + TC - 1) / TC; p.k_shares = shares;
     const int64_t grid = (int64_t)p.tiles_r * p.tiles_c * shares;
     if (grid > 0x7FFFFFFF) return FMM_ERR_SHAPE;
-    return launch_kernel(int8_cluster_kernel<KIND, TC>, (unsigned)grid, C::SMEM_BYTES, (unsigned)shares, tmR, tmS, p, st);
+    return launch_kernel(int8_cluster_kernel<KIND, TC>, (unsigned)grid, C::THREADS, C::SMEM_BYTES, (unsigned)shares, tmR, tmS, p, st);
 }
 
 template <int KIND>
@@ -534,7 +651,7 @@ fmm_status_t launch_pair(ProductParams p, const Operand& r, const Operand& s, cu
     p.tiles_r = (p.rows + 255) / 256; p.tiles_c = (p.cols + 255) / 256; p.k_shares = 1;
     // as few pairs as finish in the same number of waves
     const int64_t tiles = (int64_t)p.tiles_r * p.tiles_c, most = std::max(1, fmm_sm_count() / 2), waves = (tiles + most - 1) / most;
-    return launch_kernel(int8_pair_kernel<KIND>, (unsigned)((tiles + waves - 1) / waves * 2), C::SMEM_BYTES, 2, tmR, tmS, p, st);
+    return launch_kernel(int8_pair_kernel<KIND>, (unsigned)((tiles + waves - 1) / waves * 2), C::THREADS, C::SMEM_BYTES, 2, tmR, tmS, p, st);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -611,6 +728,7 @@ fmm_status_t grad(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* co
     }
     const uint32_t format = type == FMM_TYPE_BF16 ? 1u : 0u;
     p.kstages = (int)ceil_div(contraction, 64);
+    p.chunk = out_type == FMM_TYPE_F32 ? CHUNK : p.kstages;
     p.idesc = (1u << 4) | (format << 7) | (format << 10) | (1u << 15) | ((KIND == GRAD_W ? 1u : 0u) << 16);
     return launch_product<KIND>(p, {workspace, code_rows, K, w.ld_codes}, dy, st);
 }
@@ -636,7 +754,7 @@ fmm_status_t fmm_int8_matmul(const int8_t* A, int64_t lda, const float* a_scales
     if (K == 0) return launch_empty(p, st);
     if (!A || !B || !a_scales || !b_scales || (((uintptr_t)a_scales | (uintptr_t)b_scales) & 3) || lda < K || ldb < K ||
         !int8_aligned(A, lda, 16) || !int8_aligned(B, ldb, 16)) return FMM_ERR_INVALID_ARG;
-    p.kstages = (int)ceil_div(K, 128);
+    p.kstages = p.chunk = (int)ceil_div(K, 128);
     p.idesc = (2u << 4) | (1u << 7) | (1u << 10);
     return launch_product<INT8>(p, {B, N, K, ldb}, {A, M, K, lda}, st);
 }

@@ -148,13 +148,14 @@ __device__ __forceinline__ void codes_to_float(uint2 c, float (&f)[8])
 // ---------------------------------------------------------------------------------------- quantization of a block
 // Maxima are taken over the bit patterns of |x|: they order like the numbers, infinities above them and NaN above those, so
 // that a block that holds one of these is seen, and gets NaN as its scale.
-__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+// (The three-operand maximum of magnitudes, NaN if one is, halves what finding the maximum costs against masks and integer maxima:
+// the kernels issue in 2 of 3 cycles.)
+__device__ __forceinline__ float abs_max3(float a, float b, float c)
+{ float d; asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
 __device__ __forceinline__ uint32_t abs_max8(const float (&f)[8])
 {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(f[i]));
-    return m;
+    const float m = abs_max3(abs_max3(f[0], f[1], f[2]), f[3], f[4]);
+    return __float_as_uint(abs_max3(m, f[5], abs_max3(f[6], f[7], 0.0f)));
 }
 struct Scale { float scale, inverse; };
 __device__ __forceinline__ Scale block_scale(uint32_t amax_bits, bool pow2)
@@ -783,6 +784,7 @@ dim3 flat_block(int cols)
     while (x < 256 && 8u * FLAT_VPT * x < (unsigned)cols) x *= 2;
     return dim3(x, 256 / x);
 }
+// (a block per row instead of 32 blocks an SM: 16384 x 8192 bf16 quantized in 77.7 instead of 74.2 us, restored in 68.0 instead of 63.8)
 unsigned flat_grid(int rows, dim3 block)
 {
     const int64_t need = ((int64_t)rows + block.y - 1) / block.y, most = (int64_t)fmm_sm_count() * 32;

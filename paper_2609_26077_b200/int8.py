@@ -20,7 +20,6 @@ ValueError (shapes, strides), anything that the library refuses raises fmm.FmmEr
 from __future__ import annotations
 
 import collections
-import contextlib
 import ctypes as C
 
 import torch
@@ -76,23 +75,26 @@ def lib():
 
 
 # ------------------------------------------------------------------------------------------------ checks
+# (The calls of one token are bound by what Python does for them: a microsecond each for a context manager, an allocation, a few
+# checks.  So the checks read every attribute once and the usual device and stream take no context.)
 def _matrix(t, name, dtype, shape=None):
     """A 2-D CUDA tensor with contiguous columns; its row distance."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name}: a CUDA tensor is needed")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} is needed, not {t.dtype}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, {'two dimensions are' if shape is None else f'{shape} is'} needed")
-    rows, cols = t.shape
+    size = t.shape
+    if len(size) != 2 or (shape is not None and size != shape):
+        raise ValueError(f"{name}: shape {tuple(size)}, {'two dimensions are' if shape is None else f'{tuple(shape)} is'} needed")
+    rows, cols = size
     ld, step = t.stride()
-    if cols > 1 and step != 1:
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: columns are not contiguous")
-    if rows > 1:
-        if ld < cols:
+    if ld < cols or ld < 1:
+        if rows > 1 and cols > 0:
             raise ValueError(f"{name}: rows overlap or run backwards")
-        return ld
-    return max(ld, cols) if cols > 1 else max(cols, 1)
+        ld = max(cols, 1)
+    return ld
 
 
 def _vector(t, name, dtype, shape):
@@ -100,14 +102,15 @@ def _vector(t, name, dtype, shape):
         raise TypeError(f"{name}: a CUDA tensor is needed")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} is needed, not {t.dtype}")
-    if tuple(t.shape) != shape or not t.is_contiguous():
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous tensor of shape {shape} is needed, not {tuple(t.shape)}")
 
 
 def _float_type(dtype, name):
-    if dtype not in _TYPES:
+    kind = _TYPES.get(dtype)
+    if kind is None:
         raise TypeError(f"{name}: float32, bfloat16 or float16 is needed, not {dtype}")
-    return _TYPES[dtype]
+    return kind
 
 
 def _block(block, name="block"):
@@ -121,32 +124,31 @@ def _scale_shape(rows, cols, block):
 
 
 def _same_device(first, *tensors):
+    device = first.device
     for t in tensors:
-        if t is not None and t.device != first.device:
-            raise TypeError(f"tensors on {first.device} and {t.device} in one call")
+        if t is not None and t.device != device:
+            raise TypeError(f"tensors on {device} and {t.device} in one call")
 
 
-_here = contextlib.nullcontext()
-
-
-def _on(t, stream):
-    """The context in which a call on t's device and on `stream` allocates and launches."""
+def _elsewhere(t, stream):
+    """None where a call can run on the current device and stream, else the context in which it can."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("a CUDA tensor is needed")
     if stream is not None:
         if stream.device != t.device:
             raise TypeError(f"a stream of {stream.device} for tensors on {t.device}")
         return torch.cuda.stream(stream)
-    return _here if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+    return None if t.device.index == torch._C._cuda_getDevice() else torch.cuda.device(t.device)
+
+
+_empty = torch.empty
 
 
 def _new_codes(rows, cols, device):
     """Codes whose rows are a multiple of 16 bytes apart."""
     if cols % 16 == 0:
-        return torch.empty((rows, cols), dtype=torch.int8, device=device)
-    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
-
-
-def _new(shape, dtype, device):
-    return torch.empty(shape, dtype=dtype, device=device)
+        return _empty((rows, cols), dtype=torch.int8, device=device)
+    return _empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
 
 
 def _call(status, what):
@@ -154,38 +156,64 @@ def _call(status, what):
         fmm._check(status, what)
 
 
+_needs = {}
+
+
+def _need(name, *sizes):
+    """Workspace bytes by the library's function of that name (remembered by sizes and device)."""
+    key = (name, torch._C._cuda_getDevice(), sizes)
+    need = _needs.get(key)
+    if need is None:
+        b = C.c_size_t()
+        _call(getattr(lib(), name)(*sizes, C.byref(b)), name)
+        if len(_needs) >= 1024:
+            _needs.clear()
+        need = _needs[key] = b.value
+    return need
+
+
 # ------------------------------------------------------------------------------------------------ operators
 def quantize(x, block=0, pow2=False, out=None, stream=None):
     """Codes and scales of x (rows x cols): one scale per row, or per block of 32 or 128 columns of a row; with pow2 each is
     a power of two.  out: (codes, scales) to write to."""
+    where = _elsewhere(x, stream)
+    if where is not None:
+        with where:
+            return quantize(x, block, pow2, out)
     kind = _float_type(x.dtype, "x")
     ldx = _matrix(x, "x", x.dtype)
     rows, cols = x.shape
     shape = _scale_shape(rows, cols, _block(block))
-    with _on(x, stream):
-        codes, scales = out if out is not None else (_new_codes(rows, cols, x.device), _new(shape, torch.float32, x.device))
+    if out is None:
+        codes, scales = _new_codes(rows, cols, x.device), _empty(shape, dtype=torch.float32, device=x.device)
+        ldc = codes.stride(0) or 1
+    else:
+        codes, scales = out
         ldc = _matrix(codes, "codes", torch.int8, (rows, cols))
         _vector(scales, "scales", torch.float32, shape)
         _same_device(x, codes, scales)
-        _call(lib().fmm_int8_quantize(x.data_ptr(), kind, ldx, rows, cols, block, POW2 if pow2 else AMAX_DIV_127, codes.data_ptr(), ldc,
-                                      scales.data_ptr(), fmm._stream_ptr(None)), "fmm_int8_quantize")
+    _call((_lib or lib()).fmm_int8_quantize(x.data_ptr(), kind, ldx, rows, cols, block, POW2 if pow2 else AMAX_DIV_127, codes.data_ptr(), ldc,
+                                            scales.data_ptr(), fmm._stream_ptr(None)), "fmm_int8_quantize")
     return codes, scales
 
 
 def dequantize(codes, scales, block=0, dtype=torch.bfloat16, out=None, stream=None):
     """The values that codes stand for, code * scale, in `dtype` (or out's type)."""
+    where = _elsewhere(codes, stream)
+    if where is not None:
+        with where:
+            return dequantize(codes, scales, block, dtype, out)
     ldc = _matrix(codes, "codes", torch.int8)
     rows, cols = codes.shape
     _vector(scales, "scales", torch.float32, _scale_shape(rows, cols, _block(block)))
-    with _on(codes, stream):
-        if out is None:
-            kind, out = _float_type(dtype, "dtype"), _new((rows, cols), dtype, codes.device)
-        else:
-            kind = _float_type(out.dtype, "out")
+    if out is None:
+        kind, out, ldx = _float_type(dtype, "dtype"), _empty((rows, cols), dtype=dtype, device=codes.device), cols
+    else:
+        kind = _float_type(out.dtype, "out")
         ldx = _matrix(out, "out", out.dtype, (rows, cols))
-        _same_device(codes, scales, out)
-        _call(lib().fmm_int8_dequantize(codes.data_ptr(), ldc, scales.data_ptr(), rows, cols, block, out.data_ptr(), kind, ldx,
-                                        fmm._stream_ptr(None)), "fmm_int8_dequantize")
+    _same_device(codes, scales, out)
+    _call((_lib or lib()).fmm_int8_dequantize(codes.data_ptr(), ldc, scales.data_ptr(), rows, cols, block, out.data_ptr(), kind, ldx,
+                                              fmm._stream_ptr(None)), "fmm_int8_dequantize")
     return out
 
 
@@ -201,64 +229,79 @@ def rms_norm(x, gain, residual=None, eps=1e-6, pow2=False, checkpoint=0, hidden=
         rstd                           1 / rms(h) per row
         checkpoint, checkpoint_scales  8-bit form of h in blocks of `checkpoint` (32 or 128) columns; None with 0
     """
-    kind = _float_type(x.dtype, "x")
-    a = RmsNormArgs(kind, POW2 if pow2 else AMAX_DIV_127, _block(checkpoint, "checkpoint"))
-    a.ldx = _matrix(x, "x", x.dtype)
+    where = _elsewhere(x, stream)
+    if where is not None:
+        with where:
+            return rms_norm(x, gain, residual, eps, pow2, checkpoint, hidden)
+    dtype, device = x.dtype, x.device
+    kind = _float_type(dtype, "x")
+    ldx = _matrix(x, "x", dtype)
     rows, cols = x.shape
-    _vector(gain, "gain", x.dtype, (cols,))
-    with _on(x, stream):
-        if residual is not None:
-            a.ldr = _matrix(residual, "residual", x.dtype, (rows, cols))
-            if hidden is None:
-                hidden = _new((rows, cols), x.dtype, x.device)
-            a.ldh = _matrix(hidden, "hidden", x.dtype, (rows, cols))
-            a.residual, a.hidden = residual.data_ptr(), hidden.data_ptr()
-        elif hidden is not None:
-            raise ValueError("hidden: written with a residual only")
-        codes, scales, rstd = _new_codes(rows, cols, x.device), _new((rows,), torch.float32, x.device), _new((rows,), torch.float32, x.device)
-        kept = kept_scales = None
-        if checkpoint:
-            kept, kept_scales = _new_codes(rows, cols, x.device), _new(_scale_shape(rows, cols, checkpoint), torch.float32, x.device)
-            a.checkpoint, a.ldk, a.checkpoint_scales = kept.data_ptr(), kept.stride(0), kept_scales.data_ptr()
-        _same_device(x, gain, residual, hidden)
-        a.rows, a.cols, a.eps, a.x, a.gain = rows, cols, eps, x.data_ptr(), gain.data_ptr()
-        a.codes, a.ldc, a.scales, a.rstd = codes.data_ptr(), codes.stride(0), scales.data_ptr(), rstd.data_ptr()
-        _call(lib().fmm_int8_rms_norm(C.byref(a), fmm._stream_ptr(None)), "fmm_int8_rms_norm")
+    _vector(gain, "gain", dtype, (cols,))
+    ldr = ldh = ldk = 0
+    at_residual = at_hidden = at_kept = at_kept_scales = None
+    if residual is not None:
+        ldr = _matrix(residual, "residual", dtype, (rows, cols))
+        if hidden is None:
+            hidden, ldh = _empty((rows, cols), dtype=dtype, device=device), cols
+        else:
+            ldh = _matrix(hidden, "hidden", dtype, (rows, cols))
+        at_residual, at_hidden = residual.data_ptr(), hidden.data_ptr()
+    elif hidden is not None:
+        raise ValueError("hidden: written with a residual only")
+    _same_device(x, gain, residual, hidden)
+    codes = _new_codes(rows, cols, device)
+    scales, rstd = _empty((2, rows), dtype=torch.float32, device=device).unbind()
+    kept = kept_scales = None
+    if checkpoint:
+        kept = _new_codes(rows, cols, device)
+        kept_scales = _empty(_scale_shape(rows, cols, _block(checkpoint, "checkpoint")), dtype=torch.float32, device=device)
+        at_kept, ldk, at_kept_scales = kept.data_ptr(), kept.stride(0), kept_scales.data_ptr()
+    a = RmsNormArgs(kind, POW2 if pow2 else AMAX_DIV_127, checkpoint, rows, cols, eps, x.data_ptr(), ldx, at_residual, ldr, gain.data_ptr(),
+                    at_hidden, ldh, codes.data_ptr(), codes.stride(0), scales.data_ptr(), rstd.data_ptr(), at_kept, ldk, at_kept_scales)
+    _call((_lib or lib()).fmm_int8_rms_norm(C.byref(a), fmm._stream_ptr(None)), "fmm_int8_rms_norm")
     return Norm(x if residual is None else hidden, codes, scales, rstd, kept, kept_scales)
 
 
 def rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block=128, dresidual=None, dx=None, stream=None):
     """(dx, dgain) of the norm, from the checkpoint of its hidden rows and their rstd.  dx, the gradient of x and of residual,
     includes dresidual, the gradient that reaches the hidden rows elsewhere; it may be dy or dresidual.  dgain is float32."""
-    kind = _float_type(dy.dtype, "dy")
-    a = RmsNormBackwardArgs(kind, _block(block))
-    a.ldy = _matrix(dy, "dy", dy.dtype)
+    where = _elsewhere(dy, stream)
+    if where is not None:
+        with where:
+            return rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block, dresidual, dx)
+    dtype, device = dy.dtype, dy.device
+    kind = _float_type(dtype, "dy")
+    ldy = _matrix(dy, "dy", dtype)
     rows, cols = dy.shape
-    a.ldk = _matrix(checkpoint, "checkpoint", torch.int8, (rows, cols))
-    _vector(checkpoint_scales, "checkpoint_scales", torch.float32, _scale_shape(rows, cols, block))
+    ldk = _matrix(checkpoint, "checkpoint", torch.int8, (rows, cols))
+    _vector(checkpoint_scales, "checkpoint_scales", torch.float32, _scale_shape(rows, cols, _block(block)))
     _vector(rstd, "rstd", torch.float32, (rows,))
-    _vector(gain, "gain", dy.dtype, (cols,))
-    with _on(dy, stream):
-        if dresidual is not None:
-            a.ldr = _matrix(dresidual, "dresidual", dy.dtype, (rows, cols))
-            a.dresidual = dresidual.data_ptr()
-        if dx is None:
-            dx = _new((rows, cols), dy.dtype, dy.device)
-        a.ldx = _matrix(dx, "dx", dy.dtype, (rows, cols))
-        _same_device(dy, checkpoint, checkpoint_scales, rstd, gain, dresidual, dx)
-        dgain = _new((cols,), torch.float32, dy.device)
-        need = C.c_size_t()
-        _call(lib().fmm_int8_rms_norm_backward_workspace_bytes(rows, cols, C.byref(need)), "fmm_int8_rms_norm_backward_workspace_bytes")
-        workspace = _new((need.value,), torch.uint8, dy.device)
-        a.rows, a.cols, a.dy, a.checkpoint, a.checkpoint_scales = rows, cols, dy.data_ptr(), checkpoint.data_ptr(), checkpoint_scales.data_ptr()
-        a.rstd, a.gain, a.dx, a.dgain = rstd.data_ptr(), gain.data_ptr(), dx.data_ptr(), dgain.data_ptr()
-        _call(lib().fmm_int8_rms_norm_backward(C.byref(a), workspace.data_ptr(), need.value, fmm._stream_ptr(None)), "fmm_int8_rms_norm_backward")
+    _vector(gain, "gain", dtype, (cols,))
+    ldr, at_dresidual = 0, None
+    if dresidual is not None:
+        ldr, at_dresidual = _matrix(dresidual, "dresidual", dtype, (rows, cols)), dresidual.data_ptr()
+    if dx is None:
+        dx, ldx = _empty((rows, cols), dtype=dtype, device=device), cols
+    else:
+        ldx = _matrix(dx, "dx", dtype, (rows, cols))
+    _same_device(dy, checkpoint, checkpoint_scales, rstd, gain, dresidual, dx)
+    dgain = _empty((cols,), dtype=torch.float32, device=device)
+    need = _need("fmm_int8_rms_norm_backward_workspace_bytes", rows, cols)
+    workspace = _empty((need,), dtype=torch.uint8, device=device)
+    a = RmsNormBackwardArgs(kind, block, rows, cols, dy.data_ptr(), ldy, checkpoint.data_ptr(), ldk, checkpoint_scales.data_ptr(), rstd.data_ptr(),
+                            gain.data_ptr(), at_dresidual, ldr, dx.data_ptr(), ldx, dgain.data_ptr())
+    _call((_lib or lib()).fmm_int8_rms_norm_backward(C.byref(a), workspace.data_ptr(), need, fmm._stream_ptr(None)), "fmm_int8_rms_norm_backward")
     return dx, dgain
 
 
 def matmul(a, a_scales, b, b_scales, bias=None, dtype=torch.bfloat16, out=None, stream=None):
     """a (M x K codes, a scale per row) times the transpose of b (N x K codes, a scale per row), plus bias (N): M x N in
     `dtype` (or out's type).  The rows of a and b start on 16-byte boundaries; K is at most 131071."""
+    where = _elsewhere(a, stream)
+    if where is not None:
+        with where:
+            return matmul(a, a_scales, b, b_scales, bias, dtype, out)
     lda = _matrix(a, "a", torch.int8)
     M, K = a.shape
     ldb = _matrix(b, "b", torch.int8)
@@ -266,70 +309,85 @@ def matmul(a, a_scales, b, b_scales, bias=None, dtype=torch.bfloat16, out=None, 
     if b.shape[1] != K:
         raise ValueError(f"a and b have {K} and {b.shape[1]} columns")
     # a single row need not be any distance from the next
-    lda, ldb = lda if M > 1 else (K + 15) // 16 * 16, ldb if N > 1 else (K + 15) // 16 * 16
-    if K and (lda % 16 or ldb % 16 or (M and a.data_ptr() % 16) or (N and b.data_ptr() % 16)):
+    if M == 1:
+        lda = (K + 15) // 16 * 16
+    if N == 1:
+        ldb = (K + 15) // 16 * 16
+    at_a, at_b = a.data_ptr(), b.data_ptr()
+    if (lda | ldb | at_a | at_b) & 15 and M and N and K:
         raise ValueError("a and b: rows have to start on 16-byte boundaries (as those of quantize and rms_norm do)")
     _vector(a_scales, "a_scales", torch.float32, (M,))
     _vector(b_scales, "b_scales", torch.float32, (N,))
-    with _on(a, stream):
-        if out is None:
-            kind, out = _float_type(dtype, "dtype"), _new((M, N), dtype, a.device)
-        else:
-            kind = _float_type(out.dtype, "out")
-        ldc = _matrix(out, "out", out.dtype, (M, N))
-        if bias is not None:
-            _vector(bias, "bias", out.dtype, (N,))
-        _same_device(a, a_scales, b, b_scales, bias, out)
-        _call(lib().fmm_int8_matmul(a.data_ptr(), lda, a_scales.data_ptr(), b.data_ptr(), ldb, b_scales.data_ptr(),
-                                    None if bias is None else bias.data_ptr(), M, N, K, out.data_ptr(), kind, ldc, fmm._stream_ptr(None)),
-              "fmm_int8_matmul")
+    if out is None:
+        kind, out, ldc = _float_type(dtype, "dtype"), _empty((M, N), dtype=dtype, device=a.device), N
+    else:
+        dtype = out.dtype
+        kind = _float_type(dtype, "out")
+        ldc = _matrix(out, "out", dtype, (M, N))
+    if bias is not None:
+        _vector(bias, "bias", dtype, (N,))
+    _same_device(a, a_scales, b, b_scales, bias, out)
+    _call((_lib or lib()).fmm_int8_matmul(at_a, lda, a_scales.data_ptr(), at_b, ldb, b_scales.data_ptr(), None if bias is None else bias.data_ptr(),
+                                          M, N, K, out.data_ptr(), kind, ldc, fmm._stream_ptr(None)), "fmm_int8_matmul")
     return out
 
 
-def _grad(what, dy, codes, scales, shape, dtype, out, accumulate, stream):
-    if dy.dtype not in (torch.bfloat16, torch.float16):
-        raise TypeError(f"dy: bfloat16 or float16 is needed, not {dy.dtype}")
-    ldy = _matrix(dy, "dy", dy.dtype)
+def _grad(what, dy, codes, scales, shape, dtype, out, accumulate):
+    kind = dy.dtype
+    if kind is not torch.bfloat16 and kind is not torch.float16:
+        raise TypeError(f"dy: bfloat16 or float16 is needed, not {kind}")
+    ldy = _matrix(dy, "dy", kind)
     ldc = _matrix(codes, "codes", torch.int8)
     M, N = dy.shape
     code_rows, K = codes.shape
     _vector(scales, "scales", torch.float32, (code_rows,))
-    with _on(dy, stream):
-        if out is None:
-            if accumulate:
-                raise ValueError("accumulate: needs out")
-            out = _new(shape, dy.dtype if dtype is None else dtype, dy.device)
-        if out.dtype not in (torch.float32, dy.dtype):
-            raise TypeError(f"the gradient is float32 or of dy's type, not {out.dtype}")
-        ldo = _matrix(out, "out", out.dtype, shape)
-        _same_device(dy, codes, scales, out)
-        aligned = dy.data_ptr() % 16 == 0 and ldy % 8 == 0
-        need = C.c_size_t()
-        _call(lib().fmm_int8_grad_workspace_bytes(code_rows, K, M, N, int(aligned), C.byref(need)), "fmm_int8_grad_workspace_bytes")
-        workspace = _new((need.value,), torch.uint8, dy.device)
-        tail = (workspace.data_ptr(), need.value, fmm._stream_ptr(None))
-        head = (dy.data_ptr(), _TYPES[dy.dtype], ldy, codes.data_ptr(), ldc, scales.data_ptr(), M, N, K, out.data_ptr(), _TYPES[out.dtype], ldo)
-        if what == "fmm_int8_grad_weight":
-            _call(lib().fmm_int8_grad_weight(*head, int(accumulate), *tail), what)
-        else:
-            _call(lib().fmm_int8_grad_input(*head, *tail), what)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate: needs out")
+        dtype = kind if dtype is None else dtype
+        if dtype is not torch.float32 and dtype is not kind:
+            raise TypeError(f"the gradient is float32 or of dy's type, not {dtype}")
+        out, ldo = _empty(shape, dtype=dtype, device=dy.device), shape[1]
+    else:
+        dtype = out.dtype
+        if dtype is not torch.float32 and dtype is not kind:
+            raise TypeError(f"the gradient is float32 or of dy's type, not {dtype}")
+        ldo = _matrix(out, "out", dtype, shape)
+    _same_device(dy, codes, scales, out)
+    at = dy.data_ptr()
+    need = _need("fmm_int8_grad_workspace_bytes", code_rows, K, M, N, int(not (at & 15 or ldy & 7)))
+    workspace = _empty((need,), dtype=torch.uint8, device=dy.device)
+    head = (at, _TYPES[kind], ldy, codes.data_ptr(), ldc, scales.data_ptr(), M, N, K, out.data_ptr(), _TYPES[dtype], ldo)
+    tail = (workspace.data_ptr(), need, fmm._stream_ptr(None))
+    if what == "fmm_int8_grad_weight":
+        _call((_lib or lib()).fmm_int8_grad_weight(*head, int(accumulate), *tail), what)
+    else:
+        _call((_lib or lib()).fmm_int8_grad_input(*head, *tail), what)
     return out
 
 
 def grad_weight(dy, codes, scales, dtype=torch.float32, out=None, accumulate=False, stream=None):
     """Gradient of matmul's b: dy^T (M x N, 16-bit) times the activations that codes (M x K) and scales stand for: N x K in
     `dtype` (float32 or dy's type).  With accumulate it is added to out."""
-    if dy.dim() == 2 and codes.dim() == 2 and codes.shape[0] != dy.shape[0]:
-        raise ValueError(f"dy and codes have {dy.shape[0]} and {codes.shape[0]} rows")
-    return _grad("fmm_int8_grad_weight", dy, codes, scales, (dy.shape[-1], codes.shape[-1]), dtype, out, accumulate, stream)
+    where = _elsewhere(dy, stream)
+    if where is not None:
+        with where:
+            return grad_weight(dy, codes, scales, dtype, out, accumulate)
+    if dy.dim() != 2 or codes.dim() != 2 or codes.shape[0] != dy.shape[0]:
+        raise ValueError(f"dy and codes: two dimensions and as many rows are needed, not {tuple(dy.shape)} and {tuple(codes.shape)}")
+    return _grad("fmm_int8_grad_weight", dy, codes, scales, (dy.shape[1], codes.shape[1]), dtype, out, accumulate)
 
 
 def grad_input(dy, codes, scales, dtype=None, out=None, stream=None):
     """Gradient of matmul's a: dy (M x N, 16-bit) times the weight that codes (N x K) and scales stand for: M x K in `dtype`
     (float32 or dy's type, the default)."""
-    if dy.dim() == 2 and codes.dim() == 2 and codes.shape[0] != dy.shape[1]:
-        raise ValueError(f"dy has {dy.shape[1]} columns, codes {codes.shape[0]} rows")
-    return _grad("fmm_int8_grad_input", dy, codes, scales, (dy.shape[0], codes.shape[-1]), dtype, out, False, stream)
+    where = _elsewhere(dy, stream)
+    if where is not None:
+        with where:
+            return grad_input(dy, codes, scales, dtype, out)
+    if dy.dim() != 2 or codes.dim() != 2 or codes.shape[0] != dy.shape[1]:
+        raise ValueError(f"dy and codes: two dimensions and dy's columns as codes' rows are needed, not {tuple(dy.shape)} and {tuple(codes.shape)}")
+    return _grad("fmm_int8_grad_input", dy, codes, scales, (dy.shape[0], codes.shape[1]), dtype, out, False)
 
 
 def status():
