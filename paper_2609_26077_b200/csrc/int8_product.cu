@@ -25,6 +25,7 @@
 // The 8-bit operand of a gradient is restored to 16 bits by fmm_int8_dequantize into the workspace before the product: 3 bytes a code
 // once, against 2 M N K operations.  Restoring it tile by tile on the way into the tensor cores would take two more passes
 // through shared memory per tile (codes in, 16-bit values out), which the product's own operand traffic already fills.
+#include <math.h>
 #include <algorithm>
 #include "fmm_gemm_common.cuh"
 #include "int8_internal.h"
@@ -44,6 +45,8 @@ __device__ __forceinline__ uint4 ld_cluster128u(uint32_t addr)
     asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm)
+{ asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory"); }
 __device__ __forceinline__ void sts32u(uint32_t addr, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 
 // warp-collective, as the MMAs of fmm_ptx.cuh
@@ -77,6 +80,7 @@ struct ProductParams {
     const float* r_scales; const float* c_scales; const void* bias;      // INT8
     void* out; long long ldo;
     int out_type, accumulate;
+    int behind;                     // launched behind a kernel of the same call: may be set up while that one drains
     Int8Ranges ranges;
 };
 
@@ -213,6 +217,7 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
     const Ctl ctl{abort_flag, g_int8_product_status};
 
     const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (warp == C::OUT_WARPS && elect_one()) { prefetch_map(&tmR); prefetch_map(&tmS); }
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
         for (int b = 0; b < C::BUFS; ++b) { mbar_init(bar_tfull(b), 1); mbar_init(bar_tempty(b), C::OUT_WARPS); }
@@ -414,6 +419,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
     const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int rank = (int)warp_uniform(cluster_ctarank());
     const bool leader = rank == 0;
+    if (warp == 2 && elect_one()) { prefetch_map(&tmR); prefetch_map(&tmS); }
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(bar_tfull(b), 1); mbar_init(bar_tempty(b), 2 * C::OUT_WARPS); }
@@ -618,26 +624,16 @@ fmm_status_t launch_kernel(K kernel, unsigned grid, unsigned threads, int smem, 
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3(grid); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
+    // behind the kernel that restores its operand; its warps wait for that one before their first load or store.  (The first kernel of
+    // a call is launched in full stream order, as everywhere in this library.)
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = p.behind ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kernel, r, s, p) != cudaSuccess) { cudaGetLastError(); return FMM_ERR_CUDA; }
     return FMM_OK;
-}
-
-template <int KIND, int TC>
-fmm_status_t launch_cluster(ProductParams p, const Operand& r, const Operand& s, int shares, cudaStream_t st)
-{
-    using C = ClusterCfg<KIND, TC>;
-    static std::atomic<bool> done[64];
-    CUtensorMap tmR, tmS;
-    if (!make_operand_map<KIND, R_MN<KIND>>(&tmR, r, 128) || !make_operand_map<KIND, S_MN<KIND>>(&tmS, s, TC) ||
-        !raise_smem(int8_cluster_kernel<KIND, TC>, C::SMEM_BYTES, done)) return FMM_ERR_CUDA;
-    p.tiles_r = (p.rows + 127) / 128; p.tiles_c = (p.cols + TC - 1) / TC; p.k_shares = shares;
-    const int64_t grid = (int64_t)p.tiles_r * p.tiles_c * shares;
-    if (grid > 0x7FFFFFFF) return FMM_ERR_SHAPE;
-    return launch_kernel(int8_cluster_kernel<KIND, TC>, (unsigned)grid, C::THREADS, C::SMEM_BYTES, (unsigned)shares, tmR, tmS, p, st);
 }
 
 template <int KIND>
@@ -654,25 +650,71 @@ fmm_status_t launch_pair(ProductParams p, const Operand& r, const Operand& s, cu
     return launch_kernel(int8_pair_kernel<KIND>, (unsigned)((tiles + waves - 1) / waves * 2), C::THREADS, C::SMEM_BYTES, 2, tmR, tmS, p, st);
 }
 
+template <int KIND, int TC>
+fmm_status_t launch_cluster(ProductParams p, const Operand& r, const Operand& s, int shares, cudaStream_t st)
+{
+    using C = ClusterCfg<KIND, TC>;
+    static std::atomic<bool> done[64];
+    CUtensorMap tmR, tmS;
+    if (!make_operand_map<KIND, R_MN<KIND>>(&tmR, r, 128) || !make_operand_map<KIND, S_MN<KIND>>(&tmS, s, TC) ||
+        !raise_smem(int8_cluster_kernel<KIND, TC>, C::SMEM_BYTES, done)) return FMM_ERR_CUDA;
+    p.tiles_r = (p.rows + 127) / 128; p.tiles_c = (p.cols + TC - 1) / TC; p.k_shares = shares;
+    const int64_t grid = (int64_t)p.tiles_r * p.tiles_c * shares;
+    if (grid > 0x7FFFFFFF) return launch_pair<KIND>(p, r, s, st);       // (the model never chooses so many)
+    return launch_kernel(int8_cluster_kernel<KIND, TC>, (unsigned)grid, C::THREADS, C::SMEM_BYTES, (unsigned)shares, tmR, tmS, p, st);
+}
+
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Time models of the two kernels in microseconds (a gradient's with the restoring of its operand), fitted to 3100 timed calls of both with
+// every tile width and number of shares: 1 to 2048 tokens, 512 to 16384 channels, K of 512 to 8192; gradients of 64 to 16384 tokens, 128 to 2048
+// channels each way.  Cluster kernel: lat + rounds * fixed + the stages of an SM, of a single CTA (`stage` each) or of as many as it
+// holds (`shared` each), + what the exchange takes; a share more leaves 2 % more places in the GPCs empty.  Pairs: lat + waves of
+// stages, + what a tile's output costs beyond the next tile's stages.  The choice takes 2.6 % (gradients 0.4 %) more time than
+// the fastest of these in the mean, at worst 1.36 times it (2048 x 512 x 512: 7.8, 5.8 us).
+struct ClusterModel { int columns; float lat, stage, shared, fixed; };
+struct ProductModel { float pair_lat, pair_stage, pair_tile, exchange, exchange_share; int per_sm, widths; ClusterModel cluster[4]; };
+constexpr ProductModel MODEL_INT8 = {6.46f, 0.288f, 2.08f, 2.27f, 0.0f, 2, 4,
+    {{16, 1.15f, 0.111f, 0.172f, 1.82f}, {32, 1.65f, 0.208f, 0.190f, 1.84f}, {64, 2.15f, 0.227f, 0.207f, 2.58f}, {128, 3.36f, 0.279f, 0.257f, 3.88f}}};
+constexpr ProductModel MODEL_GRAD = {8.49f, 0.321f, 0.72f, 0.91f, 0.275f, 1, 2, {{64, 2.10f, 0.210f, 0.100f, 3.67f}, {128, 1.61f, 0.263f, 0.232f, 5.02f}}};
+
+struct ProductChoice { int columns, shares; };               // columns 256: pairs
+ProductChoice choose_product(const ProductModel& m, const ProductParams& p, double bytes, int sms)
+{
+    const float by_memory = (float)(bytes / 6.2e6);
+    const int64_t pair_tiles = ceil_div(p.rows, 256) * ceil_div(p.cols, 256), waves = ceil_div(pair_tiles, std::max(1, sms / 2));
+    float best = std::max(m.pair_lat + (float)waves * p.kstages * m.pair_stage + (float)(waves - 1) * m.pair_tile, m.pair_lat + by_memory);
+    ProductChoice choice = {256, 1};
+    for (int w = 0; w < m.widths; ++w) {
+        const ClusterModel& c = m.cluster[w];
+        if (w > 0 && p.cols <= m.cluster[w - 1].columns) break;          // a narrower tile holds every column
+        const int64_t tiles = ceil_div(p.rows, 128) * ceil_div(p.cols, c.columns);
+        for (int shares = 1; shares <= 8 && shares <= p.kstages; ++shares) {
+            const float ctas = (float)(tiles * shares), places = sms * m.per_sm * (1.0f - 0.02f * (shares - 1));
+            float rounds = std::max(1.0f, ctas / places);
+            if (shares > 1) rounds = ceilf(rounds);
+            const float stages = (float)ceil_div(p.kstages, shares);
+            const float body = std::max(stages * c.stage * rounds, ceilf(ctas / sms) * stages * c.shared);
+            const float time = std::max(c.lat + rounds * c.fixed + body + (shares > 1 ? m.exchange + m.exchange_share * shares : 0.0f), 3.0f + by_memory);
+            if (time < best) { best = time; choice = {c.columns, shares}; }
+        }
+    }
+    return choice;
+}
 
 template <int KIND>
 fmm_status_t launch_product(const ProductParams& p, const Operand& r, const Operand& s, cudaStream_t st)
 {
-    const int sms = fmm_sm_count();
-    const int64_t pairs = ceil_div(p.rows, 256) * ceil_div(p.cols, 256);
-    if (pairs >= sms / 4) return launch_pair<KIND>(p, r, s, st);
-    int tc = 128;
-    if (KIND == INT8) { if (p.cols <= 16) tc = 16; else if (p.cols <= 32) tc = 32; }
-    if (tc == 128 && (p.cols <= 64 || ceil_div(p.rows, 128) * ceil_div(p.cols, 128) < sms)) tc = 64;
-    const int64_t tiles = ceil_div(p.rows, 128) * ceil_div(p.cols, tc);
-    int shares = 1;
-    while (shares < 8 && tiles * shares * 2 <= 2 * sms && p.kstages >= 4 * shares) shares *= 2;
+    const int e = KIND == INT8 ? 1 : 2;
+    const double bytes = (double)e * ((double)r.rows * r.cols + (double)s.rows * s.cols) + (double)p.rows * p.cols * int8_type_bytes((fmm_type_t)p.out_type);
+    const ProductChoice c = choose_product(KIND == INT8 ? MODEL_INT8 : MODEL_GRAD, p, bytes, fmm_sm_count());
     if constexpr (KIND == INT8) {
-        if (tc == 16) return launch_cluster<KIND, 16>(p, r, s, shares, st);
-        if (tc == 32) return launch_cluster<KIND, 32>(p, r, s, shares, st);
+        if (c.columns == 16) return launch_cluster<KIND, 16>(p, r, s, c.shares, st);
+        if (c.columns == 32) return launch_cluster<KIND, 32>(p, r, s, c.shares, st);
     }
-    return tc == 64 ? launch_cluster<KIND, 64>(p, r, s, shares, st) : launch_cluster<KIND, 128>(p, r, s, shares, st);
+    if (c.columns == 64) return launch_cluster<KIND, 64>(p, r, s, c.shares, st);
+    if (c.columns == 128) return launch_cluster<KIND, 128>(p, r, s, c.shares, st);
+    return launch_pair<KIND>(p, r, s, st);
 }
 
 fmm_status_t launch_empty(const ProductParams& p, cudaStream_t st)
@@ -726,6 +768,7 @@ fmm_status_t grad(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* co
         if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;
         dy = {copy, M, N, w.ld_dy};
     }
+    p.behind = 1;
     const uint32_t format = type == FMM_TYPE_BF16 ? 1u : 0u;
     p.kstages = (int)ceil_div(contraction, 64);
     p.chunk = out_type == FMM_TYPE_F32 ? CHUNK : p.kstages;

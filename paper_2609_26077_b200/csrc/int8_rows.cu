@@ -483,6 +483,7 @@ template <typename T, bool AL>
 __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
 {
     constexpr int VPT = FLAT_VPT;
+    fmmptx::griddep_launch_dependents();                      // (the product of a gradient, which waits for this grid to end)
     const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, shift = p.block == 32 ? 5 : 7, step = 8 * blockDim.x;
     for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < p.rows; row += (int64_t)gridDim.x * blockDim.y) {
         const int8_t* codes = p.codes + row * p.ldc;
