@@ -76,13 +76,32 @@ def lib():
 
 # ------------------------------------------------------------------------------------------------ checks
 # (The calls of one token are bound by what Python does for them: a microsecond each for a context manager, an allocation, a few
-# checks.  So the checks read every attribute once and the usual device and stream take no context.)
-def _matrix(t, name, dtype, shape=None):
-    """A 2-D CUDA tensor with contiguous columns; its row distance."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name}: a CUDA tensor is needed")
+# checks.  So the checks read every attribute once, devices are compared by number, and the usual device and stream take no context.)
+def _device(t):
+    """Number of the CUDA device that a call's first tensor is on."""
+    try:
+        device = t.get_device()
+    except AttributeError:
+        raise TypeError("a CUDA tensor is needed") from None
+    if device < 0:
+        raise TypeError("a CUDA tensor is needed")
+    return device
+
+
+def _suits(t, name, dtype, device):
+    try:
+        where = t.get_device()
+    except AttributeError:
+        raise TypeError(f"{name}: a CUDA tensor is needed") from None
+    if where != device:
+        raise TypeError(f"{name}: on {t.device} in a call on cuda:{device}")
     if t.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} is needed, not {t.dtype}")
+
+
+def _matrix(t, name, dtype, device, shape=None):
+    """A 2-D tensor with contiguous columns; its row distance."""
+    _suits(t, name, dtype, device)
     size = t.shape
     if len(size) != 2 or (shape is not None and size != shape):
         raise ValueError(f"{name}: shape {tuple(size)}, {'two dimensions are' if shape is None else f'{tuple(shape)} is'} needed")
@@ -97,11 +116,8 @@ def _matrix(t, name, dtype, shape=None):
     return ld
 
 
-def _vector(t, name, dtype, shape):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name}: a CUDA tensor is needed")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name}: {dtype} is needed, not {t.dtype}")
+def _vector(t, name, dtype, device, shape):
+    _suits(t, name, dtype, device)
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous tensor of shape {shape} is needed, not {tuple(t.shape)}")
 
@@ -123,32 +139,23 @@ def _scale_shape(rows, cols, block):
     return (rows, -(-cols // block)) if block else (rows,)
 
 
-def _same_device(first, *tensors):
-    device = first.device
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise TypeError(f"tensors on {device} and {t.device} in one call")
-
-
-def _elsewhere(t, stream):
+def _elsewhere(device, stream):
     """None where a call can run on the current device and stream, else the context in which it can."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("a CUDA tensor is needed")
     if stream is not None:
-        if stream.device != t.device:
-            raise TypeError(f"a stream of {stream.device} for tensors on {t.device}")
+        if stream.device.index != device:
+            raise TypeError(f"a stream of {stream.device} for tensors on cuda:{device}")
         return torch.cuda.stream(stream)
-    return None if t.device.index == torch._C._cuda_getDevice() else torch.cuda.device(t.device)
+    return None if device == _current_device() else torch.cuda.device(device)
 
 
-_empty = torch.empty
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
-def _new_codes(rows, cols, device):
-    """Codes whose rows are a multiple of 16 bytes apart."""
+def _new_codes(rows, cols, like):
+    """Codes whose rows are a multiple of 16 bytes apart, on like's device."""
     if cols % 16 == 0:
-        return _empty((rows, cols), dtype=torch.int8, device=device)
-    return _empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
+        return like.new_empty((rows, cols), dtype=torch.int8)
+    return like.new_empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8)[:, :cols]
 
 
 def _call(status, what):
@@ -161,7 +168,7 @@ _needs = {}
 
 def _need(name, *sizes):
     """Workspace bytes by the library's function of that name (remembered by sizes and device)."""
-    key = (name, torch._C._cuda_getDevice(), sizes)
+    key = (name, _current_device(), sizes)
     need = _needs.get(key)
     if need is None:
         b = C.c_size_t()
@@ -176,22 +183,22 @@ def _need(name, *sizes):
 def quantize(x, block=0, pow2=False, out=None, stream=None):
     """Codes and scales of x (rows x cols): one scale per row, or per block of 32 or 128 columns of a row; with pow2 each is
     a power of two.  out: (codes, scales) to write to."""
-    where = _elsewhere(x, stream)
+    device = _device(x)
+    where = _elsewhere(device, stream)
     if where is not None:
         with where:
             return quantize(x, block, pow2, out)
     kind = _float_type(x.dtype, "x")
-    ldx = _matrix(x, "x", x.dtype)
+    ldx = _matrix(x, "x", x.dtype, device)
     rows, cols = x.shape
     shape = _scale_shape(rows, cols, _block(block))
     if out is None:
-        codes, scales = _new_codes(rows, cols, x.device), _empty(shape, dtype=torch.float32, device=x.device)
+        codes, scales = _new_codes(rows, cols, x), x.new_empty(shape, dtype=torch.float32)
         ldc = codes.stride(0) or 1
     else:
         codes, scales = out
-        ldc = _matrix(codes, "codes", torch.int8, (rows, cols))
-        _vector(scales, "scales", torch.float32, shape)
-        _same_device(x, codes, scales)
+        ldc = _matrix(codes, "codes", torch.int8, device, (rows, cols))
+        _vector(scales, "scales", torch.float32, device, shape)
     _call((_lib or lib()).fmm_int8_quantize(x.data_ptr(), kind, ldx, rows, cols, block, POW2 if pow2 else AMAX_DIV_127, codes.data_ptr(), ldc,
                                             scales.data_ptr(), fmm._stream_ptr(None)), "fmm_int8_quantize")
     return codes, scales
@@ -199,19 +206,19 @@ def quantize(x, block=0, pow2=False, out=None, stream=None):
 
 def dequantize(codes, scales, block=0, dtype=torch.bfloat16, out=None, stream=None):
     """The values that codes stand for, code * scale, in `dtype` (or out's type)."""
-    where = _elsewhere(codes, stream)
+    device = _device(codes)
+    where = _elsewhere(device, stream)
     if where is not None:
         with where:
             return dequantize(codes, scales, block, dtype, out)
-    ldc = _matrix(codes, "codes", torch.int8)
+    ldc = _matrix(codes, "codes", torch.int8, device)
     rows, cols = codes.shape
-    _vector(scales, "scales", torch.float32, _scale_shape(rows, cols, _block(block)))
+    _vector(scales, "scales", torch.float32, device, _scale_shape(rows, cols, _block(block)))
     if out is None:
-        kind, out, ldx = _float_type(dtype, "dtype"), _empty((rows, cols), dtype=dtype, device=codes.device), cols
+        kind, out, ldx = _float_type(dtype, "dtype"), codes.new_empty((rows, cols), dtype=dtype), cols
     else:
         kind = _float_type(out.dtype, "out")
-        ldx = _matrix(out, "out", out.dtype, (rows, cols))
-    _same_device(codes, scales, out)
+        ldx = _matrix(out, "out", out.dtype, device, (rows, cols))
     _call((_lib or lib()).fmm_int8_dequantize(codes.data_ptr(), ldc, scales.data_ptr(), rows, cols, block, out.data_ptr(), kind, ldx,
                                               fmm._stream_ptr(None)), "fmm_int8_dequantize")
     return out
@@ -229,33 +236,33 @@ def rms_norm(x, gain, residual=None, eps=1e-6, pow2=False, checkpoint=0, hidden=
         rstd                           1 / rms(h) per row
         checkpoint, checkpoint_scales  8-bit form of h in blocks of `checkpoint` (32 or 128) columns; None with 0
     """
-    where = _elsewhere(x, stream)
+    device = _device(x)
+    where = _elsewhere(device, stream)
     if where is not None:
         with where:
             return rms_norm(x, gain, residual, eps, pow2, checkpoint, hidden)
-    dtype, device = x.dtype, x.device
+    dtype = x.dtype
     kind = _float_type(dtype, "x")
-    ldx = _matrix(x, "x", dtype)
+    ldx = _matrix(x, "x", dtype, device)
     rows, cols = x.shape
-    _vector(gain, "gain", dtype, (cols,))
+    _vector(gain, "gain", dtype, device, (cols,))
     ldr = ldh = ldk = 0
     at_residual = at_hidden = at_kept = at_kept_scales = None
     if residual is not None:
-        ldr = _matrix(residual, "residual", dtype, (rows, cols))
+        ldr = _matrix(residual, "residual", dtype, device, (rows, cols))
         if hidden is None:
-            hidden, ldh = _empty((rows, cols), dtype=dtype, device=device), cols
+            hidden, ldh = x.new_empty((rows, cols)), cols
         else:
-            ldh = _matrix(hidden, "hidden", dtype, (rows, cols))
+            ldh = _matrix(hidden, "hidden", dtype, device, (rows, cols))
         at_residual, at_hidden = residual.data_ptr(), hidden.data_ptr()
     elif hidden is not None:
         raise ValueError("hidden: written with a residual only")
-    _same_device(x, gain, residual, hidden)
-    codes = _new_codes(rows, cols, device)
-    scales, rstd = _empty((2, rows), dtype=torch.float32, device=device).unbind()
+    codes = _new_codes(rows, cols, x)
+    scales, rstd = x.new_empty((rows,), dtype=torch.float32), x.new_empty((rows,), dtype=torch.float32)
     kept = kept_scales = None
     if checkpoint:
-        kept = _new_codes(rows, cols, device)
-        kept_scales = _empty(_scale_shape(rows, cols, _block(checkpoint, "checkpoint")), dtype=torch.float32, device=device)
+        kept = _new_codes(rows, cols, x)
+        kept_scales = x.new_empty(_scale_shape(rows, cols, _block(checkpoint, "checkpoint")), dtype=torch.float32)
         at_kept, ldk, at_kept_scales = kept.data_ptr(), kept.stride(0), kept_scales.data_ptr()
     a = RmsNormArgs(kind, POW2 if pow2 else AMAX_DIV_127, checkpoint, rows, cols, eps, x.data_ptr(), ldx, at_residual, ldr, gain.data_ptr(),
                     at_hidden, ldh, codes.data_ptr(), codes.stride(0), scales.data_ptr(), rstd.data_ptr(), at_kept, ldk, at_kept_scales)
@@ -266,29 +273,29 @@ def rms_norm(x, gain, residual=None, eps=1e-6, pow2=False, checkpoint=0, hidden=
 def rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block=128, dresidual=None, dx=None, stream=None):
     """(dx, dgain) of the norm, from the checkpoint of its hidden rows and their rstd.  dx, the gradient of x and of residual,
     includes dresidual, the gradient that reaches the hidden rows elsewhere; it may be dy or dresidual.  dgain is float32."""
-    where = _elsewhere(dy, stream)
+    device = _device(dy)
+    where = _elsewhere(device, stream)
     if where is not None:
         with where:
             return rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block, dresidual, dx)
-    dtype, device = dy.dtype, dy.device
+    dtype = dy.dtype
     kind = _float_type(dtype, "dy")
-    ldy = _matrix(dy, "dy", dtype)
+    ldy = _matrix(dy, "dy", dtype, device)
     rows, cols = dy.shape
-    ldk = _matrix(checkpoint, "checkpoint", torch.int8, (rows, cols))
-    _vector(checkpoint_scales, "checkpoint_scales", torch.float32, _scale_shape(rows, cols, _block(block)))
-    _vector(rstd, "rstd", torch.float32, (rows,))
-    _vector(gain, "gain", dtype, (cols,))
+    ldk = _matrix(checkpoint, "checkpoint", torch.int8, device, (rows, cols))
+    _vector(checkpoint_scales, "checkpoint_scales", torch.float32, device, _scale_shape(rows, cols, _block(block)))
+    _vector(rstd, "rstd", torch.float32, device, (rows,))
+    _vector(gain, "gain", dtype, device, (cols,))
     ldr, at_dresidual = 0, None
     if dresidual is not None:
-        ldr, at_dresidual = _matrix(dresidual, "dresidual", dtype, (rows, cols)), dresidual.data_ptr()
+        ldr, at_dresidual = _matrix(dresidual, "dresidual", dtype, device, (rows, cols)), dresidual.data_ptr()
     if dx is None:
-        dx, ldx = _empty((rows, cols), dtype=dtype, device=device), cols
+        dx, ldx = dy.new_empty((rows, cols)), cols
     else:
-        ldx = _matrix(dx, "dx", dtype, (rows, cols))
-    _same_device(dy, checkpoint, checkpoint_scales, rstd, gain, dresidual, dx)
-    dgain = _empty((cols,), dtype=torch.float32, device=device)
+        ldx = _matrix(dx, "dx", dtype, device, (rows, cols))
+    dgain = dy.new_empty((cols,), dtype=torch.float32)
     need = _need("fmm_int8_rms_norm_backward_workspace_bytes", rows, cols)
-    workspace = _empty((need,), dtype=torch.uint8, device=device)
+    workspace = dy.new_empty((need,), dtype=torch.uint8)
     a = RmsNormBackwardArgs(kind, block, rows, cols, dy.data_ptr(), ldy, checkpoint.data_ptr(), ldk, checkpoint_scales.data_ptr(), rstd.data_ptr(),
                             gain.data_ptr(), at_dresidual, ldr, dx.data_ptr(), ldx, dgain.data_ptr())
     _call((_lib or lib()).fmm_int8_rms_norm_backward(C.byref(a), workspace.data_ptr(), need, fmm._stream_ptr(None)), "fmm_int8_rms_norm_backward")
@@ -298,13 +305,14 @@ def rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block=128, 
 def matmul(a, a_scales, b, b_scales, bias=None, dtype=torch.bfloat16, out=None, stream=None):
     """a (M x K codes, a scale per row) times the transpose of b (N x K codes, a scale per row), plus bias (N): M x N in
     `dtype` (or out's type).  The rows of a and b start on 16-byte boundaries; K is at most 131071."""
-    where = _elsewhere(a, stream)
+    device = _device(a)
+    where = _elsewhere(device, stream)
     if where is not None:
         with where:
             return matmul(a, a_scales, b, b_scales, bias, dtype, out)
-    lda = _matrix(a, "a", torch.int8)
+    lda = _matrix(a, "a", torch.int8, device)
     M, K = a.shape
-    ldb = _matrix(b, "b", torch.int8)
+    ldb = _matrix(b, "b", torch.int8, device)
     N = b.shape[0]
     if b.shape[1] != K:
         raise ValueError(f"a and b have {K} and {b.shape[1]} columns")
@@ -316,47 +324,45 @@ def matmul(a, a_scales, b, b_scales, bias=None, dtype=torch.bfloat16, out=None, 
     at_a, at_b = a.data_ptr(), b.data_ptr()
     if (lda | ldb | at_a | at_b) & 15 and M and N and K:
         raise ValueError("a and b: rows have to start on 16-byte boundaries (as those of quantize and rms_norm do)")
-    _vector(a_scales, "a_scales", torch.float32, (M,))
-    _vector(b_scales, "b_scales", torch.float32, (N,))
+    _vector(a_scales, "a_scales", torch.float32, device, (M,))
+    _vector(b_scales, "b_scales", torch.float32, device, (N,))
     if out is None:
-        kind, out, ldc = _float_type(dtype, "dtype"), _empty((M, N), dtype=dtype, device=a.device), N
+        kind, out, ldc = _float_type(dtype, "dtype"), a.new_empty((M, N), dtype=dtype), N
     else:
         dtype = out.dtype
         kind = _float_type(dtype, "out")
-        ldc = _matrix(out, "out", dtype, (M, N))
+        ldc = _matrix(out, "out", dtype, device, (M, N))
     if bias is not None:
-        _vector(bias, "bias", dtype, (N,))
-    _same_device(a, a_scales, b, b_scales, bias, out)
+        _vector(bias, "bias", dtype, device, (N,))
     _call((_lib or lib()).fmm_int8_matmul(at_a, lda, a_scales.data_ptr(), at_b, ldb, b_scales.data_ptr(), None if bias is None else bias.data_ptr(),
                                           M, N, K, out.data_ptr(), kind, ldc, fmm._stream_ptr(None)), "fmm_int8_matmul")
     return out
 
 
-def _grad(what, dy, codes, scales, shape, dtype, out, accumulate):
+def _grad(what, device, dy, codes, scales, shape, dtype, out, accumulate):
     kind = dy.dtype
     if kind is not torch.bfloat16 and kind is not torch.float16:
         raise TypeError(f"dy: bfloat16 or float16 is needed, not {kind}")
-    ldy = _matrix(dy, "dy", kind)
-    ldc = _matrix(codes, "codes", torch.int8)
+    ldy = _matrix(dy, "dy", kind, device)
+    ldc = _matrix(codes, "codes", torch.int8, device)
     M, N = dy.shape
     code_rows, K = codes.shape
-    _vector(scales, "scales", torch.float32, (code_rows,))
+    _vector(scales, "scales", torch.float32, device, (code_rows,))
     if out is None:
         if accumulate:
             raise ValueError("accumulate: needs out")
         dtype = kind if dtype is None else dtype
         if dtype is not torch.float32 and dtype is not kind:
             raise TypeError(f"the gradient is float32 or of dy's type, not {dtype}")
-        out, ldo = _empty(shape, dtype=dtype, device=dy.device), shape[1]
+        out, ldo = dy.new_empty(shape, dtype=dtype), shape[1]
     else:
         dtype = out.dtype
         if dtype is not torch.float32 and dtype is not kind:
             raise TypeError(f"the gradient is float32 or of dy's type, not {dtype}")
-        ldo = _matrix(out, "out", dtype, shape)
-    _same_device(dy, codes, scales, out)
+        ldo = _matrix(out, "out", dtype, device, shape)
     at = dy.data_ptr()
     need = _need("fmm_int8_grad_workspace_bytes", code_rows, K, M, N, int(not (at & 15 or ldy & 7)))
-    workspace = _empty((need,), dtype=torch.uint8, device=dy.device)
+    workspace = dy.new_empty((need,), dtype=torch.uint8)
     head = (at, _TYPES[kind], ldy, codes.data_ptr(), ldc, scales.data_ptr(), M, N, K, out.data_ptr(), _TYPES[dtype], ldo)
     tail = (workspace.data_ptr(), need, fmm._stream_ptr(None))
     if what == "fmm_int8_grad_weight":
@@ -369,25 +375,27 @@ def _grad(what, dy, codes, scales, shape, dtype, out, accumulate):
 def grad_weight(dy, codes, scales, dtype=torch.float32, out=None, accumulate=False, stream=None):
     """Gradient of matmul's b: dy^T (M x N, 16-bit) times the activations that codes (M x K) and scales stand for: N x K in
     `dtype` (float32 or dy's type).  With accumulate it is added to out."""
-    where = _elsewhere(dy, stream)
+    device = _device(dy)
+    where = _elsewhere(device, stream)
     if where is not None:
         with where:
             return grad_weight(dy, codes, scales, dtype, out, accumulate)
     if dy.dim() != 2 or codes.dim() != 2 or codes.shape[0] != dy.shape[0]:
         raise ValueError(f"dy and codes: two dimensions and as many rows are needed, not {tuple(dy.shape)} and {tuple(codes.shape)}")
-    return _grad("fmm_int8_grad_weight", dy, codes, scales, (dy.shape[1], codes.shape[1]), dtype, out, accumulate)
+    return _grad("fmm_int8_grad_weight", device, dy, codes, scales, (dy.shape[1], codes.shape[1]), dtype, out, accumulate)
 
 
 def grad_input(dy, codes, scales, dtype=None, out=None, stream=None):
     """Gradient of matmul's a: dy (M x N, 16-bit) times the weight that codes (N x K) and scales stand for: M x K in `dtype`
     (float32 or dy's type, the default)."""
-    where = _elsewhere(dy, stream)
+    device = _device(dy)
+    where = _elsewhere(device, stream)
     if where is not None:
         with where:
             return grad_input(dy, codes, scales, dtype, out)
     if dy.dim() != 2 or codes.dim() != 2 or codes.shape[0] != dy.shape[1]:
         raise ValueError(f"dy and codes: two dimensions and dy's columns as codes' rows are needed, not {tuple(dy.shape)} and {tuple(codes.shape)}")
-    return _grad("fmm_int8_grad_input", dy, codes, scales, (dy.shape[0], codes.shape[1]), dtype, out, False)
+    return _grad("fmm_int8_grad_input", device, dy, codes, scales, (dy.shape[0], codes.shape[1]), dtype, out, False)
 
 
 def status():
