@@ -125,6 +125,9 @@ fmm_status_t fmm_int8_grad_input(const void* dY, fmm_type_t type, int64_t ldy, c
  * Debug build (fmm_debug_build): also the first store outside the ranges that a launch was given. */
 fmm_status_t fmm_int8_status(int* code);
 fmm_status_t fmm_int8_status_clear(void);
+/* Self-test of that status: enqueues a one-warp kernel that waits, with the products' bounded-wait routine, on a barrier that nothing
+ * signals; after limit_ns (1 .. 2e9) it gives up and records location 901.  Look up the status once before capturing this. */
+fmm_status_t fmm_int8_selftest_bounded_wait(int64_t limit_ns, void* cuda_stream);
 
 #ifdef __cplusplus
 }

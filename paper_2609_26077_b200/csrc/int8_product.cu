@@ -34,8 +34,8 @@ namespace {
 
 enum Kind { INT8 = 0, GRAD_W = 1, GRAD_X = 2 };
 
-// [0] first bounded wait that gave up, [1] store outside its range (FMM_DEBUG build)
-__device__ int g_int8_product_status[2];
+// [0] first bounded wait that gave up, [1] set by the self-test if its wait did not, [2] store outside its range (FMM_DEBUG build)
+__device__ int g_int8_product_status[3];
 
 __device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t cta)
 { uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(cta)); return r; }
@@ -120,7 +120,7 @@ __device__ __forceinline__ float scaled(uint32_t acc, float a, float b)
 template <typename T> __device__ __forceinline__ void put_one(const ProductParams& p, long long at, float v)
 {
     T* q = static_cast<T*>(p.out) + at;
-    if (!INT8_STORE_OK(p.ranges, q, sizeof(T), 2201, &g_int8_product_status[1])) return;
+    if (!INT8_STORE_OK(p.ranges, q, sizeof(T), 2201, &g_int8_product_status[2])) return;
     if (p.accumulate) v += to_float(*q);
     *q = from_float<T>(v);
 }
@@ -826,26 +826,34 @@ fmm_status_t fmm_int8_status(int* code)
 {
     if (!code) return FMM_ERR_INVALID_ARG;
     *code = 0;
-    int words[2] = {0, 0}, rows = 0;
+    int words[3] = {0, 0, 0}, rows = 0;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(words, g_int8_product_status, sizeof(words)) != cudaSuccess) {
         cudaGetLastError();
         return FMM_ERR_CUDA;
     }
     const fmm_status_t s = int8_rows_guard_read(&rows, false);
     if (s != FMM_OK) return s;
-    *code = words[0] ? words[0] : words[1] ? words[1] : rows;
+    *code = words[0] ? words[0] : words[2] ? words[2] : rows;
     return words[0] ? FMM_ERR_DEVICE_TIMEOUT : FMM_OK;
 }
 
 fmm_status_t fmm_int8_status_clear(void)
 {
-    const int zero[2] = {0, 0};
+    const int zero[3] = {0, 0, 0};
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyToSymbol(g_int8_product_status, zero, sizeof(zero)) != cudaSuccess) {
         cudaGetLastError();
         return FMM_ERR_CUDA;
     }
     int unused = 0;
     return int8_rows_guard_read(&unused, true);
+}
+
+fmm_status_t fmm_int8_selftest_bounded_wait(int64_t limit_ns, void* stream)
+{
+    if (limit_ns < 1 || limit_ns > 2000000000) return FMM_ERR_INVALID_ARG;
+    int* status = nullptr;
+    if (cudaGetSymbolAddress((void**)&status, g_int8_product_status) != cudaSuccess) { cudaGetLastError(); return FMM_ERR_CUDA; }
+    return fmm_launch_bounded_wait_selftest(status, (unsigned long long)limit_ns, reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -32,7 +32,7 @@ _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 EXPORTS = ["fmm_int8_quantize", "fmm_int8_dequantize", "fmm_int8_rms_norm", "fmm_int8_rms_norm_backward_workspace_bytes",
            "fmm_int8_rms_norm_backward", "fmm_int8_matmul", "fmm_int8_grad_workspace_bytes", "fmm_int8_grad_weight",
-           "fmm_int8_grad_input", "fmm_int8_status", "fmm_int8_status_clear"]
+           "fmm_int8_grad_input", "fmm_int8_status", "fmm_int8_status_clear", "fmm_int8_selftest_bounded_wait"]
 
 
 class RmsNormArgs(C.Structure):
@@ -70,6 +70,7 @@ def lib():
         L.fmm_int8_grad_weight.argtypes = [ptr, i32, i64, ptr, i64, ptr, i64, i64, i64, ptr, i32, i64, i32, ptr, size, ptr]
         L.fmm_int8_grad_input.argtypes = [ptr, i32, i64, ptr, i64, ptr, i64, i64, i64, ptr, i32, i64, ptr, size, ptr]
         L.fmm_int8_status.argtypes = [ptr]
+        L.fmm_int8_selftest_bounded_wait.argtypes = [i64, ptr]
         _lib = L
     return _lib
 
@@ -406,3 +407,7 @@ def status():
 
 def status_clear():
     _call(lib().fmm_int8_status_clear(), "fmm_int8_status_clear")
+
+
+def selftest_bounded_wait(limit_ns, stream=None):
+    _call(lib().fmm_int8_selftest_bounded_wait(int(limit_ns), fmm._stream_ptr(stream)), "fmm_int8_selftest_bounded_wait")
