@@ -35,15 +35,29 @@ extern "C" {
 typedef enum { FMM_INT8_SCALE_AMAX_DIV_127 = 0, FMM_INT8_SCALE_POW2 = 1 } fmm_int8_scale_t;
 typedef enum { FMM_TYPE_F32 = 0, FMM_TYPE_BF16 = 1, FMM_TYPE_F16 = 2 } fmm_type_t;
 
-/* 8-bit form of X (dev, rows x cols of `type`): codes (dev, rows x cols) and scales (dev, rows if block == 0, else
+/* 8-bit form of x (dev, rows x cols of `type`): codes (dev, rows x cols) and scales (dev, rows if block == 0, else
  * rows x ceil(cols / block), dense). */
-fmm_status_t fmm_int8_quantize(const void* X, fmm_type_t type, int64_t ldx, int64_t rows, int64_t cols, int block,
-                               fmm_int8_scale_t scale_mode, int8_t* codes, int64_t ldc, float* scales, void* cuda_stream);
+typedef struct {
+    fmm_type_t type;
+    int block;
+    fmm_int8_scale_t scale_mode;
+    int64_t rows, cols;
+    const void* x;        int64_t ldx;
+    int8_t* codes;        int64_t ldc;
+    float* scales;
+} fmm_int8_quantize_t;
+fmm_status_t fmm_int8_quantize(const fmm_int8_quantize_t* p, void* cuda_stream);
 
-/* X = code * scale, taken in fp32 and rounded once to `type` (dev, rows x cols).  Rows of codes may lie in any order
- * that `ldc` gives. */
-fmm_status_t fmm_int8_dequantize(const int8_t* codes, int64_t ldc, const float* scales, int64_t rows, int64_t cols,
-                                 int block, void* X, fmm_type_t type, int64_t ldx, void* cuda_stream);
+/* x = code * scale, taken in fp32 and rounded once to `type` (dev, rows x cols); codes and scales as above. */
+typedef struct {
+    fmm_type_t type;
+    int block;
+    int64_t rows, cols;
+    const int8_t* codes;  int64_t ldc;
+    const float* scales;
+    void* x;              int64_t ldx;
+} fmm_int8_dequantize_t;
+fmm_status_t fmm_int8_dequantize(const fmm_int8_dequantize_t* p, void* cuda_stream);
 
 /* Residual's addition, root-mean-square norm and 8-bit output, row by row:
  *     h = fl(x + residual)  (x itself where residual is NULL);  rstd = fl32(1 / sqrt(sum h^2 / cols + eps)), in fp64;
@@ -95,30 +109,44 @@ fmm_status_t fmm_int8_rms_norm_backward(const fmm_int8_rms_norm_backward_t* p, v
 
 /* C = (A B^T) scaled by row and column, plus a bias: C[i][j] = acc * a_scales[i] * b_scales[j] + bias[j], the sum acc of
  * the products of codes being exact, the rest in fp32, rounded once to `type`.
- *   A dev, M x K codes (tokens); B dev, N x K codes (a weight, one row per output channel); C dev, M x N; bias dev, N of
- *   `type`, or NULL.  A and B 16-byte aligned, lda and ldb multiples of 16 (FMM_ERR_INVALID_ARG; the codes that
+ *   a dev, M x K codes (tokens); b dev, N x K codes (a weight, one row per output channel); c dev, M x N; bias dev, N of
+ *   `type`, or NULL.  a and b 16-byte aligned, lda and ldb multiples of 16 (FMM_ERR_INVALID_ARG; the codes that
  *   fmm_int8_quantize and fmm_int8_rms_norm write may have any such ld); K <= 131071, so that no sum leaves 32 bits, and
  *   M, N < 2^31 - 512 (FMM_ERR_SHAPE). */
-fmm_status_t fmm_int8_matmul(const int8_t* A, int64_t lda, const float* a_scales, const int8_t* B, int64_t ldb,
-                             const float* b_scales, const void* bias, int64_t M, int64_t N, int64_t K, void* C,
-                             fmm_type_t type, int64_t ldc, void* cuda_stream);
+typedef struct {
+    fmm_type_t type;
+    int64_t M, N, K;
+    const int8_t* a;      int64_t lda;
+    const float* a_scales;
+    const int8_t* b;      int64_t ldb;
+    const float* b_scales;
+    const void* bias;
+    void* c;              int64_t ldc;
+} fmm_int8_matmul_t;
+fmm_status_t fmm_int8_matmul(const fmm_int8_matmul_t* p, void* cuda_stream);
 
-/* Gradients of that product for dY (dev, M x N of `type`, FMM_TYPE_BF16 or FMM_TYPE_F16), from what is held in 8 bits.
- * The 8-bit values code * scale are restored in dY's type (exactly, for bf16 and power-of-two scales; otherwise rounded
+/* Gradients of that product for dy (dev, M x N of `type`, FMM_TYPE_BF16 or FMM_TYPE_F16), from what is held in 8 bits.
+ * The 8-bit values code * scale are restored in dy's type (exactly, for bf16 and power-of-two scales; otherwise rounded
  * once), products are summed in fp32.
- *     fmm_int8_grad_weight: dW[j][k] (+)= sum_i dY[i][j] * (X[i][k] * x_scales[i])
- *         X dev, M x K codes; dW dev, N x K of out_type: FMM_TYPE_F32 or dY's type.  accumulate != 0 adds to dW.
- *     fmm_int8_grad_input:  dX[i][k] = sum_j dY[i][j] * (W[j][k] * w_scales[j])
- *         W dev, N x K codes; dX dev, M x K of out_type: FMM_TYPE_F32 or dY's type.
+ *     fmm_int8_grad_weight: out[j][k] (+)= sum_i dy[i][j] * (codes[i][k] * scales[i])      codes M x K, out N x K
+ *     fmm_int8_grad_input:  out[i][k] (+)= sum_j dy[i][j] * (codes[j][k] * scales[j])      codes N x K, out M x K
+ *   out: dev, of out_type, FMM_TYPE_F32 or dy's type; accumulate != 0 adds to what it holds.
  *   M, N, K < 2^31 - 512 (FMM_ERR_SHAPE).  The workspace holds the restored operand and, where its rows are not 16-byte
- *   aligned, a copy of dY; its size depends on dY's alignment (dy_aligned: dY and ldy * 2 are multiples of 16). */
-fmm_status_t fmm_int8_grad_workspace_bytes(int64_t code_rows, int64_t K, int64_t M, int64_t N, int dy_aligned, size_t* bytes);
-fmm_status_t fmm_int8_grad_weight(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* X, int64_t ldx,
-                                  const float* x_scales, int64_t M, int64_t N, int64_t K, void* dW, fmm_type_t out_type,
-                                  int64_t ldw, int accumulate, void* workspace, size_t workspace_bytes, void* cuda_stream);
-fmm_status_t fmm_int8_grad_input(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* W, int64_t ldw,
-                                 const float* w_scales, int64_t M, int64_t N, int64_t K, void* dX, fmm_type_t out_type,
-                                 int64_t ldx, void* workspace, size_t workspace_bytes, void* cuda_stream);
+ *   aligned, a copy of dy; its size is asked for with the same arguments (of which the matrices' own addresses but dy's
+ *   do not matter). */
+typedef struct {
+    fmm_type_t type, out_type;
+    int accumulate;
+    int64_t M, N, K;
+    const void* dy;       int64_t ldy;
+    const int8_t* codes;  int64_t ldc;
+    const float* scales;
+    void* out;            int64_t ldo;
+} fmm_int8_grad_t;
+fmm_status_t fmm_int8_grad_weight_workspace_bytes(const fmm_int8_grad_t* p, size_t* bytes);
+fmm_status_t fmm_int8_grad_input_workspace_bytes(const fmm_int8_grad_t* p, size_t* bytes);
+fmm_status_t fmm_int8_grad_weight(const fmm_int8_grad_t* p, void* workspace, size_t workspace_bytes, void* cuda_stream);
+fmm_status_t fmm_int8_grad_input(const fmm_int8_grad_t* p, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* Status of the product kernels on the current device, read after cudaDeviceSynchronize: *code == 0, or the location of
  * the first bounded device-side wait that gave up (FMM_ERR_DEVICE_TIMEOUT; the results of that call are invalid).

@@ -646,7 +646,7 @@ fmm_status_t launch_pair(ProductParams p, const Operand& r, const Operand& s, cu
         !raise_smem(int8_pair_kernel<KIND>, C::SMEM_BYTES, done)) return FMM_ERR_CUDA;
     p.tiles_r = (p.rows + 255) / 256; p.tiles_c = (p.cols + 255) / 256; p.k_shares = 1;
     // as few pairs as finish in the same number of waves
-    const int64_t tiles = (int64_t)p.tiles_r * p.tiles_c, most = std::max(1, fmm_sm_count() / 2), waves = (tiles + most - 1) / most;
+    const int64_t tiles = (int64_t)p.tiles_r * p.tiles_c, most = std::max(1, int8_sm_count() / 2), waves = (tiles + most - 1) / most;
     return launch_kernel(int8_pair_kernel<KIND>, (unsigned)((tiles + waves - 1) / waves * 2), C::THREADS, C::SMEM_BYTES, 2, tmR, tmS, p, st);
 }
 
@@ -707,7 +707,7 @@ fmm_status_t launch_product(const ProductParams& p, const Operand& r, const Oper
 {
     const int e = KIND == INT8 ? 1 : 2;
     const double bytes = (double)e * ((double)r.rows * r.cols + (double)s.rows * s.cols) + (double)p.rows * p.cols * int8_type_bytes((fmm_type_t)p.out_type);
-    const ProductChoice c = choose_product(KIND == INT8 ? MODEL_INT8 : MODEL_GRAD, p, bytes, fmm_sm_count());
+    const ProductChoice c = choose_product(KIND == INT8 ? MODEL_INT8 : MODEL_GRAD, p, bytes, int8_sm_count());
     if constexpr (KIND == INT8) {
         if (c.columns == 16) return launch_cluster<KIND, 16>(p, r, s, c.shares, st);
         if (c.columns == 32) return launch_cluster<KIND, 32>(p, r, s, c.shares, st);
@@ -719,7 +719,7 @@ fmm_status_t launch_product(const ProductParams& p, const Operand& r, const Oper
 
 fmm_status_t launch_empty(const ProductParams& p, cudaStream_t st)
 {
-    empty_sum_kernel<<<(unsigned)fmm_sm_count() * 8, 256, 0, st>>>(p);
+    empty_sum_kernel<<<(unsigned)int8_sm_count() * 8, 256, 0, st>>>(p);
     return cudaGetLastError() == cudaSuccess ? FMM_OK : FMM_ERR_CUDA;
 }
 
@@ -737,34 +737,46 @@ GradWorkspace grad_workspace(int64_t code_rows, int64_t K, int64_t M, int64_t N,
     return w;
 }
 
-// Both gradients: `codes` (code_rows x K) restored to `type` in the workspace, dY realigned there if it has to be, one product.
-template <int KIND>
-fmm_status_t grad(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* codes, int64_t ldc, const float* scales, int64_t M, int64_t N, int64_t K,
-                  void* out, fmm_type_t out_type, int64_t ldo, int accumulate, void* workspace, size_t workspace_bytes, void* stream)
+template <int KIND> fmm_status_t grad_workspace_bytes(const fmm_int8_grad_t* a, size_t* bytes)
 {
-    if (type != FMM_TYPE_BF16 && type != FMM_TYPE_F16) return FMM_ERR_INVALID_ARG;
-    if (out_type != FMM_TYPE_F32 && out_type != type) return FMM_ERR_INVALID_ARG;
+    if (!a || !bytes) return FMM_ERR_INVALID_ARG;
+    if (!dim_ok(a->M) || !dim_ok(a->N) || !dim_ok(a->K)) return FMM_ERR_SHAPE;
+    *bytes = grad_workspace(KIND == GRAD_W ? a->M : a->N, a->K, a->M, a->N, int8_aligned(a->dy, a->ldy * 2, 16)).total;
+    return FMM_OK;
+}
+
+// Both gradients: the codes restored to dy's type in the workspace, dy realigned there if it has to be, one product.
+template <int KIND>
+fmm_status_t grad(const fmm_int8_grad_t* a, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!a || (a->type != FMM_TYPE_BF16 && a->type != FMM_TYPE_F16) || (a->out_type != FMM_TYPE_F32 && a->out_type != a->type)) return FMM_ERR_INVALID_ARG;
+    const fmm_type_t type = a->type, out_type = a->out_type;
+    const int64_t M = a->M, N = a->N, K = a->K, ldy = a->ldy, ldc = a->ldc, ldo = a->ldo;
+    const void* dY = a->dy;
+    const int8_t* codes = a->codes;
+    const float* scales = a->scales;
     if (!dim_ok(M) || !dim_ok(N) || !dim_ok(K)) return FMM_ERR_SHAPE;
     const int64_t code_rows = KIND == GRAD_W ? M : N, contraction = code_rows, cols = KIND == GRAD_W ? N : M;
     if (K == 0 || cols == 0) return FMM_OK;
     const int eo = int8_type_bytes(out_type);
-    if (!out || ldo < K || ((uintptr_t)out & (eo - 1))) return FMM_ERR_INVALID_ARG;
+    if (!a->out || ldo < K || ((uintptr_t)a->out & (eo - 1))) return FMM_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     ProductParams p = {};
     p.rows = (int)K; p.cols = (int)cols;
-    p.out = out; p.ldo = ldo; p.out_type = out_type; p.accumulate = accumulate != 0;
-    int8_add_range(p.ranges, out, cols, K, ldo, eo);
-    if (contraction == 0) return accumulate ? FMM_OK : launch_empty(p, st);
+    p.out = a->out; p.ldo = ldo; p.out_type = out_type; p.accumulate = a->accumulate != 0;
+    int8_add_range(p.ranges, a->out, cols, K, ldo, eo);
+    if (contraction == 0) return a->accumulate ? FMM_OK : launch_empty(p, st);
     if (!dY || ldy < N || ((uintptr_t)dY & 1) || !codes || ldc < K || !scales || ((uintptr_t)scales & 3)) return FMM_ERR_INVALID_ARG;
     const bool dy_aligned = int8_aligned(dY, ldy * 2, 16);
     const GradWorkspace w = grad_workspace(code_rows, K, M, N, dy_aligned);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < w.total) return FMM_ERR_WORKSPACE;
-    fmm_status_t s = fmm_int8_dequantize(codes, ldc, scales, code_rows, K, 0, workspace, type, w.ld_codes, stream);
+    const fmm_int8_dequantize_t restore = {type, 0, code_rows, K, codes, ldc, scales, workspace, w.ld_codes};
+    fmm_status_t s = fmm_int8_dequantize(&restore, stream);
     if (s != FMM_OK) return s;
     Operand dy = {dY, M, N, ldy};
     if (!dy_aligned) {
         uint16_t* copy = reinterpret_cast<uint16_t*>(static_cast<char*>(workspace) + w.dy);
-        realign_kernel<<<(unsigned)std::min<int64_t>(M, (int64_t)fmm_sm_count() * 8), 256, 0, st>>>(static_cast<const uint16_t*>(dY), ldy, copy, w.ld_dy, (int)M, (int)N);
+        realign_kernel<<<(unsigned)std::min<int64_t>(M, (int64_t)int8_sm_count() * 8), 256, 0, st>>>(static_cast<const uint16_t*>(dY), ldy, copy, w.ld_dy, (int)M, (int)N);
         if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;
         dy = {copy, M, N, w.ld_dy};
     }
@@ -780,46 +792,37 @@ fmm_status_t grad(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* co
 
 extern "C" {
 
-fmm_status_t fmm_int8_matmul(const int8_t* A, int64_t lda, const float* a_scales, const int8_t* B, int64_t ldb, const float* b_scales,
-                             const void* bias, int64_t M, int64_t N, int64_t K, void* Cm, fmm_type_t type, int64_t ldc, void* stream)
+fmm_status_t fmm_int8_matmul(const fmm_int8_matmul_t* a, void* stream)
 {
-    if (!int8_type_ok(type)) return FMM_ERR_INVALID_ARG;
+    if (!a || !int8_type_ok(a->type)) return FMM_ERR_INVALID_ARG;
+    const int64_t M = a->M, N = a->N, K = a->K;
     if (!dim_ok(M) || !dim_ok(N) || K < 0 || K > 131071) return FMM_ERR_SHAPE;
     if (M == 0 || N == 0) return FMM_OK;
-    const int e = int8_type_bytes(type);
-    if (!Cm || ldc < N || ((uintptr_t)Cm & (e - 1)) || ((uintptr_t)bias & (e - 1))) return FMM_ERR_INVALID_ARG;
+    const int e = int8_type_bytes(a->type);
+    if (!a->c || a->ldc < N || ((uintptr_t)a->c & (e - 1)) || ((uintptr_t)a->bias & (e - 1))) return FMM_ERR_INVALID_ARG;
     ProductParams p = {};
     p.rows = (int)N; p.cols = (int)M;
-    p.r_scales = b_scales; p.c_scales = a_scales; p.bias = bias;
-    p.out = Cm; p.ldo = ldc; p.out_type = type;
-    int8_add_range(p.ranges, Cm, M, N, ldc, e);
+    p.r_scales = a->b_scales; p.c_scales = a->a_scales; p.bias = a->bias;
+    p.out = a->c; p.ldo = a->ldc; p.out_type = a->type;
+    int8_add_range(p.ranges, a->c, M, N, a->ldc, e);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     if (K == 0) return launch_empty(p, st);
-    if (!A || !B || !a_scales || !b_scales || (((uintptr_t)a_scales | (uintptr_t)b_scales) & 3) || lda < K || ldb < K ||
-        !int8_aligned(A, lda, 16) || !int8_aligned(B, ldb, 16)) return FMM_ERR_INVALID_ARG;
+    if (!a->a || !a->b || !a->a_scales || !a->b_scales || (((uintptr_t)a->a_scales | (uintptr_t)a->b_scales) & 3) || a->lda < K || a->ldb < K ||
+        !int8_aligned(a->a, a->lda, 16) || !int8_aligned(a->b, a->ldb, 16)) return FMM_ERR_INVALID_ARG;
     p.kstages = p.chunk = (int)ceil_div(K, 128);
     p.idesc = (2u << 4) | (1u << 7) | (1u << 10);
-    return launch_product<INT8>(p, {B, N, K, ldb}, {A, M, K, lda}, st);
+    return launch_product<INT8>(p, {a->b, N, K, a->ldb}, {a->a, M, K, a->lda}, st);
 }
 
-fmm_status_t fmm_int8_grad_workspace_bytes(int64_t code_rows, int64_t K, int64_t M, int64_t N, int dy_aligned, size_t* bytes)
+fmm_status_t fmm_int8_grad_weight_workspace_bytes(const fmm_int8_grad_t* p, size_t* bytes) { return grad_workspace_bytes<GRAD_W>(p, bytes); }
+fmm_status_t fmm_int8_grad_input_workspace_bytes(const fmm_int8_grad_t* p, size_t* bytes) { return grad_workspace_bytes<GRAD_X>(p, bytes); }
+fmm_status_t fmm_int8_grad_weight(const fmm_int8_grad_t* p, void* workspace, size_t workspace_bytes, void* stream)
 {
-    if (!bytes) return FMM_ERR_INVALID_ARG;
-    if (!dim_ok(code_rows) || !dim_ok(K) || !dim_ok(M) || !dim_ok(N)) return FMM_ERR_SHAPE;
-    *bytes = grad_workspace(code_rows, K, M, N, dy_aligned != 0).total;
-    return FMM_OK;
+    return grad<GRAD_W>(p, workspace, workspace_bytes, stream);
 }
-
-fmm_status_t fmm_int8_grad_weight(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* X, int64_t ldx, const float* x_scales, int64_t M, int64_t N,
-                                  int64_t K, void* dW, fmm_type_t out_type, int64_t ldw, int accumulate, void* workspace, size_t workspace_bytes, void* stream)
+fmm_status_t fmm_int8_grad_input(const fmm_int8_grad_t* p, void* workspace, size_t workspace_bytes, void* stream)
 {
-    return grad<GRAD_W>(dY, type, ldy, X, ldx, x_scales, M, N, K, dW, out_type, ldw, accumulate, workspace, workspace_bytes, stream);
-}
-
-fmm_status_t fmm_int8_grad_input(const void* dY, fmm_type_t type, int64_t ldy, const int8_t* W, int64_t ldw, const float* w_scales, int64_t M, int64_t N,
-                                 int64_t K, void* dX, fmm_type_t out_type, int64_t ldx, void* workspace, size_t workspace_bytes, void* stream)
-{
-    return grad<GRAD_X>(dY, type, ldy, W, ldw, w_scales, M, N, K, dX, out_type, ldx, 0, workspace, workspace_bytes, stream);
+    return grad<GRAD_X>(p, workspace, workspace_bytes, stream);
 }
 
 fmm_status_t fmm_int8_status(int* code)

@@ -751,7 +751,7 @@ BackShape back_shape(int64_t rows, int64_t cols)
     const int64_t groups = (cols + 7) / 8;
     const int threads = groups <= 1024 ? (int)(groups + 32 * BACK_VPT - 1) / (32 * BACK_VPT) * 32 : 0;
     const int64_t per_sm = threads == 32 ? 4 : threads ? 512 / threads : 1, rows_at_once = threads == 32 ? 4 : 1;
-    const int64_t resident = (int64_t)fmm_sm_count() * per_sm, by_rows = (rows + 4 * rows_at_once - 1) / (4 * rows_at_once);
+    const int64_t resident = (int64_t)int8_sm_count() * per_sm, by_rows = (rows + 4 * rows_at_once - 1) / (4 * rows_at_once);
     return {threads, (int)(by_rows < 1 ? 1 : by_rows < resident ? by_rows : resident)};
 }
 int64_t partial_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
@@ -788,7 +788,8 @@ dim3 flat_block(int cols)
 // (a block per row instead of 32 blocks an SM: 16384 x 8192 bf16 quantized in 77.7 instead of 74.2 us, restored in 68.0 instead of 63.8)
 unsigned flat_grid(int rows, dim3 block)
 {
-    const int64_t need = ((int64_t)rows + block.y - 1) / block.y, most = (int64_t)fmm_sm_count() * 32;
+    constexpr int64_t most = 148 * 32;
+    const int64_t need = ((int64_t)rows + block.y - 1) / block.y;
     return (unsigned)(need < most ? need : most);
 }
 
@@ -814,16 +815,21 @@ fmm_status_t int8_rows_guard_read(int* code, bool clear)
 
 extern "C" {
 
-fmm_status_t fmm_int8_quantize(const void* X, fmm_type_t type, int64_t ldx, int64_t rows, int64_t cols, int block,
-                               fmm_int8_scale_t scale_mode, int8_t* codes, int64_t ldc, float* scales, void* stream)
+fmm_status_t fmm_int8_quantize(const fmm_int8_quantize_t* a, void* stream)
 {
-    if (!int8_type_ok(type) || !block_ok(block) || (scale_mode != FMM_INT8_SCALE_AMAX_DIV_127 && scale_mode != FMM_INT8_SCALE_POW2)) return FMM_ERR_INVALID_ARG;
-    if (!dims_ok(rows, cols)) return FMM_ERR_SHAPE;
+    if (!a || !int8_type_ok(a->type) || !block_ok(a->block) ||
+        (a->scale_mode != FMM_INT8_SCALE_AMAX_DIV_127 && a->scale_mode != FMM_INT8_SCALE_POW2)) return FMM_ERR_INVALID_ARG;
+    if (!dims_ok(a->rows, a->cols)) return FMM_ERR_SHAPE;
+    const int64_t rows = a->rows, cols = a->cols, ldx = a->ldx, ldc = a->ldc;
+    const int block = a->block, e = int8_type_bytes(a->type);
+    const fmm_type_t type = a->type;
+    const void* X = a->x;
+    int8_t* codes = a->codes;
+    float* scales = a->scales;
     if (rows == 0 || (cols == 0 && block)) return FMM_OK;
-    const int e = int8_type_bytes(type);
     if (!matrix_ok(scales, 1, 1, 4) || (cols > 0 && (!matrix_ok(X, cols, ldx, e) || !matrix_ok(codes, cols, ldc, 1)))) return FMM_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const bool vx = int8_aligned(X, ldx * e, 16) && cols % 8 == 0, vc = int8_aligned(codes, ldc, 8), pow2 = scale_mode == FMM_INT8_SCALE_POW2;
+    const bool vx = int8_aligned(X, ldx * e, 16) && cols % 8 == 0, vc = int8_aligned(codes, ldc, 8), pow2 = a->scale_mode == FMM_INT8_SCALE_POW2;
     Int8Ranges ranges = {};
     int8_add_range(ranges, codes, rows, cols, ldc, 1);
     if (block) {
@@ -850,13 +856,17 @@ fmm_status_t fmm_int8_quantize(const void* X, fmm_type_t type, int64_t ldx, int6
     return launch_rows<__half, false>(p, st);
 }
 
-fmm_status_t fmm_int8_dequantize(const int8_t* codes, int64_t ldc, const float* scales, int64_t rows, int64_t cols, int block,
-                                 void* X, fmm_type_t type, int64_t ldx, void* stream)
+fmm_status_t fmm_int8_dequantize(const fmm_int8_dequantize_t* a, void* stream)
 {
-    if (!int8_type_ok(type) || !block_ok(block)) return FMM_ERR_INVALID_ARG;
-    if (!dims_ok(rows, cols)) return FMM_ERR_SHAPE;
+    if (!a || !int8_type_ok(a->type) || !block_ok(a->block)) return FMM_ERR_INVALID_ARG;
+    if (!dims_ok(a->rows, a->cols)) return FMM_ERR_SHAPE;
+    const int64_t rows = a->rows, cols = a->cols, ldx = a->ldx, ldc = a->ldc;
+    const int block = a->block, e = int8_type_bytes(a->type);
+    const fmm_type_t type = a->type;
+    const int8_t* codes = a->codes;
+    const float* scales = a->scales;
+    void* X = a->x;
     if (rows == 0 || cols == 0) return FMM_OK;
-    const int e = int8_type_bytes(type);
     if (!matrix_ok(codes, cols, ldc, 1) || !matrix_ok(scales, 1, 1, 4) || !matrix_ok(X, cols, ldx, e)) return FMM_ERR_INVALID_ARG;
     Int8Ranges ranges = {};
     int8_add_range(ranges, X, rows, cols, ldx, e);

@@ -29,10 +29,19 @@ def test_every_declared_symbol_is_exported(lib):
         assert hasattr(lib, name)
 
 
+def filled(kind, base, changes):
+    a = kind()
+    for k, v in {**base, **changes}.items():
+        assert k in dict(kind._fields_)
+        setattr(a, k, v)
+    return C.byref(a)
+
+
 def test_quantize_refusals(lib):
-    def call(x=P, type=0, ldx=64, rows=4, cols=64, block=0, mode=0, codes=P, ldc=64, scales=P):
-        return lib.fmm_int8_quantize(x, type, ldx, rows, cols, block, mode, codes, ldc, scales, None)
-    for bad in (dict(x=None), dict(codes=None), dict(scales=None), dict(type=3), dict(block=64), dict(mode=2), dict(ldx=63), dict(ldc=63),
+    base = dict(x=P, type=0, ldx=64, rows=4, cols=64, block=0, scale_mode=0, codes=P, ldc=64, scales=P)
+    call = lambda **kw: lib.fmm_int8_quantize(filled(int8.QuantizeArgs, base, kw), None)
+    assert lib.fmm_int8_quantize(None, None) == INVALID
+    for bad in (dict(x=None), dict(codes=None), dict(scales=None), dict(type=3), dict(block=64), dict(scale_mode=2), dict(ldx=63), dict(ldc=63),
                 dict(x=P + 2), dict(x=P + 1, type=1), dict(scales=P + 2)):
         assert call(**bad) == INVALID, bad
     for bad in (dict(rows=-1), dict(cols=-1), dict(rows=1 << 31), dict(cols=1 << 40), dict(rows=(1 << 62) + 1, cols=8)):
@@ -42,8 +51,9 @@ def test_quantize_refusals(lib):
 
 
 def test_dequantize_refusals(lib):
-    def call(codes=P, ldc=64, scales=P, rows=4, cols=64, block=0, x=P, type=0, ldx=64):
-        return lib.fmm_int8_dequantize(codes, ldc, scales, rows, cols, block, x, type, ldx, None)
+    base = dict(codes=P, ldc=64, scales=P, rows=4, cols=64, block=0, x=P, type=0, ldx=64)
+    call = lambda **kw: lib.fmm_int8_dequantize(filled(int8.DequantizeArgs, base, kw), None)
+    assert lib.fmm_int8_dequantize(None, None) == INVALID
     for bad in (dict(x=None), dict(codes=None), dict(scales=None), dict(type=-1), dict(block=16), dict(ldx=63), dict(ldc=63), dict(x=P + 2)):
         assert call(**bad) == INVALID, bad
     assert call(rows=-1) == SHAPE
@@ -91,34 +101,38 @@ def test_rms_norm_backward_refusals(lib):
 
 
 def test_matmul_refusals(lib):
-    def call(a=P, lda=64, sa=P, b=P, ldb=64, sb=P, bias=None, M=4, N=4, K=64, c=P, type=0, ldc=4):
-        return lib.fmm_int8_matmul(a, lda, sa, b, ldb, sb, bias, M, N, K, c, type, ldc, None)
-    for bad in (dict(a=None), dict(b=None), dict(sa=None), dict(sb=None), dict(c=None), dict(type=3), dict(lda=48), dict(ldb=48), dict(lda=72), dict(ldb=72),
-                dict(a=P + 8), dict(b=P + 8), dict(ldc=3), dict(c=P + 2), dict(bias=P + 2), dict(sa=P + 2)):
+    base = dict(a=P, lda=64, a_scales=P, b=P, ldb=64, b_scales=P, bias=None, M=4, N=4, K=64, c=P, type=0, ldc=4)
+    call = lambda **kw: lib.fmm_int8_matmul(filled(int8.MatmulArgs, base, kw), None)
+    assert lib.fmm_int8_matmul(None, None) == INVALID
+    for bad in (dict(a=None), dict(b=None), dict(a_scales=None), dict(b_scales=None), dict(c=None), dict(type=3), dict(lda=48), dict(ldb=48), dict(lda=72),
+                dict(ldb=72), dict(a=P + 8), dict(b=P + 8), dict(ldc=3), dict(c=P + 2), dict(bias=P + 2), dict(a_scales=P + 2)):
         assert call(**bad) == INVALID, bad
     for bad in (dict(M=-1), dict(N=-1), dict(K=-1), dict(K=131072, lda=131072, ldb=131072), dict(M=1 << 31), dict(N=1 << 33, ldc=1 << 33)):
         assert call(**bad) == SHAPE, bad
     assert call(M=0, a=None, c=None) == OK and call(N=0, b=None, c=None) == OK
 
 
-def test_grad_refusals(lib):
-    def call(dy=P, type=1, ldy=64, codes=P, ldc=32, scales=P, M=8, N=64, K=32, out=P, out_type=0, ldo=32, ws=P, ws_bytes=1 << 30, weight=True):
-        head = (dy, type, ldy, codes, ldc, scales, M, N, K, out, out_type, ldo)
-        return lib.fmm_int8_grad_weight(*head, 0, ws, ws_bytes, None) if weight else lib.fmm_int8_grad_input(*head, ws, ws_bytes, None)
-    for weight in (True, False):
-        for bad in (dict(dy=None), dict(codes=None), dict(scales=None), dict(out=None), dict(type=0), dict(out_type=2), dict(ldy=63), dict(ldc=31),
-                    dict(ldo=31), dict(out=P + 2), dict(dy=P + 1), dict(scales=P + 1)):
-            assert call(weight=weight, **bad) == INVALID, bad
-        assert call(weight=weight, M=-1) == SHAPE and call(weight=weight, N=1 << 31) == SHAPE
-        assert call(weight=weight, ws=None) == WORKSPACE and call(weight=weight, ws=P + 128) == WORKSPACE
-        rows = 8 if weight else 64
-        need = C.c_size_t()
-        for aligned in (1, 0):
-            assert lib.fmm_int8_grad_workspace_bytes(rows, 32, 8, 64, aligned, C.byref(need)) == OK
-            shift = 0 if aligned else 2
-            assert call(weight=weight, dy=P + shift, ws_bytes=need.value - 1) == WORKSPACE
-        assert call(weight=weight, K=0, out=None) == OK
-    assert lib.fmm_int8_grad_workspace_bytes(8, 32, 8, 64, 1, None) == INVALID
+@pytest.mark.parametrize("which", ["weight", "input"])
+def test_grad_refusals(lib, which):
+    base = dict(dy=P, type=1, ldy=64, codes=P, ldc=32, scales=P, M=8, N=64, K=32, out=P, out_type=0, ldo=32)
+    run, ask = getattr(lib, f"fmm_int8_grad_{which}"), getattr(lib, f"fmm_int8_grad_{which}_workspace_bytes")
+    call = lambda ws=P, ws_bytes=1 << 30, **kw: run(filled(int8.GradArgs, base, kw), ws, ws_bytes, None)
+    assert run(None, P, 1 << 30, None) == INVALID
+    for bad in (dict(dy=None), dict(codes=None), dict(scales=None), dict(out=None), dict(type=0), dict(out_type=2), dict(ldy=63), dict(ldc=31),
+                dict(ldo=31), dict(out=P + 2), dict(dy=P + 1), dict(scales=P + 1)):
+        assert call(**bad) == INVALID, bad
+    assert call(M=-1) == SHAPE and call(N=1 << 31) == SHAPE
+    assert call(ws=None) == WORKSPACE and call(ws=P + 128) == WORKSPACE
+    need = C.c_size_t()
+    sizes = []
+    for dy in (P, P + 2):
+        assert ask(filled(int8.GradArgs, base, dict(dy=dy)), C.byref(need)) == OK
+        assert call(dy=dy, ws_bytes=need.value - 1) == WORKSPACE
+        sizes.append(need.value)
+    assert sizes[1] > sizes[0] >= 2 * 32 * (8 if which == "weight" else 64)
+    assert call(K=0, out=None) == OK
+    assert ask(filled(int8.GradArgs, base, {}), None) == INVALID and ask(None, C.byref(need)) == INVALID
+    assert ask(filled(int8.GradArgs, base, dict(K=-1)), C.byref(need)) == SHAPE
 
 
 def test_binding_wants_cuda_tensors_of_the_right_type():
