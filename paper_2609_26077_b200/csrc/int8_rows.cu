@@ -5,6 +5,7 @@
 // A thread owns groups of eight consecutive columns (16 bytes of a 16-bit type); group v of a row is thread v mod NT, so
 // that a block of 32 (128) columns is 4 (16) neighbouring lanes of one warp and its maximum takes 2 (4) shuffles.
 #include <math.h>
+#include <type_traits>
 #include "fmm_ptx.cuh"
 #include "int8_internal.h"
 
@@ -16,17 +17,18 @@ __device__ int g_int8_rows_guard;
 #define ROW_STORE_OK(ptr, bytes, code) INT8_STORE_OK(p.ranges, ptr, bytes, code, &g_int8_rows_guard)
 
 // ---------------------------------------------------------------------------------------- eight columns of a row
-// Kernels exist for rows that all start on 16-byte boundaries and have a multiple of eight columns (AL: all of a thread's eight exist,
-// or none), and for any.  In the second kind a row is read by the aligned 16-byte vectors that hold an element of it, and a thread's eight columns are shifted out of two (fp32: three) of them; it is
+// Kernels exist for any rows (AL 0), for rows that all start on 16-byte boundaries and have a multiple of eight columns (1: all of a
+// thread's eight exist, or none), and for such rows that fill every thread (2: nothing is tested).  Of the first kind a row is read by the
+// aligned 16-byte vectors that hold an element of it, and a thread's eight columns are shifted out of two (fp32: three) of them; it is
 // written the same way, neighbouring lanes passing on what belongs to the other's vector; so an output in an input's place holds: a
 // lane stores its neighbour's columns only with that lane's numbers, and what else a vector held of others is not used.  (1000 rows of 4095 fp16 columns through the
 // norm: 19.3 us element by element, 8.3 this way.)  The offset `m` of a row within its vector is the same for all its columns.
-template <typename T, bool AL> struct Raw8 { uint32_t w[AL ? sizeof(T) * 2 : sizeof(T) * 2 + 4]; };
+template <typename T, int AL> struct Raw8 { uint32_t w[AL ? sizeof(T) * 2 : sizeof(T) * 2 + 4]; };
 
 template <typename T> __device__ __forceinline__ int row_offset(const T* row) { return (int)(((uintptr_t)row & 15) / sizeof(T)); }
 
 // columns [col, col + 8) of a row of which n are left from col on (0 or less: none is read, zeros)
-template <typename T, bool AL> __device__ __forceinline__ Raw8<T, AL> load8(const T* row, int col, int n)
+template <typename T, int AL> __device__ __forceinline__ Raw8<T, AL> load8(const T* row, int col, int n)
 {
     constexpr int PER = 16 / sizeof(T);
     const int m = AL ? 0 : row_offset(row);
@@ -34,7 +36,7 @@ template <typename T, bool AL> __device__ __forceinline__ Raw8<T, AL> load8(cons
     Raw8<T, AL> r;
 #pragma unroll
     for (int i = 0; i < 8 / PER + (AL ? 0 : 1); ++i) {
-        const bool some = AL || i == 0 ? n > 0 : i * PER < m + 8 && n > i * PER - m;
+        const bool some = AL == 2 || (AL || i == 0 ? n > 0 : i * PER < m + 8 && n > i * PER - m);
         const uint4 v = some ? p[i] : make_uint4(0u, 0u, 0u, 0u);
         r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
     }
@@ -54,7 +56,7 @@ template <typename T, int N, int M> __device__ __forceinline__ void shift_words(
     }
 }
 // the eight numbers, zeros for those behind the row's end.  m: row_offset
-template <typename T, bool AL> __device__ __forceinline__ void unpack8(const Raw8<T, AL>& r, int m, int n, float (&f)[8])
+template <typename T, int AL> __device__ __forceinline__ void unpack8(const Raw8<T, AL>& r, int m, int n, float (&f)[8])
 {
     constexpr int N = sizeof(T) * 2;
     uint32_t w[AL ? N : N + 4];
@@ -75,7 +77,7 @@ template <typename T, bool AL> __device__ __forceinline__ void unpack8(const Raw
     }
 }
 // Columns [col, col + 8) of a row of which n are left.  Every lane of the warp calls it, lane l + 1 for the next eight columns.
-template <typename T, bool AL, typename P> __device__ __forceinline__ void store8(T* row, int col, int n, const float (&f)[8], const P& p, int code)
+template <typename T, int AL, typename P> __device__ __forceinline__ void store8(T* row, int col, int n, const float (&f)[8], const P& p, int code)
 {
     constexpr int N = sizeof(T) * 2;
     uint32_t w[N + 4 + N];                                    // (aligned: the first N)
@@ -97,7 +99,7 @@ template <typename T, bool AL, typename P> __device__ __forceinline__ void store
         for (int i = 0; i < 8; ++i) if (i >= from && i < to && i < n) q[i] = from_float<T>(f[i]);
     };
     if constexpr (AL) {
-        if (n > 0) store_vectors(q);
+        if (AL == 2 || n > 0) store_vectors(q);
     } else {
         // this lane's vectors hold the last m elements of the lane before and the first 8 - m of its own
         const int m = row_offset(row), lane = threadIdx.x & 31;
@@ -183,12 +185,12 @@ __device__ __forceinline__ uint2 codes8(const float (&f)[8], float inverse)
     auto four = [&](int o) { return __byte_perm(__byte_perm(b[o], b[o + 1], 0x0040), __byte_perm(b[o + 2], b[o + 3], 0x0040), 0x5410); };
     return make_uint2(four(0), four(4));
 }
+template <int N> __device__ __forceinline__ void share_scales(const uint32_t (&m)[N], int lanes, bool pow2, Scale (&s)[N]);
+
 // Maxima of N groups of eight columns to those of the blocks they lie in, a block being `lanes` (4 or 16) neighbouring lanes, and the
-// blocks' scales.  A block's lanes share the divisions out (two IEEE divisions per block and thread made the quantization of 16384 x
-// 8192 bf16 numbers take 118 us instead of 66).
+// blocks' scales.
 template <int N> __device__ __forceinline__ void block_scales(uint32_t (&m)[N], int lanes, bool pow2, Scale (&s)[N])
 {
-    static_assert(N == 1 || N == 2 || N == 4, "groups of a thread");
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         m[i] = max(m[i], __shfl_xor_sync(0xffffffffu, m[i], 1));
@@ -198,6 +200,12 @@ template <int N> __device__ __forceinline__ void block_scales(uint32_t (&m)[N], 
             m[i] = max(m[i], __shfl_xor_sync(0xffffffffu, m[i], 8));
         }
     }
+    share_scales(m, lanes, pow2, s);
+}
+// The scales of N blocks whose maxima all of `lanes` neighbouring lanes know: they share the divisions out.
+template <int N> __device__ __forceinline__ void share_scales(const uint32_t (&m)[N], int lanes, bool pow2, Scale (&s)[N])
+{
+    static_assert(N == 1 || N == 2 || N == 4, "groups of a thread");
     const int lane = threadIdx.x & 31, k = lane & (lanes - 1), first = lane - k;
     uint32_t mine = m[0];
     if (N > 1) mine = k & 1 ? m[1] : mine;
@@ -225,32 +233,60 @@ template <int N> __device__ __forceinline__ void block_scales(uint32_t (&m)[N], 
 }
 
 // ---------------------------------------------------------------------------------------- sums over a row's threads
-template <int NT> __device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* red)
+// (`warps` of them, of a block's row; one: no shared memory)
+__device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* red, int warps)
 {
     m = __reduce_max_sync(0xffffffffu, m);
-    if constexpr (NT > 32) {
+    if (warps > 1) {
         if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
         __syncthreads();
         const int lane = threadIdx.x & 31;
-        m = __reduce_max_sync(0xffffffffu, lane < NT / 32 ? red[lane] : 0u);
+        m = __reduce_max_sync(0xffffffffu, lane < warps ? red[lane] : 0u);
     }
     return m;
 }
 // always the same order: lanes by halves, then the warps by halves
-template <int NT, typename F> __device__ __forceinline__ F row_sum(F v, F* red)
+template <typename F> __device__ __forceinline__ F warp_sum(F v)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if constexpr (NT > 32) {
+    return v;
+}
+__device__ __forceinline__ float row_sum(float v, float* red, int warps)
+{
+    v = warp_sum(v);
+    if (warps > 1) {
         if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
         __syncthreads();
         const int lane = threadIdx.x & 31;
-        v = lane < NT / 32 ? red[lane] : (F)0;
-#pragma unroll
-        for (int o = NT / 64; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        v = __shfl_sync(0xffffffffu, v, 0);
+        v = warp_sum(lane < warps ? red[lane] : 0.0f);
     }
     return v;
+}
+// 1 / sqrt(mean of squares + eps).  One warp takes the last sum, the division and the root (in fp64 a fifth of what a norm issued, by
+// all warps)
+__device__ __forceinline__ float row_rstd(double v, double* red, float* result, int warps, int cols, double eps)
+{
+    auto root = [&](double sum) { return (float)(1.0 / sqrt(sum / (double)cols + eps)); };
+    v = warp_sum(v);
+    if (warps == 1) return root(v);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        v = warp_sum(lane < warps ? red[lane] : 0.0);
+        if (lane == 0) *result = root(v);
+    }
+    __syncthreads();
+    return *result;
+}
+// both numbers of a row's scale, a division by half of the lanes each
+__device__ __forceinline__ Scale row_scale(uint32_t amax_bits, bool pow2)
+{
+    uint32_t m[1] = {amax_bits};
+    Scale s[1];
+    share_scales(m, 4, pow2, s);
+    return s[0];
 }
 
 // ---------------------------------------------------------------------------------------- norm / row-wise quantization
@@ -266,7 +302,7 @@ struct RowsParams {
 };
 
 // N groups of eight columns, at col, col + step, ...
-template <int N> __device__ __forceinline__ void checkpoint8(const RowsParams& p, int64_t row, int col, int step, const float (&h)[N][8])
+template <int AL, int N> __device__ __forceinline__ void checkpoint8(const RowsParams& p, int64_t row, int col, int step, const float (&h)[N][8])
 {
     const int shift = p.block == 32 ? 5 : 7, lanes = 1 << (shift - 3), per_row = (p.cols + p.block - 1) >> shift;
     uint32_t m[N];
@@ -274,104 +310,101 @@ template <int N> __device__ __forceinline__ void checkpoint8(const RowsParams& p
 #pragma unroll
     for (int i = 0; i < N; ++i) m[i] = abs_max8(h[i]);
     block_scales(m, lanes, false, s);
+    int8_t* codes = p.checkpoint + row * p.ldk;
+    float* scales = p.checkpoint_scales + row * per_row;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int c = col + i * step, n = p.cols - c;
+        const int c = col + i * step, n = AL == 2 ? 8 : p.cols - c;
         if (n <= 0) continue;
-        store_codes8(p.checkpoint + row * p.ldk + c, codes8(h[i], s[i].inverse), n, p.vk, p, 2101);
-        if ((c & (p.block - 1)) == 0) {
-            float* q = p.checkpoint_scales + row * per_row + (c >> shift);
-            if (ROW_STORE_OK(q, 4, 2102)) *q = s[i].scale;
-        }
+        store_codes8(codes + c, codes8(h[i], s[i].inverse), n, AL == 2 || p.vk, p, 2101);
+        if ((c & (p.block - 1)) == 0 && ROW_STORE_OK(scales + (c >> shift), 4, 2102)) scales[c >> shift] = s[i].scale;
     }
 }
 
-// A row per NT threads, held in registers: VPT groups of eight columns a thread.  The squares are summed in fp64 (they are
-// exact there), so that the reciprocal root does not depend on the order of the sum and codes are the same on every machine.
-template <typename T, bool NORM, bool AL, int NT, int VPT>
-__global__ void __launch_bounds__(NT == 32 ? 128 : NT) rows_kernel(const RowsParams p)
+// A row per block of threads, or (SHORT) per warp, four to a block; held in registers, VPT groups of eight columns a thread.  The squares
+// are summed in fp64 (they are exact there), so that the reciprocal root does not depend on the order of the sum and codes are the same
+// on every machine.
+template <typename T, bool NORM, int AL, int VPT, bool SHORT>
+__global__ void __launch_bounds__(SHORT ? 128 : VPT == 2 ? 256 : 512) rows_kernel(const RowsParams p)
 {
     __shared__ double red_sum[32];
+    __shared__ float rstd_all;
     __shared__ uint32_t red_max[32];
-    constexpr int RPC = NT == 32 ? 4 : 1;
-    const int t = threadIdx.x;
-    const int64_t row = (int64_t)blockIdx.x * RPC + threadIdx.y;
-    if (RPC > 1 && row >= p.rows) return;                     // whole warps
+    const int t = threadIdx.x, NT = SHORT ? 32 : blockDim.x, step = 8 * NT;
+    const int64_t row = SHORT ? (int64_t)blockIdx.x * 4 + threadIdx.y : (int64_t)blockIdx.x;
+    if (SHORT && row >= p.rows) return;                       // whole warps
+    auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (8 * t + i * step); };
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const int mx = AL ? 0 : row_offset(x);
     float h[VPT][8];
     Raw8<T, AL> raw[VPT];
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); raw[i] = load8<T, AL>(x, col, p.cols - col); }
+    for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(x, 8 * t + i * step, left(i));
     if constexpr (NORM) {
         if (p.residual) {
             const T* r = static_cast<const T*>(p.residual) + row * p.ldr;
             const int mr = AL ? 0 : row_offset(r);
             Raw8<T, AL> rawr[VPT];
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); rawr[i] = load8<T, AL>(r, col, p.cols - col); }
+            for (int i = 0; i < VPT; ++i) rawr[i] = load8<T, AL>(r, 8 * t + i * step, left(i));
             T* hid = static_cast<T*>(p.hidden) + row * p.ldh;
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int n = p.cols - 8 * (i * NT + t);
                 float b[8];
-                unpack8<T, AL>(raw[i], mx, n, h[i]);
-                unpack8<T, AL>(rawr[i], mr, n, b);
+                unpack8<T, AL>(raw[i], mx, left(i), h[i]);
+                unpack8<T, AL>(rawr[i], mr, left(i), b);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[i][j] = __fadd_rn(h[i][j], b[j]);
             }
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); store8<T, AL>(hid, col, p.cols - col, h[i], p, 2103); }
+            for (int i = 0; i < VPT; ++i) store8<T, AL>(hid, 8 * t + i * step, left(i), h[i], p, 2103);
         } else {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) unpack8<T, AL>(raw[i], mx, p.cols - 8 * (i * NT + t), h[i]);
+            for (int i = 0; i < VPT; ++i) unpack8<T, AL>(raw[i], mx, left(i), h[i]);
         }
         const T* gain = static_cast<const T*>(p.gain);
         const int mg = AL ? 0 : row_offset(gain);
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); raw[i] = load8<T, AL>(gain, col, p.cols - col); }
+        for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(gain, 8 * t + i * step, left(i));
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) { const double v = (double)h[i][j]; sum = fma(v, v, sum); }
-        if (p.block) checkpoint8<VPT>(p, row, 8 * t, 8 * NT, h);
-        sum = row_sum<NT>(sum, red_sum);
-        const float rstd = (float)(1.0 / sqrt(sum / (double)p.cols + p.eps));
+        if (p.block) checkpoint8<AL>(p, row, 8 * t, step, h);
+        const float rstd = row_rstd(sum, red_sum, &rstd_all, NT / 32, p.cols, p.eps);
         if (t == 0 && p.rstd && ROW_STORE_OK(p.rstd + row, 4, 2104)) p.rstd[row] = rstd;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             float g[8];
-            unpack8<T, AL>(raw[i], mg, p.cols - 8 * (i * NT + t), g);
+            unpack8<T, AL>(raw[i], mg, left(i), g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] = __fmul_rn(__fmul_rn(h[i][j], rstd), g[j]);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) unpack8<T, AL>(raw[i], mx, p.cols - 8 * (i * NT + t), h[i]);
+        for (int i = 0; i < VPT; ++i) unpack8<T, AL>(raw[i], mx, left(i), h[i]);
     }
     // behind the last column: h is 0 there, and 0 * rstd is NaN where rstd is infinite (a row of zeros with eps 0), which is what
     // the row's own zeros are as well
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) m = max(m, abs_max8(h[i]));
-    m = row_max<NT>(m, red_max);
-    const Scale s = block_scale(m, p.pow2);
+    const Scale s = row_scale(row_max(m, red_max, NT / 32), p.pow2);
+    int8_t* codes = p.codes + row * p.ldc;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int col = 8 * (i * NT + t);
-        store_codes8(p.codes + row * p.ldc + col, codes8(h[i], s.inverse), p.cols - col, p.vc, p, 2105);
-    }
+    for (int i = 0; i < VPT; ++i) store_codes8(codes + 8 * t + i * step, codes8(h[i], s.inverse), left(i), AL == 2 || p.vc, p, 2105);
     if (t == 0 && ROW_STORE_OK(p.scales + row, 4, 2106)) p.scales[row] = s.scale;
 }
 
 // Rows that do not fit registers: read again for each pass (from L2, mostly).  hidden may be x or residual, so it is written in the
 // last pass.  Every lane goes round as often, as lanes exchange numbers.
-template <typename T, bool NORM, bool AL>
+template <typename T, bool NORM, int AL>
 __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
 {
     constexpr int NT = 1024;
     __shared__ double red_sum[32];
+    __shared__ float rstd_all;
     __shared__ uint32_t red_max[32];
     const int64_t row = blockIdx.x;
     const int t = threadIdx.x, end = (p.cols + 8 * NT - 1) / (8 * NT) * (8 * NT);
@@ -395,10 +428,9 @@ __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
             hidden8(col, h[0]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) { const double d = (double)h[0][j]; sum = fma(d, d, sum); }
-            if (p.block) checkpoint8<1>(p, row, col, 0, h);
+            if (p.block) checkpoint8<AL>(p, row, col, 0, h);
         }
-        sum = row_sum<NT>(sum, red_sum);
-        rstd = (float)(1.0 / sqrt(sum / (double)p.cols + p.eps));
+        rstd = row_rstd(sum, red_sum, &rstd_all, NT / 32, p.cols, p.eps);
         if (t == 0 && p.rstd && ROW_STORE_OK(p.rstd + row, 4, 2114)) p.rstd[row] = rstd;
     }
     auto normed8 = [&](int col, float (&h)[8]) {
@@ -416,7 +448,7 @@ __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
         normed8(col, h);
         m = max(m, abs_max8(h));
     }
-    const Scale s = block_scale(row_max<NT>(m, red_max), p.pow2);
+    const Scale s = row_scale(row_max(m, red_max, NT / 32), p.pow2);
     for (int col = 8 * t; col < end; col += 8 * NT) {
         float h[8];
         hidden8(col, h);
@@ -427,8 +459,11 @@ __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
     if (t == 0 && ROW_STORE_OK(p.scales + row, 4, 2116)) p.scales[row] = s.scale;
 }
 
-// ---------------------------------------------------------------------------------------- quantization in blocks
-// blockDim (columns / 8 / VPT, rows): a thread takes VPT groups of eight columns at a time, all of them loaded before the first is used.
+// ---------------------------------------------------------------------------------------- quantization in blocks, restoring
+// Nothing is summed over a row, so a row is cut into pieces of 1024 columns, a warp to each: four groups of eight columns a thread, 256
+// columns apart, all of them loaded before the first is used.  A block has eight warps, side by side along a row first.
+constexpr int FLAT_VPT = 4, FLAT_STEP = 256, FLAT_PIECE = FLAT_VPT * FLAT_STEP;
+
 struct BlocksParams {
     const void* x; int8_t* codes; float* scales;
     int64_t ldx, ldc;
@@ -436,42 +471,41 @@ struct BlocksParams {
     bool pow2, vc;
     Int8Ranges ranges;
 };
-constexpr int FLAT_VPT = 4;
 
-template <typename T, bool AL>
-__global__ void __launch_bounds__(256) quantize_blocks_kernel(const BlocksParams p)
+template <typename T, int AL>
+__global__ void __launch_bounds__(256, 3) quantize_blocks_kernel(const BlocksParams p)
 {
     constexpr int VPT = FLAT_VPT;
-    const int shift = p.block == 32 ? 5 : 7, lanes = 1 << (shift - 3), per_row = (p.cols + p.block - 1) >> shift, step = 8 * blockDim.x;
-    for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < p.rows; row += (int64_t)gridDim.x * blockDim.y) {
+    const int shift = p.block == 32 ? 5 : 7, lanes = 1 << (shift - 3), per_row = (p.cols + p.block - 1) >> shift;
+    for (int64_t row = (int64_t)blockIdx.x * blockDim.z + threadIdx.z; row < p.rows; row += (int64_t)gridDim.x * blockDim.z) {
         const T* x = static_cast<const T*>(p.x) + row * p.ldx;
         const int mx = AL ? 0 : row_offset(x);
-        for (int first = 0; first < p.cols; first += VPT * step) {
-            const int col = first + 8 * threadIdx.x;
+        for (int piece = threadIdx.y * FLAT_PIECE; piece < p.cols; piece += blockDim.y * FLAT_PIECE) {
+            const int col = piece + 8 * threadIdx.x;
+            auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (col + i * FLAT_STEP); };
             Raw8<T, AL> raw[VPT];
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(x, col + i * step, p.cols - (col + i * step));
+            for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(x, col + i * FLAT_STEP, left(i));
             float f[VPT][8];
             uint32_t m[VPT];
             Scale s[VPT];
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) { unpack8<T, AL>(raw[i], mx, p.cols - (col + i * step), f[i]); m[i] = abs_max8(f[i]); }
+            for (int i = 0; i < VPT; ++i) { unpack8<T, AL>(raw[i], mx, left(i), f[i]); m[i] = abs_max8(f[i]); }
             block_scales(m, lanes, p.pow2, s);
+            int8_t* codes = p.codes + row * p.ldc + col;
+            float* scales = p.scales + row * per_row + (col >> shift);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int c = col + i * step, n = p.cols - c;
+                const int n = left(i);
                 if (n <= 0) continue;
-                store_codes8(p.codes + row * p.ldc + c, codes8(f[i], s[i].inverse), n, p.vc, p, 2121);
-                if ((c & (p.block - 1)) == 0) {
-                    float* q = p.scales + row * per_row + (c >> shift);
-                    if (ROW_STORE_OK(q, 4, 2122)) *q = s[i].scale;
-                }
+                store_codes8(codes + i * FLAT_STEP, codes8(f[i], s[i].inverse), n, AL == 2 || p.vc, p, 2121);
+                float* q = scales + (i * FLAT_STEP >> shift);
+                if ((col & (p.block - 1)) == 0 && ROW_STORE_OK(q, 4, 2122)) *q = s[i].scale;
             }
         }
     }
 }
 
-// ---------------------------------------------------------------------------------------- restoring
 struct RestoreParams {
     const int8_t* codes; const float* scales; void* x;
     int64_t ldc, ldx;
@@ -479,25 +513,26 @@ struct RestoreParams {
     bool vc;
     Int8Ranges ranges;
 };
-template <typename T, bool AL>
+template <typename T, int AL>
 __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
 {
     constexpr int VPT = FLAT_VPT;
     fmmptx::griddep_launch_dependents();                      // (the product of a gradient, which waits for this grid to end)
-    const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, shift = p.block == 32 ? 5 : 7, step = 8 * blockDim.x;
-    for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < p.rows; row += (int64_t)gridDim.x * blockDim.y) {
+    const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, shift = p.block == 32 ? 5 : 7;
+    for (int64_t row = (int64_t)blockIdx.x * blockDim.z + threadIdx.z; row < p.rows; row += (int64_t)gridDim.x * blockDim.z) {
         const int8_t* codes = p.codes + row * p.ldc;
         const float* scales = p.scales + row * per_row;
         T* x = static_cast<T*>(p.x) + row * p.ldx;
-        for (int first = 0; first < p.cols; first += VPT * step) {
-            const int col = first + 8 * threadIdx.x;
+        for (int piece = threadIdx.y * FLAT_PIECE; piece < p.cols; piece += blockDim.y * FLAT_PIECE) {
+            const int col = piece + 8 * threadIdx.x;
+            auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (col + i * FLAT_STEP); };
             uint2 c[VPT];
             float s[VPT];
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int at = col + i * step, n = p.cols - at;
-                c[i] = load_codes8(codes + at, n, p.vc);
-                s[i] = n > 0 ? scales[p.block ? at >> shift : 0] : 0.0f;
+                const int at = col + i * FLAT_STEP;
+                c[i] = load_codes8(codes + at, left(i), AL == 2 || p.vc);
+                s[i] = left(i) > 0 ? scales[p.block ? at >> shift : 0] : 0.0f;
             }
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
@@ -505,7 +540,7 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
                 codes_to_float(c[i], f);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], s[i]);
-                store8<T, AL>(x, col + i * step, p.cols - (col + i * step), f, p, 2131);
+                store8<T, AL>(x, col + i * FLAT_STEP, left(i), f, p, 2131);
             }
         }
     }
@@ -532,28 +567,12 @@ __device__ __forceinline__ void xhat8(uint2 codes, float scale, float rstd, floa
     for (int j = 0; j < 8; ++j) f[j] *= s;
 }
 
-// sum over the warps of a row's threads, however many, in a fixed order
-__device__ __forceinline__ float row_sum_of(float v, float* red, int warps)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (warps > 1) {
-        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-        __syncthreads();
-        const int lane = threadIdx.x & 31;
-        v = lane < warps ? red[lane] : 0.0f;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    }
-    return v;
-}
-
 // Rows are dealt out to groups of threads, a block or (SHORT) a warp, four to a block; each thread has two groups of eight columns.
 // It keeps its columns' sums of dy * xhat in registers over all its rows and the block writes them once, as one row of `partial`;
 // column_sum_kernel adds those rows up in a fixed order.  128 registers a thread let the next row's loads be in flight while this one
 // is summed (NEXT: aligned rows of a 16-bit type; the others' loads are issued together where the row begins).  The gain, the same for
 // all rows, comes from L1 each time.
-template <typename T, bool AL, bool SHORT>
+template <typename T, int AL, bool SHORT>
 __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(const BackParams p)
 {
     constexpr bool NEXT = AL && sizeof(T) == 2;
@@ -577,9 +596,9 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
         rstd = p.rstd[row];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int col = 8 * (i * NT + t), n = p.cols - col;
+            const int col = 8 * (i * NT + t), n = AL == 2 ? 8 : p.cols - col;
             dy[i] = load8<T, AL>(static_cast<const T*>(p.dy) + row * p.ldy, col, n);
-            codes[i] = load_codes8(p.checkpoint + row * p.ldk + col, n, p.vk);
+            codes[i] = load_codes8(p.checkpoint + row * p.ldk + col, n, AL == 2 || p.vk);
             scale[i] = n > 0 ? p.scales[row * per_row + (p.block ? col >> shift : 0)] : 0.0f;
         }
     };
@@ -593,12 +612,12 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
         Raw8<T, AL> add[VPT];
         if (p.dresidual) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); add[i] = load8<T, AL>(dres, col, p.cols - col); }
+            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); add[i] = load8<T, AL>(dres, col, AL == 2 ? 8 : p.cols - col); }
         }
         float out[VPT][8], xh[VPT][8], c = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int col = 8 * (i * NT + t), n = p.cols - col;
+            const int col = 8 * (i * NT + t), n = AL == 2 ? 8 : p.cols - col;
             float g[8];
             unpack8<T, AL>(load8<T, AL>(gain, col, n), mg, n, g);
             unpack8<T, AL>(dy[i], my, n, out[i]);
@@ -611,12 +630,12 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
             }
         }
         if (NEXT && row + groups < p.rows) fetch(row + groups);
-        c = row_sum_of(c, red[parity], NT / 32) / (float)p.cols;
+        c = row_sum(c, red[parity], NT / 32) / (float)p.cols;
         T* dx = static_cast<T*>(p.dx) + row * p.ldx;
         const int mr = AL ? 0 : row_offset(dres);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int col = 8 * (i * NT + t), n = p.cols - col;
+            const int col = 8 * (i * NT + t), n = AL == 2 ? 8 : p.cols - col;
             float b[8];
             if (p.dresidual) unpack8<T, AL>(add[i], mr, n, b);
 #pragma unroll
@@ -648,12 +667,12 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
     }
     float* q = p.partial + (int64_t)blockIdx.x * p.ldp;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); store8<float, true>(q, col, p.cols - col, sum[i], p, 2142); }
+    for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); store8<float, AL == 2 ? 2 : 1>(q, col, p.cols - col, sum[i], p, 2142); }
 }
 
 // Rows that do not fit registers: dy and the codes are read twice (the second time from L2, mostly), and the sums of a group live in
 // its row of `partial`, which no other group touches.
-template <typename T, bool AL>
+template <typename T, int AL>
 __global__ void __launch_bounds__(1024) back_long_kernel(const BackParams p)
 {
     constexpr int NT = 1024;
@@ -682,12 +701,12 @@ __global__ void __launch_bounds__(1024) back_long_kernel(const BackParams p)
             if (row == part) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[j] = 0.0f;
-            } else unpack8<float, true>(load8<float, true>(q, col, p.cols - col), 0, p.cols - col, s);
+            } else unpack8<float, 1>(load8<float, 1>(q, col, p.cols - col), 0, p.cols - col, s);
 #pragma unroll
             for (int j = 0; j < 8; ++j) { s[j] = fmaf(d[j], xh[j], s[j]); c = fmaf(d[j] * g[j], xh[j], c); }
-            store8<float, true>(q, col, p.cols - col, s, p, 2152);
+            store8<float, 1>(q, col, p.cols - col, s, p, 2152);
         }
-        c = row_sum<NT>(c, red[parity]) / (float)p.cols;
+        c = row_sum(c, red[parity], NT / 32) / (float)p.cols;
         for (int col = 8 * t; col < end; col += 8 * NT) {
             float d[8], xh[8], g[8], b[8];
             both8(col, d, xh, g);
@@ -726,21 +745,24 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const BackParams p)
 // ---------------------------------------------------------------------------------------- launches
 fmm_status_t launched() { return cudaGetLastError() == cudaSuccess ? FMM_OK : FMM_ERR_CUDA; }
 
-template <typename T, bool NORM, bool AL> fmm_status_t launch_rows_aligned(const RowsParams& p, cudaStream_t st)
+template <typename T, bool NORM> fmm_status_t launch_rows(const RowsParams& p, cudaStream_t st)
 {
     const int groups = (p.cols + 7) / 8;
     const unsigned rows = (unsigned)p.rows;
-    if (groups <= 64) rows_kernel<T, NORM, AL, 32, 2><<<(rows + 3) / 4, dim3(32, 4), 0, st>>>(p);
-    else if (groups <= 256) rows_kernel<T, NORM, AL, 128, 2><<<rows, 128, 0, st>>>(p);
-    else if (groups <= 512) rows_kernel<T, NORM, AL, 256, 2><<<rows, 256, 0, st>>>(p);
-    else if (groups <= 1024) rows_kernel<T, NORM, AL, 256, 4><<<rows, 256, 0, st>>>(p);
-    else if (groups <= 2048) rows_kernel<T, NORM, AL, 512, 4><<<rows, 512, 0, st>>>(p);
-    else rows_long_kernel<T, NORM, AL><<<rows, 1024, 0, st>>>(p);
+    // two groups a thread up to 4096 columns, four up to 16384
+    const int vpt = groups <= 512 ? 2 : 4, threads = (groups + 32 * vpt - 1) / (32 * vpt) * 32;
+    const bool full = p.aligned && groups == vpt * threads && p.vc && (!p.block || p.vk);
+    auto launch = [&](auto al) {
+        constexpr int AL = decltype(al)::value;
+        if (threads <= 32) rows_kernel<T, NORM, AL, 2, true><<<(rows + 3) / 4, dim3(32, 4), 0, st>>>(p);
+        else if (groups <= 512) rows_kernel<T, NORM, AL, 2, false><<<rows, threads, 0, st>>>(p);
+        else if (groups <= 2048) rows_kernel<T, NORM, AL, 4, false><<<rows, threads, 0, st>>>(p);
+        else rows_long_kernel<T, NORM, AL ? 1 : 0><<<rows, 1024, 0, st>>>(p);
+    };
+    if (full) launch(std::integral_constant<int, 2>{});
+    else if (p.aligned) launch(std::integral_constant<int, 1>{});
+    else launch(std::integral_constant<int, 0>{});
     return launched();
-}
-template <typename T, bool NORM> fmm_status_t launch_rows(const RowsParams& p, cudaStream_t st)
-{
-    return p.aligned ? launch_rows_aligned<T, NORM, true>(p, st) : launch_rows_aligned<T, NORM, false>(p, st);
 }
 
 // Threads among which a row of the norm's gradients is split (0: long rows), and blocks.  A group of threads has at least four rows, so that
@@ -756,16 +778,18 @@ BackShape back_shape(int64_t rows, int64_t cols)
 }
 int64_t partial_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 
-template <typename T, bool AL> void launch_back_aligned(const BackParams& p, int threads, cudaStream_t st)
-{
-    const unsigned blocks = (unsigned)p.parts;
-    if (threads == 32) back_kernel<T, AL, true><<<blocks, dim3(32, 4), 0, st>>>(p);
-    else if (threads) back_kernel<T, AL, false><<<blocks, threads, 0, st>>>(p);
-    else back_long_kernel<T, AL><<<blocks, 1024, 0, st>>>(p);
-}
 template <typename T> fmm_status_t launch_back(const BackParams& p, int threads, cudaStream_t st)
 {
-    if (p.aligned) launch_back_aligned<T, true>(p, threads, st); else launch_back_aligned<T, false>(p, threads, st);
+    const unsigned blocks = (unsigned)p.parts;
+    auto launch = [&](auto al) {
+        constexpr int AL = decltype(al)::value;
+        if (threads == 32) back_kernel<T, AL, true><<<blocks, dim3(32, 4), 0, st>>>(p);
+        else if (threads) back_kernel<T, AL, false><<<blocks, threads, 0, st>>>(p);
+        else back_long_kernel<T, AL ? 1 : 0><<<blocks, 1024, 0, st>>>(p);
+    };
+    if (p.aligned && p.vk && p.cols == 8 * BACK_VPT * threads) launch(std::integral_constant<int, 2>{});
+    else if (p.aligned) launch(std::integral_constant<int, 1>{});
+    else launch(std::integral_constant<int, 0>{});
     if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;
     // set up while the rows are dealt with; it waits for them before its first load
     cudaLaunchConfig_t cfg = {};
@@ -778,18 +802,18 @@ template <typename T> fmm_status_t launch_back(const BackParams& p, int threads,
     return FMM_OK;
 }
 
-// blocks of 256 threads for row-parallel kernels without a reduction: columns / 8 / FLAT_VPT along x, rows along y
+// eight warps of a block without a reduction: pieces of a row along y, rows along z
 dim3 flat_block(int cols)
 {
-    unsigned x = 32;
-    while (x < 256 && 8u * FLAT_VPT * x < (unsigned)cols) x *= 2;
-    return dim3(x, 256 / x);
+    unsigned y = 1;
+    while (y < 8 && y * FLAT_PIECE < (unsigned)cols) y *= 2;
+    return dim3(32, y, 8 / y);
 }
 // (a block per row instead of 32 blocks an SM: 16384 x 8192 bf16 quantized in 77.7 instead of 74.2 us, restored in 68.0 instead of 63.8)
 unsigned flat_grid(int rows, dim3 block)
 {
     constexpr int64_t most = 148 * 32;
-    const int64_t need = ((int64_t)rows + block.y - 1) / block.y;
+    const int64_t need = ((int64_t)rows + block.z - 1) / block.z;
     return (unsigned)(need < most ? need : most);
 }
 
@@ -840,7 +864,9 @@ fmm_status_t fmm_int8_quantize(const fmm_int8_quantize_t* a, void* stream)
         const unsigned grid = flat_grid((int)rows, b);
         auto launch = [&](auto type) {
             using T = decltype(type);
-            if (vx) quantize_blocks_kernel<T, true><<<grid, b, 0, st>>>(p); else quantize_blocks_kernel<T, false><<<grid, b, 0, st>>>(p);
+            if (vx && vc && cols % FLAT_PIECE == 0) quantize_blocks_kernel<T, 2><<<grid, b, 0, st>>>(p);
+            else if (vx) quantize_blocks_kernel<T, 1><<<grid, b, 0, st>>>(p);
+            else quantize_blocks_kernel<T, 0><<<grid, b, 0, st>>>(p);
         };
         if (type == FMM_TYPE_F32) launch(float{});
         else if (type == FMM_TYPE_BF16) launch(__nv_bfloat16{});
@@ -876,7 +902,10 @@ fmm_status_t fmm_int8_dequantize(const fmm_int8_dequantize_t* a, void* stream)
     const unsigned grid = flat_grid((int)rows, b);
     auto launch = [&](auto type) {
         using T = decltype(type);
-        if (int8_aligned(X, ldx * e, 16) && cols % 8 == 0) dequantize_kernel<T, true><<<grid, b, 0, st>>>(p); else dequantize_kernel<T, false><<<grid, b, 0, st>>>(p);
+        const bool aligned = int8_aligned(X, ldx * e, 16) && cols % 8 == 0;
+        if (aligned && p.vc && cols % FLAT_PIECE == 0) dequantize_kernel<T, 2><<<grid, b, 0, st>>>(p);
+        else if (aligned) dequantize_kernel<T, 1><<<grid, b, 0, st>>>(p);
+        else dequantize_kernel<T, 0><<<grid, b, 0, st>>>(p);
     };
     if (type == FMM_TYPE_F32) launch(float{});
     else if (type == FMM_TYPE_BF16) launch(__nv_bfloat16{});
