@@ -325,7 +325,7 @@ template <int AL, int N> __device__ __forceinline__ void checkpoint8(const RowsP
 // are summed in fp64 (they are exact there), so that the reciprocal root does not depend on the order of the sum and codes are the same
 // on every machine.
 template <typename T, bool NORM, int AL, int VPT, bool SHORT>
-__global__ void __launch_bounds__(SHORT ? 128 : VPT == 2 ? 256 : 512) rows_kernel(const RowsParams p)
+__global__ void __launch_bounds__(SHORT ? 128 : VPT == 2 ? 256 : 512, !SHORT && VPT == 4 && AL && sizeof(T) == 2 ? 2 : 1) rows_kernel(const RowsParams p)
 {
     __shared__ double red_sum[32];
     __shared__ float rstd_all;
@@ -362,22 +362,23 @@ __global__ void __launch_bounds__(SHORT ? 128 : VPT == 2 ? 256 : 512) rows_kerne
 #pragma unroll
             for (int i = 0; i < VPT; ++i) unpack8<T, AL>(raw[i], mx, left(i), h[i]);
         }
-        const T* gain = static_cast<const T*>(p.gain);
-        const int mg = AL ? 0 : row_offset(gain);
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(gain, 8 * t + i * step, left(i));
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) { const double v = (double)h[i][j]; sum = fma(v, v, sum); }
-        if (p.block) checkpoint8<AL>(p, row, 8 * t, step, h);
+        if (p.block) {
+#pragma unroll
+            for (int i = 0; i < VPT; i += 2) checkpoint8<AL, 2>(p, row, 8 * t + i * step, step, *reinterpret_cast<const float (*)[2][8]>(&h[i]));
+        }
+        const T* gain = static_cast<const T*>(p.gain);
+        const int mg = AL ? 0 : row_offset(gain);
         const float rstd = row_rstd(sum, red_sum, &rstd_all, NT / 32, p.cols, p.eps);
         if (t == 0 && p.rstd && ROW_STORE_OK(p.rstd + row, 4, 2104)) p.rstd[row] = rstd;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             float g[8];
-            unpack8<T, AL>(raw[i], mg, left(i), g);
+            unpack8<T, AL>(load8<T, AL>(gain, 8 * t + i * step, left(i)), mg, left(i), g);       // (the same for all rows: from L1)
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] = __fmul_rn(__fmul_rn(h[i][j], rstd), g[j]);
         }
