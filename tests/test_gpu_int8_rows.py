@@ -8,8 +8,8 @@ from paper_2609_26077_b200 import fmm, int8
 
 pytestmark = pytest.mark.gpu
 
-# one column, odd ones, around 8 (a thread's columns), 32 and 128 (blocks), 512, 2048, 4096, 8192 (kernels), 16384 and behind (long rows)
-COLS = [1, 7, 31, 33, 127, 130, 512, 520, 1000, 2048, 2056, 4095, 4104, 8192, 8200, 16384]
+# one column, odd ones, around 8 (a thread's columns), 32 and 128 (blocks), 512, 1024, 8192 (kernels), 16384 and behind (long rows)
+COLS = [1, 7, 31, 33, 127, 130, 512, 520, 1000, 1024, 1032, 2048, 2056, 4095, 5120, 8192, 8200, 16384]
 LONG = [16392, 40001]
 
 
