@@ -575,6 +575,98 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
     }
 }
 
+// ------------------------------------------------------------------------------------------------ few tokens
+// C of up to eight tokens: the weight's way from memory bounds it, and this kernel has nothing to set up (the cluster kernel: barriers,
+// TMEM, tensor maps, an exchange; 1 x 8192 x 8192 15.2 us, 14.0 here, 8 x 4096 x 4096 7.7 and 5.4, 1 x 2048 x 2048 5.1 and 2.8).  A block takes
+// 16 output channels, its warps share K: 16 of them, where two such blocks an SM hold all channels (1 x 2048 x 8192 6.7 us, with eight 9.6), else
+// eight, four blocks an SM, so that they come in one wave or in many (1 x 8192 x 8192 14.0 us, with 16 15.4).  The weight goes from global memory straight into the A fragments of mma.m16n8k32, the tokens into the B fragments:
+// a lane loads 16 codes of channel lane / 4, of channel lane / 4 + 8 and of token lane / 4, all at the same place of K, and takes the first
+// eight of each for one mma and the others for the next - both sides number the contraction alike, so any numbering will do.  (dp4a
+// in place of the mma: as fast for one token, 19.3 us for four of them at 8192 x 8192.)
+constexpr int FEW_TOKENS = 8, FEW_CHANNELS = 16, FEW_LOADS = 2;
+
+struct FewParams {
+    const int8_t* a; const int8_t* b;
+    long long lda, ldb;
+    int k;
+    ProductParams p;
+};
+
+__device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16 bytes of a weight, which is read once: not kept in L1, 256 bytes brought into L2
+__device__ __forceinline__ uint4 load_once(const int8_t* p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+template <int FEW_WARPS>
+__global__ void __launch_bounds__(FEW_WARPS * 32, 32 / FEW_WARPS) int8_few_tokens_kernel(const FewParams f)
+{
+    __shared__ int meet[FEW_WARPS][FEW_TOKENS][FEW_CHANNELS + 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const long long n0 = (long long)blockIdx.x * FEW_CHANNELS;
+    const int channels = (int)min((long long)FEW_CHANNELS, f.p.rows - n0), tokens = f.p.cols;
+    const int8_t* w0 = f.b + (n0 + g) * f.ldb + 16 * q;
+    const int8_t* w1 = w0 + 8 * f.ldb;
+    const int8_t* x0 = f.a + g * f.lda + 16 * q;
+    const bool some0 = g < channels, some1 = g + 8 < channels, some = g < tokens;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    int acc[4] = {0, 0, 0, 0};
+    // 64 codes of K a step; a warp takes FEW_LOADS steps at a time, the block's warps side by side
+    constexpr int PIECE = 64 * FEW_LOADS;
+    for (int k0 = warp * PIECE; k0 < f.k; k0 += FEW_WARPS * PIECE) {
+        uint4 u[FEW_LOADS], v[FEW_LOADS], x[FEW_LOADS];
+#pragma unroll
+        for (int i = 0; i < FEW_LOADS; ++i) {
+            const int k = k0 + 64 * i;
+            const bool in = k + 16 * q < f.k;
+            u[i] = in && some0 ? load_once(w0 + k) : zero;
+            v[i] = in && some1 ? load_once(w1 + k) : zero;
+            x[i] = in && some ? *reinterpret_cast<const uint4*>(x0 + k) : zero;
+        }
+#pragma unroll
+        for (int i = 0; i < FEW_LOADS; ++i) {
+            const int left = f.k - (k0 + 64 * i + 16 * q);
+            if (left < 16) {
+                // the codes behind the last one may be anything, on either side: zeros on this one
+                uint32_t* y = &x[i].x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int n = left - 4 * j;
+                    y[j] = n >= 4 ? y[j] : n <= 0 ? 0u : y[j] & ((1u << (8 * n)) - 1u);
+                }
+            }
+            mma_s8(acc, u[i].x, v[i].x, u[i].y, v[i].y, x[i].x, x[i].y);
+            mma_s8(acc, u[i].z, v[i].z, u[i].w, v[i].w, x[i].z, x[i].w);
+        }
+    }
+    // accumulators: channels g and g + 8 of tokens 2q and 2q + 1
+    meet[warp][2 * q][g] = acc[0];
+    meet[warp][2 * q + 1][g] = acc[1];
+    meet[warp][2 * q][g + 8] = acc[2];
+    meet[warp][2 * q + 1][g + 8] = acc[3];
+    __syncthreads();
+    const int r = threadIdx.x % FEW_CHANNELS, m = threadIdx.x / FEW_CHANNELS;
+    if (m < tokens && r < channels) {
+        int s = 0;
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w) s += meet[w][m][r];
+        const int row = (int)n0 + r;
+        const float y = scaled((uint32_t)s, f.p.r_scales[row], f.p.c_scales[m]) + load_bias(f.p, row);
+        const long long at = m * f.p.ldo + row;
+        if (f.p.out_type == FMM_TYPE_F32) put_one<float>(f.p, at, y);
+        else if (f.p.out_type == FMM_TYPE_BF16) put_one<__nv_bfloat16>(f.p, at, y);
+        else put_one<__half>(f.p, at, y);
+    }
+}
+
 // An empty contraction: C = bias, or 0
 __global__ void __launch_bounds__(256) empty_sum_kernel(const ProductParams p)
 {
@@ -677,6 +769,15 @@ struct ProductModel { float pair_lat, pair_stage, pair_tile, exchange, exchange_
 constexpr ProductModel MODEL_INT8 = {6.46f, 0.288f, 2.08f, 2.27f, 0.0f, 2, 4,
     {{16, 1.15f, 0.111f, 0.172f, 1.82f}, {32, 1.65f, 0.208f, 0.190f, 1.84f}, {64, 2.15f, 0.227f, 0.207f, 2.58f}, {128, 3.36f, 0.279f, 0.257f, 3.88f}}};
 constexpr ProductModel MODEL_GRAD = {8.49f, 0.321f, 0.72f, 0.91f, 0.275f, 1, 2, {{64, 2.10f, 0.210f, 0.100f, 3.67f}, {128, 1.61f, 0.263f, 0.232f, 5.02f}}};
+
+fmm_status_t launch_few_tokens(const ProductParams& p, const Operand& b, const Operand& a, cudaStream_t st)
+{
+    const FewParams f = {static_cast<const int8_t*>(a.p), static_cast<const int8_t*>(b.p), a.ld, b.ld, (int)a.cols, p};
+    const int64_t blocks = ceil_div(p.rows, FEW_CHANNELS);
+    if (blocks <= 2 * int8_sm_count()) int8_few_tokens_kernel<16><<<(unsigned)blocks, 512, 0, st>>>(f);
+    else int8_few_tokens_kernel<8><<<(unsigned)blocks, 256, 0, st>>>(f);
+    return cudaGetLastError() == cudaSuccess ? FMM_OK : FMM_ERR_CUDA;
+}
 
 struct ProductChoice { int columns, shares; };               // columns 256: pairs
 ProductChoice choose_product(const ProductModel& m, const ProductParams& p, double bytes, int sms)
@@ -810,6 +911,7 @@ fmm_status_t fmm_int8_matmul(const fmm_int8_matmul_t* a, void* stream)
     if (!a->a || !a->b || !a->a_scales || !a->b_scales || (((uintptr_t)a->a_scales | (uintptr_t)a->b_scales) & 3) || a->lda < K || a->ldb < K ||
         !int8_aligned(a->a, a->lda, 16) || !int8_aligned(a->b, a->ldb, 16)) return FMM_ERR_INVALID_ARG;
     p.kstages = p.chunk = (int)ceil_div(K, 128);
+    if (M <= FEW_TOKENS) return launch_few_tokens(p, {a->b, N, K, a->ldb}, {a->a, M, K, a->lda}, st);
     p.idesc = (2u << 4) | (1u << 7) | (1u << 10);
     return launch_product<INT8>(p, {a->b, N, K, a->ldb}, {a->a, M, K, a->lda}, st);
 }
