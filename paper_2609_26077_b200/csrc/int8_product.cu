@@ -19,7 +19,7 @@
 //
 // The tensor cores add in fp32 by cutting off what does not fit, so the sums of a gradient drift towards zero as the contraction
 // grows: 2.4e-6 of their size over 8192 terms, 6e-6 over 16384.  Where the output is fp32 they are therefore taken out of the
-// accumulator every CHUNK stages (1024 terms) and added up in registers, rounded to nearest: XXX and XXX.  An output of 16 bits has no
+// accumulator every CHUNK stages (1024 terms) and added up in registers, rounded to nearest: 1.9e-7 for both.  An output of 16 bits has no
 // use for that.
 //
 // The 8-bit operand of a gradient is restored to 16 bits by fmm_int8_dequantize into the workspace before the product: 3 bytes a code
@@ -133,7 +133,7 @@ __device__ __forceinline__ float load_bias(const ProductParams& p, int row)
 }
 // N columns from col0 of one row of the output, from a thread's registers, `valid` of which exist.  c_scale: shared address of column
 // col0's scale.  All of them are computed before the first is stored, and whole groups without a test in between: with one the
-// columns came one after the other, 75 cycles each (4096 x 4096 x 128: 47.6 us a call, XXX without).
+// columns came one after the other, 75 cycles each (4096 x 4096 x 128: 47.6 us a call, 19.4 without).
 template <int KIND, int N>
 __device__ __forceinline__ void put_columns(const ProductParams& p, const uint32_t (&v)[N], int row, int col0, int valid, float r_scale, float bias, uint32_t c_scale)
 {

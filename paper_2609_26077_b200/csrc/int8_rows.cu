@@ -2,8 +2,8 @@
 // norm's gradients from an 8-bit checkpoint.  All of them are bound by memory: every kernel reads each input and writes
 // each output once, rows staying in registers between the passes that a row needs (sum of squares, maximum, codes).
 //
-// A thread owns groups of eight consecutive columns (16 bytes of a 16-bit type); group v of a row is thread v mod NT, so
-// that a block of 32 (128) columns is 4 (16) neighbouring lanes of one warp and its maximum takes 2 (4) shuffles.
+// A thread owns groups of eight consecutive columns (16 bytes of a 16-bit type), a warp N * 256 consecutive columns: group i of lane l are
+// columns 256 i + 8 l and on, so that a block of 32 (128) columns is 4 (16) neighbouring lanes and its maximum takes 2 (4) shuffles.
 #include <math.h>
 #include <type_traits>
 #include "fmm_ptx.cuh"
@@ -76,49 +76,68 @@ template <typename T, int AL> __device__ __forceinline__ void unpack8(const Raw8
         for (int i = 0; i < 8; ++i) f[i] = i < n ? f[i] : 0.0f;
     }
 }
-// Columns [col, col + 8) of a row of which n are left.  Every lane of the warp calls it, lane l + 1 for the next eight columns.
-template <typename T, int AL, typename P> __device__ __forceinline__ void store8(T* row, int col, int n, const float (&f)[8], const P& p, int code)
+// The N groups of a warp's lanes, from column col on, of which n are left.  Every lane of the warp calls it.
+constexpr int GROUP = 256;
+template <int AL, int N, typename T, typename P> __device__ __forceinline__ void store_groups(T* row, int col, int n, const float (&f)[N][8], const P& p, int code)
 {
-    constexpr int N = sizeof(T) * 2;
-    uint32_t w[N + 4 + N];                                    // (aligned: the first N)
-    uint32_t* own = w + (AL ? 0 : N);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if constexpr (sizeof(T) == 4) own[i] = __float_as_uint(f[i]);
-        else own[i] = pack_two<T>(f[2 * i], f[2 * i + 1]);
-    }
+    constexpr int W = sizeof(T) * 2;                          // words of a group
     T* q = row + col;
-    auto store_vectors = [&](T* at) {
+    auto pack = [](const float (&g)[8], uint32_t* w) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(g[i]);
+            else w[i] = pack_two<T>(g[2 * i], g[2 * i + 1]);
+        }
+    };
+    auto store_vectors = [&](T* at, const uint32_t* w) {
         if (!ROW_STORE_OK(at, 8 * sizeof(T), code)) return;
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) reinterpret_cast<uint4*>(at)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-    };
-    auto store_some = [&](int from, int to) {                 // elements [from, to) that exist, one by one
-        if (from >= min(to, n) || !ROW_STORE_OK(q + from, (min(to, n) - from) * sizeof(T), code)) return;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i >= from && i < to && i < n) q[i] = from_float<T>(f[i]);
+        for (int i = 0; i < W / 4; ++i) reinterpret_cast<uint4*>(at)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     };
     if constexpr (AL) {
-        if (AL == 2 || n > 0) store_vectors(q);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t w[W];
+            pack(f[i], w);
+            if (AL == 2 || n > i * GROUP) store_vectors(q + i * GROUP, w);
+        }
     } else {
-        // this lane's vectors hold the last m elements of the lane before and the first 8 - m of its own
+        // a lane's vectors hold the last m elements of the lane before (lane 0: of lane 31's group before) and the first 8 - m of its own
         const int m = row_offset(row), lane = threadIdx.x & 31;
+        uint32_t before[W] = {};
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = __shfl_up_sync(0xffffffffu, own[i], 1);
-        if (m == 0 ? n >= 8 : lane > 0 && n >= 8 - m) {
+        for (int i = 0; i < N; ++i) {
+            const int left = n - i * GROUP;
+            T* at = q + i * GROUP;
+            auto store_some = [&](int from, int to) {         // elements [from, to) that exist, one by one
+                if (from >= min(to, left) || !ROW_STORE_OK(at + from, (min(to, left) - from) * sizeof(T), code)) return;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) if (j >= from && j < to && j < left) at[j] = from_float<T>(f[i][j]);
+            };
+            uint32_t w[W + 4 + W];
+            uint32_t* own = w + W;
+            pack(f[i], own);
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                w[j] = __shfl_sync(0xffffffffu, lane == 31 ? before[j] : own[j], (lane + 31) & 31);
+                before[j] = own[j];
+            }
             if (m == 0) {
+                if (left >= 8) store_vectors(at, own); else store_some(0, 8);
+            } else {
+                if (left >= 8 - m && (i > 0 || lane > 0)) {
+                    if constexpr (sizeof(T) == 4) {
+                        // 8 - m words on: 4, then 4 - m
 #pragma unroll
-                for (int i = 0; i < N; ++i) w[i] = own[i];
-            } else if constexpr (sizeof(T) == 4) {
-                // 8 - m words on: 4, then 4 - m
-#pragma unroll
-                for (int i = 0; i < 2 * N - 4; ++i) w[i] = w[i + 4];
-                shift_words<T, N>(w, 4 - m);
-            } else shift_words<T, N>(w, 8 - m);
-            store_vectors(q - m);
-        } else store_some(0, 8 - m);
-        // the last m elements are the next lane's to store, unless there is none or its vectors are not whole
-        if (m > 0 && (lane == 31 || n - 8 < 8 - m)) store_some(8 - m, 8);
+                        for (int j = 0; j < 2 * W - 4; ++j) w[j] = w[j + 4];
+                        shift_words<T, W>(w, 4 - m);
+                    } else shift_words<T, W>(w, 8 - m);
+                    store_vectors(at - m, w);
+                } else store_some(0, 8 - m);
+                // the last m elements are the next lane's to store, unless there is none or its vectors are not whole
+                if ((i == N - 1 && lane == 31) || left - 8 < 8 - m) store_some(8 - m, 8);
+            }
+        }
     }
 }
 // eight codes; vec: 8-byte aligned
@@ -301,8 +320,7 @@ struct RowsParams {
     Int8Ranges ranges;
 };
 
-// N groups of eight columns, at col, col + step, ...
-template <int AL, int N> __device__ __forceinline__ void checkpoint8(const RowsParams& p, int64_t row, int col, int step, const float (&h)[N][8])
+template <int AL, int N> __device__ __forceinline__ void checkpoint8(const RowsParams& p, int64_t row, int col, const float (&h)[N][8])
 {
     const int shift = p.block == 32 ? 5 : 7, lanes = 1 << (shift - 3), per_row = (p.cols + p.block - 1) >> shift;
     uint32_t m[N];
@@ -314,7 +332,7 @@ template <int AL, int N> __device__ __forceinline__ void checkpoint8(const RowsP
     float* scales = p.checkpoint_scales + row * per_row;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int c = col + i * step, n = AL == 2 ? 8 : p.cols - c;
+        const int c = col + i * GROUP, n = AL == 2 ? 8 : p.cols - c;
         if (n <= 0) continue;
         store_codes8(codes + c, codes8(h[i], s[i].inverse), n, AL == 2 || p.vk, p, 2101);
         if ((c & (p.block - 1)) == 0 && ROW_STORE_OK(scales + (c >> shift), 4, 2102)) scales[c >> shift] = s[i].scale;
@@ -330,23 +348,23 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, !SHORT && AL && sizeof(T) =
     __shared__ double red_sum[32];
     __shared__ float rstd_all;
     __shared__ uint32_t red_max[32];
-    const int t = threadIdx.x, NT = SHORT ? 32 : blockDim.x, step = 8 * NT;
+    const int t = threadIdx.x, warps = SHORT ? 1 : blockDim.x / 32, col = ((t >> 5) * VPT * 32 + (t & 31)) * 8;
     const int64_t row = SHORT ? (int64_t)blockIdx.x * 4 + threadIdx.y : (int64_t)blockIdx.x;
     if (SHORT && row >= p.rows) return;                       // whole warps
-    auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (8 * t + i * step); };
+    auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (col + i * GROUP); };
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const int mx = AL ? 0 : row_offset(x);
     float h[VPT][8];
     Raw8<T, AL> raw[VPT];
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(x, 8 * t + i * step, left(i));
+    for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(x, col + i * GROUP, left(i));
     if constexpr (NORM) {
         if (p.residual) {
             const T* r = static_cast<const T*>(p.residual) + row * p.ldr;
             const int mr = AL ? 0 : row_offset(r);
             Raw8<T, AL> rawr[VPT];
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) rawr[i] = load8<T, AL>(r, 8 * t + i * step, left(i));
+            for (int i = 0; i < VPT; ++i) rawr[i] = load8<T, AL>(r, col + i * GROUP, left(i));
             T* hid = static_cast<T*>(p.hidden) + row * p.ldh;
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
@@ -356,8 +374,7 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, !SHORT && AL && sizeof(T) =
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[i][j] = __fadd_rn(h[i][j], b[j]);
             }
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) store8<T, AL>(hid, 8 * t + i * step, left(i), h[i], p, 2103);
+            store_groups<AL>(hid, col, p.cols - col, h, p, 2103);
         } else {
 #pragma unroll
             for (int i = 0; i < VPT; ++i) unpack8<T, AL>(raw[i], mx, left(i), h[i]);
@@ -369,16 +386,16 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, !SHORT && AL && sizeof(T) =
             for (int j = 0; j < 8; ++j) { const double v = (double)h[i][j]; sum = fma(v, v, sum); }
         if (p.block) {
 #pragma unroll
-            for (int i = 0; i < VPT; i += 2) checkpoint8<AL, 2>(p, row, 8 * t + i * step, step, *reinterpret_cast<const float (*)[2][8]>(&h[i]));
+            for (int i = 0; i < VPT; i += 2) checkpoint8<AL, 2>(p, row, col + i * GROUP, *reinterpret_cast<const float (*)[2][8]>(&h[i]));
         }
         const T* gain = static_cast<const T*>(p.gain);
         const int mg = AL ? 0 : row_offset(gain);
-        const float rstd = row_rstd(sum, red_sum, &rstd_all, NT / 32, p.cols, p.eps);
+        const float rstd = row_rstd(sum, red_sum, &rstd_all, warps, p.cols, p.eps);
         if (t == 0 && p.rstd && ROW_STORE_OK(p.rstd + row, 4, 2104)) p.rstd[row] = rstd;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             float g[8];
-            unpack8<T, AL>(load8<T, AL>(gain, 8 * t + i * step, left(i)), mg, left(i), g);       // (the same for all rows: from L1)
+            unpack8<T, AL>(load8<T, AL>(gain, col + i * GROUP, left(i)), mg, left(i), g);       // (the same for all rows: from L1)
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] = __fmul_rn(__fmul_rn(h[i][j], rstd), g[j]);
         }
@@ -391,10 +408,10 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, !SHORT && AL && sizeof(T) =
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) m = max(m, abs_max8(h[i]));
-    const Scale s = row_scale(row_max(m, red_max, NT / 32), p.pow2);
+    const Scale s = row_scale(row_max(m, red_max, warps), p.pow2);
     int8_t* codes = p.codes + row * p.ldc;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) store_codes8(codes + 8 * t + i * step, codes8(h[i], s.inverse), left(i), AL == 2 || p.vc, p, 2105);
+    for (int i = 0; i < VPT; ++i) store_codes8(codes + col + i * GROUP, codes8(h[i], s.inverse), left(i), AL == 2 || p.vc, p, 2105);
     if (t == 0 && ROW_STORE_OK(p.scales + row, 4, 2106)) p.scales[row] = s.scale;
 }
 
@@ -429,7 +446,7 @@ __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
             hidden8(col, h[0]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) { const double d = (double)h[0][j]; sum = fma(d, d, sum); }
-            if (p.block) checkpoint8<AL>(p, row, col, 0, h);
+            if (p.block) checkpoint8<AL>(p, row, col, h);
         }
         rstd = row_rstd(sum, red_sum, &rstd_all, NT / 32, p.cols, p.eps);
         if (t == 0 && p.rstd && ROW_STORE_OK(p.rstd + row, 4, 2114)) p.rstd[row] = rstd;
@@ -451,11 +468,11 @@ __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
     }
     const Scale s = row_scale(row_max(m, red_max, NT / 32), p.pow2);
     for (int col = 8 * t; col < end; col += 8 * NT) {
-        float h[8];
-        hidden8(col, h);
-        if (r) store8<T, AL>(static_cast<T*>(p.hidden) + row * p.ldh, col, p.cols - col, h, p, 2113);
-        normed8(col, h);
-        store_codes8(p.codes + row * p.ldc + col, codes8(h, s.inverse), p.cols - col, p.vc, p, 2115);
+        float h[1][8];
+        hidden8(col, h[0]);
+        if (r) store_groups<AL>(static_cast<T*>(p.hidden) + row * p.ldh, col, p.cols - col, h, p, 2113);
+        normed8(col, h[0]);
+        store_codes8(p.codes + row * p.ldc + col, codes8(h[0], s.inverse), p.cols - col, p.vc, p, 2115);
     }
     if (t == 0 && ROW_STORE_OK(p.scales + row, 4, 2116)) p.scales[row] = s.scale;
 }
@@ -463,7 +480,7 @@ __global__ void __launch_bounds__(1024) rows_long_kernel(const RowsParams p)
 // ---------------------------------------------------------------------------------------- quantization in blocks, restoring
 // Nothing is summed over a row, so a row is cut into pieces of 1024 columns, a warp to each: four groups of eight columns a thread, 256
 // columns apart, all of them loaded before the first is used.  A block has eight warps, side by side along a row first.
-constexpr int FLAT_VPT = 4, FLAT_STEP = 256, FLAT_PIECE = FLAT_VPT * FLAT_STEP;
+constexpr int FLAT_VPT = 4, FLAT_PIECE = FLAT_VPT * GROUP;
 
 struct BlocksParams {
     const void* x; int8_t* codes; float* scales;
@@ -483,10 +500,10 @@ __global__ void __launch_bounds__(256, 3) quantize_blocks_kernel(const BlocksPar
         const int mx = AL ? 0 : row_offset(x);
         for (int piece = threadIdx.y * FLAT_PIECE; piece < p.cols; piece += blockDim.y * FLAT_PIECE) {
             const int col = piece + 8 * threadIdx.x;
-            auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (col + i * FLAT_STEP); };
+            auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (col + i * GROUP); };
             Raw8<T, AL> raw[VPT];
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(x, col + i * FLAT_STEP, left(i));
+            for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(x, col + i * GROUP, left(i));
             float f[VPT][8];
             uint32_t m[VPT];
             Scale s[VPT];
@@ -499,8 +516,8 @@ __global__ void __launch_bounds__(256, 3) quantize_blocks_kernel(const BlocksPar
             for (int i = 0; i < VPT; ++i) {
                 const int n = left(i);
                 if (n <= 0) continue;
-                store_codes8(codes + i * FLAT_STEP, codes8(f[i], s[i].inverse), n, AL == 2 || p.vc, p, 2121);
-                float* q = scales + (i * FLAT_STEP >> shift);
+                store_codes8(codes + i * GROUP, codes8(f[i], s[i].inverse), n, AL == 2 || p.vc, p, 2121);
+                float* q = scales + (i * GROUP >> shift);
                 if ((col & (p.block - 1)) == 0 && ROW_STORE_OK(q, 4, 2122)) *q = s[i].scale;
             }
         }
@@ -526,23 +543,23 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
         T* x = static_cast<T*>(p.x) + row * p.ldx;
         for (int piece = threadIdx.y * FLAT_PIECE; piece < p.cols; piece += blockDim.y * FLAT_PIECE) {
             const int col = piece + 8 * threadIdx.x;
-            auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (col + i * FLAT_STEP); };
+            auto left = [&](int i) { return AL == 2 ? 8 : p.cols - (col + i * GROUP); };
             uint2 c[VPT];
             float s[VPT];
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int at = col + i * FLAT_STEP;
+                const int at = col + i * GROUP;
                 c[i] = load_codes8(codes + at, left(i), AL == 2 || p.vc);
                 s[i] = left(i) > 0 ? scales[p.block ? at >> shift : 0] : 0.0f;
             }
+            float f[VPT][8];
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                float f[8];
-                codes_to_float(c[i], f);
+                codes_to_float(c[i], f[i]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], s[i]);
-                store8<T, AL>(x, col + i * FLAT_STEP, left(i), f, p, 2131);
+                for (int j = 0; j < 8; ++j) f[i][j] = __fmul_rn(f[i][j], s[i]);
             }
+            store_groups<AL>(x, col, p.cols - col, f, p, 2131);
         }
     }
 }
@@ -581,7 +598,7 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
     __shared__ float red[2][32];
     __shared__ float4 meet[RPC > 1 ? RPC * VPT * 32 * 2 : 1];
     fmmptx::griddep_launch_dependents();
-    const int NT = SHORT ? 32 : blockDim.x, t = threadIdx.x, group = blockIdx.x * RPC + threadIdx.y, groups = gridDim.x * RPC;
+    const int t = threadIdx.x, warps = SHORT ? 1 : blockDim.x / 32, first = ((t >> 5) * VPT * 32 + (t & 31)) * 8, group = blockIdx.x * RPC + threadIdx.y, groups = gridDim.x * RPC;
     const int shift = p.block == 32 ? 5 : 7, per_row = p.block ? (p.cols + p.block - 1) >> shift : 1;
     float sum[VPT][8];
 #pragma unroll
@@ -597,7 +614,7 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
         rstd = p.rstd[row];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int col = 8 * (i * NT + t), n = AL == 2 ? 8 : p.cols - col;
+            const int col = first + i * GROUP, n = AL == 2 ? 8 : p.cols - col;
             dy[i] = load8<T, AL>(static_cast<const T*>(p.dy) + row * p.ldy, col, n);
             codes[i] = load_codes8(p.checkpoint + row * p.ldk + col, n, AL == 2 || p.vk);
             scale[i] = n > 0 ? p.scales[row * per_row + (p.block ? col >> shift : 0)] : 0.0f;
@@ -613,12 +630,12 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
         Raw8<T, AL> add[VPT];
         if (p.dresidual) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); add[i] = load8<T, AL>(dres, col, AL == 2 ? 8 : p.cols - col); }
+            for (int i = 0; i < VPT; ++i) { const int col = first + i * GROUP; add[i] = load8<T, AL>(dres, col, AL == 2 ? 8 : p.cols - col); }
         }
         float out[VPT][8], xh[VPT][8], c = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int col = 8 * (i * NT + t), n = AL == 2 ? 8 : p.cols - col;
+            const int col = first + i * GROUP, n = AL == 2 ? 8 : p.cols - col;
             float g[8];
             unpack8<T, AL>(load8<T, AL>(gain, col, n), mg, n, g);
             unpack8<T, AL>(dy[i], my, n, out[i]);
@@ -631,12 +648,12 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
             }
         }
         if (NEXT && row + groups < p.rows) fetch(row + groups);
-        c = row_sum(c, red[parity], NT / 32) / (float)p.cols;
+        c = row_sum(c, red[parity], warps) / (float)p.cols;
         T* dx = static_cast<T*>(p.dx) + row * p.ldx;
         const int mr = AL ? 0 : row_offset(dres);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int col = 8 * (i * NT + t), n = AL == 2 ? 8 : p.cols - col;
+            const int col = first + i * GROUP, n = AL == 2 ? 8 : p.cols - col;
             float b[8];
             if (p.dresidual) unpack8<T, AL>(add[i], mr, n, b);
 #pragma unroll
@@ -644,8 +661,9 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
                 out[i][j] = rs * (out[i][j] - xh[i][j] * c);
                 if (p.dresidual) out[i][j] += b[j];
             }
-            store8<T, AL>(dx, col, n, out[i], p, 2141);
+            if constexpr (AL != 0) store_groups<AL>(dx, col, n, *reinterpret_cast<const float (*)[1][8]>(&out[i]), p, 2141);
         }
+        if constexpr (AL == 0) store_groups<AL>(dx, first, p.cols - first, out, p, 2141);
     }
     if constexpr (RPC > 1) {
         // the block's groups meet, in their order
@@ -667,8 +685,7 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, SHORT ? 4 : 1) back_kernel(
                 }
     }
     float* q = p.partial + (int64_t)blockIdx.x * p.ldp;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) { const int col = 8 * (i * NT + t); store8<float, AL == 2 ? 2 : 1>(q, col, p.cols - col, sum[i], p, 2142); }
+    store_groups<AL == 2 ? 2 : 1>(q, first, p.cols - first, sum, p, 2142);
 }
 
 // Rows that do not fit registers: dy and the codes are read twice (the second time from L2, mostly), and the sums of a group live in
@@ -697,27 +714,27 @@ __global__ void __launch_bounds__(1024) back_long_kernel(const BackParams p)
         };
         float c = 0.0f;
         for (int col = 8 * t; col < p.cols; col += 8 * NT) {
-            float d[8], xh[8], g[8], s[8];
+            float d[8], xh[8], g[8], s[1][8];
             both8(col, d, xh, g);
             if (row == part) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] = 0.0f;
-            } else unpack8<float, 1>(load8<float, 1>(q, col, p.cols - col), 0, p.cols - col, s);
+                for (int j = 0; j < 8; ++j) s[0][j] = 0.0f;
+            } else unpack8<float, 1>(load8<float, 1>(q, col, p.cols - col), 0, p.cols - col, s[0]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { s[j] = fmaf(d[j], xh[j], s[j]); c = fmaf(d[j] * g[j], xh[j], c); }
-            store8<float, 1>(q, col, p.cols - col, s, p, 2152);
+            for (int j = 0; j < 8; ++j) { s[0][j] = fmaf(d[j], xh[j], s[0][j]); c = fmaf(d[j] * g[j], xh[j], c); }
+            store_groups<1>(q, col, p.cols - col, s, p, 2152);
         }
         c = row_sum(c, red[parity], NT / 32) / (float)p.cols;
         for (int col = 8 * t; col < end; col += 8 * NT) {
-            float d[8], xh[8], g[8], b[8];
+            float d[8], xh[8], g[8], b[8], out[1][8];
             both8(col, d, xh, g);
             if (p.dresidual) number8(p.dresidual, p.ldr, row, col, b);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                d[j] = rs * (d[j] * g[j] - xh[j] * c);
-                if (p.dresidual) d[j] += b[j];
+                out[0][j] = rs * (d[j] * g[j] - xh[j] * c);
+                if (p.dresidual) out[0][j] += b[j];
             }
-            store8<T, AL>(static_cast<T*>(p.dx) + row * p.ldx, col, p.cols - col, d, p, 2151);
+            store_groups<AL>(static_cast<T*>(p.dx) + row * p.ldx, col, p.cols - col, out, p, 2151);
         }
     }
 }
@@ -789,7 +806,9 @@ template <typename T> fmm_status_t launch_back(const BackParams& p, int threads,
         else if (threads) back_kernel<T, AL, false><<<blocks, threads, 0, st>>>(p);
         else back_long_kernel<T, AL ? 1 : 0><<<blocks, 1024, 0, st>>>(p);
     };
-    if (p.aligned && p.vk && p.cols == 8 * BACK_VPT * threads) launch(std::integral_constant<int, 2>{});
+    // (32-bit rows that fill every thread: 16 bytes more than 128 registers hold, and no faster)
+    constexpr int FULL = sizeof(T) == 2 ? 2 : 1;
+    if (p.aligned && p.vk && p.cols == 8 * BACK_VPT * threads) launch(std::integral_constant<int, FULL>{});
     else if (p.aligned) launch(std::integral_constant<int, 1>{});
     else launch(std::integral_constant<int, 0>{});
     if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;

@@ -21,6 +21,7 @@ from __future__ import annotations
 
 import collections
 import ctypes as C
+import struct
 
 import torch
 
@@ -35,7 +36,6 @@ EXPORTS = ["fmm_int8_quantize", "fmm_int8_dequantize", "fmm_int8_rms_norm", "fmm
            "fmm_int8_grad_input_workspace_bytes", "fmm_int8_grad_weight", "fmm_int8_grad_input", "fmm_int8_status", "fmm_int8_status_clear", "fmm_int8_selftest_bounded_wait"]
 
 
-# (argument structures: ctypes takes 0.13 us to hand over an argument and 0.04 us to fill a field)
 class QuantizeArgs(C.Structure):
     """fmm_int8_quantize_t"""
     _fields_ = [("type", C.c_int), ("block", C.c_int), ("scale_mode", C.c_int), ("rows", C.c_int64), ("cols", C.c_int64), ("x", C.c_void_p),
@@ -77,6 +77,18 @@ class RmsNormBackwardArgs(C.Structure):
                 ("gain", C.c_void_p), ("dresidual", C.c_void_p), ("ldr", C.c_int64), ("dx", C.c_void_p), ("ldx", C.c_int64),
                 ("dgain", C.c_void_p)]
 
+
+def _packer(kind):
+    """pack() of the same bytes as kind(*fields): a quarter of the time that filling a ctypes structure takes, and a new object
+    for every call, so that threads do not share one.  Addresses are 0, not None."""
+    code = {C.c_int: "i", C.c_int64: "q", C.c_double: "d", C.c_void_p: "P"}
+    s = struct.Struct("@" + "".join(code[c] for _, c in kind._fields_))
+    assert s.size == C.sizeof(kind)
+    return s.pack
+
+
+_quantize_args, _dequantize_args, _matmul_args = _packer(QuantizeArgs), _packer(DequantizeArgs), _packer(MatmulArgs)
+_grad_args, _norm_args, _back_args = _packer(GradArgs), _packer(RmsNormArgs), _packer(RmsNormBackwardArgs)
 
 _lib = None
 
@@ -171,6 +183,8 @@ def _elsewhere(device, stream):
     return None if device == _current_device() else torch.cuda.device(device)
 
 
+# (torch.cuda.current_stream builds an object; the raw handle is what is needed)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
@@ -222,8 +236,8 @@ def quantize(x, block=0, pow2=False, out=None, stream=None):
         codes, scales = out
         ldc = _matrix(codes, "codes", torch.int8, device, (rows, cols))
         _vector(scales, "scales", torch.float32, device, shape)
-    a = QuantizeArgs(kind, block, POW2 if pow2 else AMAX_DIV_127, rows, cols, x.data_ptr(), ldx, codes.data_ptr(), ldc, scales.data_ptr())
-    _call((_lib or lib()).fmm_int8_quantize(C.byref(a), fmm._stream_ptr(None)), "fmm_int8_quantize")
+    a = _quantize_args(kind, block, POW2 if pow2 else AMAX_DIV_127, rows, cols, x.data_ptr(), ldx, codes.data_ptr(), ldc, scales.data_ptr())
+    _call((_lib or lib()).fmm_int8_quantize(a, _stream(device)), "fmm_int8_quantize")
     return codes, scales
 
 
@@ -242,8 +256,8 @@ def dequantize(codes, scales, block=0, dtype=torch.bfloat16, out=None, stream=No
     else:
         kind = _float_type(out.dtype, "out")
         ldx = _matrix(out, "out", out.dtype, device, (rows, cols))
-    a = DequantizeArgs(kind, block, rows, cols, codes.data_ptr(), ldc, scales.data_ptr(), out.data_ptr(), ldx)
-    _call((_lib or lib()).fmm_int8_dequantize(C.byref(a), fmm._stream_ptr(None)), "fmm_int8_dequantize")
+    a = _dequantize_args(kind, block, rows, cols, codes.data_ptr(), ldc, scales.data_ptr(), out.data_ptr(), ldx)
+    _call((_lib or lib()).fmm_int8_dequantize(a, _stream(device)), "fmm_int8_dequantize")
     return out
 
 
@@ -270,7 +284,7 @@ def rms_norm(x, gain, residual=None, eps=1e-6, pow2=False, checkpoint=0, hidden=
     rows, cols = x.shape
     _vector(gain, "gain", dtype, device, (cols,))
     ldr = ldh = ldk = 0
-    at_residual = at_hidden = at_kept = at_kept_scales = None
+    at_residual = at_hidden = at_kept = at_kept_scales = 0
     if residual is not None:
         ldr = _matrix(residual, "residual", dtype, device, (rows, cols))
         if hidden is None:
@@ -287,9 +301,9 @@ def rms_norm(x, gain, residual=None, eps=1e-6, pow2=False, checkpoint=0, hidden=
         kept = _new_codes(rows, cols, x)
         kept_scales = x.new_empty(_scale_shape(rows, cols, _block(checkpoint, "checkpoint")), dtype=torch.float32)
         at_kept, ldk, at_kept_scales = kept.data_ptr(), kept.stride(0), kept_scales.data_ptr()
-    a = RmsNormArgs(kind, POW2 if pow2 else AMAX_DIV_127, checkpoint, rows, cols, eps, x.data_ptr(), ldx, at_residual, ldr, gain.data_ptr(),
+    a = _norm_args(kind, POW2 if pow2 else AMAX_DIV_127, checkpoint, rows, cols, eps, x.data_ptr(), ldx, at_residual, ldr, gain.data_ptr(),
                     at_hidden, ldh, codes.data_ptr(), codes.stride(0), scales.data_ptr(), rstd.data_ptr(), at_kept, ldk, at_kept_scales)
-    _call((_lib or lib()).fmm_int8_rms_norm(C.byref(a), fmm._stream_ptr(None)), "fmm_int8_rms_norm")
+    _call((_lib or lib()).fmm_int8_rms_norm(a, _stream(device)), "fmm_int8_rms_norm")
     return Norm(x if residual is None else hidden, codes, scales, rstd, kept, kept_scales)
 
 
@@ -309,7 +323,7 @@ def rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block=128, 
     _vector(checkpoint_scales, "checkpoint_scales", torch.float32, device, _scale_shape(rows, cols, _block(block)))
     _vector(rstd, "rstd", torch.float32, device, (rows,))
     _vector(gain, "gain", dtype, device, (cols,))
-    ldr, at_dresidual = 0, None
+    ldr = at_dresidual = 0
     if dresidual is not None:
         ldr, at_dresidual = _matrix(dresidual, "dresidual", dtype, device, (rows, cols)), dresidual.data_ptr()
     if dx is None:
@@ -319,9 +333,9 @@ def rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block=128, 
     dgain = dy.new_empty((cols,), dtype=torch.float32)
     need = _need("fmm_int8_rms_norm_backward_workspace_bytes", (rows, cols), rows, cols)
     workspace = dy.new_empty((need,), dtype=torch.uint8)
-    a = RmsNormBackwardArgs(kind, block, rows, cols, dy.data_ptr(), ldy, checkpoint.data_ptr(), ldk, checkpoint_scales.data_ptr(), rstd.data_ptr(),
+    a = _back_args(kind, block, rows, cols, dy.data_ptr(), ldy, checkpoint.data_ptr(), ldk, checkpoint_scales.data_ptr(), rstd.data_ptr(),
                             gain.data_ptr(), at_dresidual, ldr, dx.data_ptr(), ldx, dgain.data_ptr())
-    _call((_lib or lib()).fmm_int8_rms_norm_backward(C.byref(a), workspace.data_ptr(), need, fmm._stream_ptr(None)), "fmm_int8_rms_norm_backward")
+    _call((_lib or lib()).fmm_int8_rms_norm_backward(a, workspace.data_ptr(), need, _stream(device)), "fmm_int8_rms_norm_backward")
     return dx, dgain
 
 
@@ -357,9 +371,9 @@ def matmul(a, a_scales, b, b_scales, bias=None, dtype=torch.bfloat16, out=None, 
         ldc = _matrix(out, "out", dtype, device, (M, N))
     if bias is not None:
         _vector(bias, "bias", dtype, device, (N,))
-    p = MatmulArgs(kind, M, N, K, at_a, lda, a_scales.data_ptr(), at_b, ldb, b_scales.data_ptr(), None if bias is None else bias.data_ptr(),
+    p = _matmul_args(kind, M, N, K, at_a, lda, a_scales.data_ptr(), at_b, ldb, b_scales.data_ptr(), 0 if bias is None else bias.data_ptr(),
                    out.data_ptr(), ldc)
-    _call((_lib or lib()).fmm_int8_matmul(C.byref(p), fmm._stream_ptr(None)), "fmm_int8_matmul")
+    _call((_lib or lib()).fmm_int8_matmul(p, _stream(device)), "fmm_int8_matmul")
     return out
 
 
@@ -385,11 +399,11 @@ def _grad(what, device, dy, codes, scales, shape, dtype, out, accumulate):
             raise TypeError(f"the gradient is float32 or of dy's type, not {dtype}")
         ldo = _matrix(out, "out", dtype, device, shape)
     at = dy.data_ptr()
-    a = C.byref(GradArgs(_TYPES[kind], _TYPES[dtype], int(accumulate), M, N, K, at, ldy, codes.data_ptr(), ldc, scales.data_ptr(), out.data_ptr(), ldo))
+    a = _grad_args(_TYPES[kind], _TYPES[dtype], int(accumulate), M, N, K, at, ldy, codes.data_ptr(), ldc, scales.data_ptr(), out.data_ptr(), ldo)
     need = _need(what + "_workspace_bytes", (M, N, K, not (at & 15 or ldy & 7)), a)
     workspace = dy.new_empty((need,), dtype=torch.uint8)
     call = (_lib or lib()).fmm_int8_grad_weight if what == "fmm_int8_grad_weight" else (_lib or lib()).fmm_int8_grad_input
-    _call(call(a, workspace.data_ptr(), need, fmm._stream_ptr(None)), what)
+    _call(call(a, workspace.data_ptr(), need, _stream(device)), what)
     return out
 
 
