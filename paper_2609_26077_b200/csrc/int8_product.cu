@@ -6,7 +6,8 @@
 //
 // The tile's rows (TMEM lanes) run along the output's contiguous axis - output channels j of C, input channels k of the gradients - and
 // its columns along the other one, so that 32 lanes store 32 neighbouring elements straight from registers, and a product of
-// few tokens is a tile of few columns: the weight streams through the side with 128 rows whatever the number of tokens.
+// few tokens is a tile of few columns: the weight streams through the side with 128 rows whatever the number of tokens.  (Up to eight
+// tokens take a kernel without tiles.)
 //
 //               rows operand ("R")                  columns operand ("S")
 //   INT8        B (N x K), K-major                  A (M x K), K-major
@@ -759,16 +760,17 @@ fmm_status_t launch_cluster(ProductParams p, const Operand& r, const Operand& s,
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Time models of the two kernels in microseconds (a gradient's with the restoring of its operand), fitted to 3100 timed calls of both with
-// every tile width and number of shares: 1 to 2048 tokens, 512 to 16384 channels, K of 512 to 8192; gradients of 64 to 16384 tokens, 128 to 2048
+// every tile width and number of shares: 16 to 2048 tokens, 512 to 16384 channels, K of 512 to 8192; gradients of 64 to 16384 tokens, 128 to 2048
 // channels each way.  Cluster kernel: lat + rounds * fixed + the stages of an SM, of a single CTA (`stage` each) or of as many as it
-// holds (`shared` each), + what the exchange takes; a share more leaves 2 % more places in the GPCs empty.  Pairs: lat + waves of
-// stages, + what a tile's output costs beyond the next tile's stages.  The choice takes 2.6 % (gradients 0.4 %) more time than
-// the fastest of these in the mean, at worst 1.36 times it (2048 x 512 x 512: 7.8, 5.8 us).
+// holds (`shared` each), + what the exchange takes; a share more leaves 2 % more places in the GPCs empty.  CTAs without an exchange
+// make room one by one, so their rounds are a fraction.  Pairs: lat + waves of stages, + what a tile's output costs beyond the next
+// tile's stages.  The choice takes 1.1 % (gradients 0.1 %) more time than the fastest of these in the mean, at worst 1.31 times it (2048 x
+// 512 x 8192: 22.9, 17.4 us).
 struct ClusterModel { int columns; float lat, stage, shared, fixed; };
 struct ProductModel { float pair_lat, pair_stage, pair_tile, exchange, exchange_share; int per_sm, widths; ClusterModel cluster[4]; };
-constexpr ProductModel MODEL_INT8 = {6.46f, 0.288f, 2.08f, 2.27f, 0.0f, 2, 4,
-    {{16, 1.15f, 0.111f, 0.172f, 1.82f}, {32, 1.65f, 0.208f, 0.190f, 1.84f}, {64, 2.15f, 0.227f, 0.207f, 2.58f}, {128, 3.36f, 0.279f, 0.257f, 3.88f}}};
-constexpr ProductModel MODEL_GRAD = {8.49f, 0.321f, 0.72f, 0.91f, 0.275f, 1, 2, {{64, 2.10f, 0.210f, 0.100f, 3.67f}, {128, 1.61f, 0.263f, 0.232f, 5.02f}}};
+constexpr ProductModel MODEL_INT8 = {6.544f, 0.277f, 2.584f, 2.365f, 0.022f, 2, 4,
+    {{16, 0.937f, 0.216f, 0.199f, 1.682f}, {32, 1.818f, 0.242f, 0.251f, 1.138f}, {64, 2.255f, 0.221f, 0.157f, 2.707f}, {128, 2.161f, 0.282f, 0.458f, 2.846f}}};
+constexpr ProductModel MODEL_GRAD = {5.718f, 0.348f, 0.852f, 0.617f, 0.223f, 1, 2, {{64, 1.203f, 0.175f, 0.222f, 3.804f}, {128, 1.266f, 0.213f, 0.278f, 4.779f}}};
 
 fmm_status_t launch_few_tokens(const ProductParams& p, const Operand& b, const Operand& a, cudaStream_t st)
 {
@@ -795,7 +797,7 @@ ProductChoice choose_product(const ProductModel& m, const ProductParams& p, doub
             float rounds = std::max(1.0f, ctas / places);
             if (shares > 1) rounds = ceilf(rounds);
             const float stages = (float)ceil_div(p.kstages, shares);
-            const float body = std::max(stages * c.stage * rounds, ceilf(ctas / sms) * stages * c.shared);
+            const float held = shares > 1 ? ceilf(ctas / sms) : ctas / sms, body = std::max(stages * c.stage * rounds, held * stages * c.shared);
             const float time = std::max(c.lat + rounds * c.fixed + body + (shares > 1 ? m.exchange + m.exchange_share * shares : 0.0f), 3.0f + by_memory);
             if (time < best) { best = time; choice = {c.columns, shares}; }
         }
