@@ -19,7 +19,8 @@
  *     alignment that their type allows is accepted where nothing else is said (16-byte aligned rows are read and
  *     written fastest).  Nothing is written behind the last column of a row, and nothing read but what shares an
  *     aligned 16-byte vector with an element of the row.
- *   - Rows and columns may be 0: then nothing is read, and what an empty sum gives is written.
+ *   - Rows and columns may be 0: then nothing is read, and what an empty sum gives is written.  They are below
+ *     2^31 - 16384 (FMM_ERR_SHAPE).
  *   - An output may not overlap an input or another output, except where it is said.
  *   - workspace: dev, 256-byte aligned, caller-owned; calls that share one must be stream-ordered.
  */
@@ -111,8 +112,8 @@ fmm_status_t fmm_int8_rms_norm_backward(const fmm_int8_rms_norm_backward_t* p, v
  * the products of codes being exact, the rest in fp32, rounded once to `type`.
  *   a dev, M x K codes (tokens); b dev, N x K codes (a weight, one row per output channel); c dev, M x N; bias dev, N of
  *   `type`, or NULL.  a and b 16-byte aligned, lda and ldb multiples of 16 (FMM_ERR_INVALID_ARG; the codes that
- *   fmm_int8_quantize and fmm_int8_rms_norm write may have any such ld); K <= 131071, so that no sum leaves 32 bits, and
- *   M, N < 2^31 - 512 (FMM_ERR_SHAPE). */
+ *   fmm_int8_quantize and fmm_int8_rms_norm write may have any such ld); K <= 131071, so that no sum leaves 32 bits
+ *   (FMM_ERR_SHAPE). */
 typedef struct {
     fmm_type_t type;
     int64_t M, N, K;
@@ -131,8 +132,8 @@ fmm_status_t fmm_int8_matmul(const fmm_int8_matmul_t* p, void* cuda_stream);
  *     fmm_int8_grad_weight: out[j][k] (+)= sum_i dy[i][j] * (codes[i][k] * scales[i])      codes M x K, out N x K
  *     fmm_int8_grad_input:  out[i][k] (+)= sum_j dy[i][j] * (codes[j][k] * scales[j])      codes N x K, out M x K
  *   out: dev, of out_type, FMM_TYPE_F32 or dy's type; accumulate != 0 adds to what it holds.
- *   M, N, K < 2^31 - 512 (FMM_ERR_SHAPE).  The workspace holds the restored operand and, where its rows are not 16-byte
- *   aligned, a copy of dy; its size is asked for with the same arguments (of which the matrices' own addresses but dy's
+ *   The workspace holds the restored operand and, where its rows are not 16-byte aligned, a copy of dy (FMM_ERR_SHAPE
+ *   where that would be 2^46 bytes or more); its size is asked for with the same arguments (of which the matrices' own addresses but dy's
  *   do not matter). */
 typedef struct {
     fmm_type_t type, out_type;

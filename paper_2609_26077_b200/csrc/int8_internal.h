@@ -41,8 +41,8 @@ __device__ __forceinline__ bool int8_store_ok(const Int8Ranges& r, const void* p
 static inline int int8_type_bytes(fmm_type_t t) { return t == FMM_TYPE_F32 ? 4 : 2; }
 static inline bool int8_type_ok(fmm_type_t t) { return t == FMM_TYPE_F32 || t == FMM_TYPE_BF16 || t == FMM_TYPE_F16; }
 static inline bool int8_aligned(const void* p, int64_t ld_bytes, unsigned a) { return (((uintptr_t)p | (uintptr_t)ld_bytes) & (a - 1)) == 0; }
-// Rows and columns that 32-bit indexes hold with room for a tile behind them
-constexpr int64_t INT8_MAX_DIM = ((int64_t)1 << 31) - 512;
+// Rows and columns that 32-bit indexes hold with room for a step of any kernel behind them
+constexpr int64_t INT8_MAX_DIM = ((int64_t)1 << 31) - 16384;
 
 // SMs of the current device, asked for once per device: the runtime takes 0.7 us for the two calls, a third of a launch
 static inline int int8_sm_count()

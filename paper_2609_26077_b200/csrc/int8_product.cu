@@ -254,6 +254,7 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
         }
     } else if (warp == C::OUT_WARPS + 1) {
         int stage = 0, buf = 0; uint32_t phase = 0, bphase = 0;
+        griddep_wait();                                      // (the limit of the waits counts from here)
         const uint32_t idesc = p.idesc | ((uint32_t)(TC >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
         bool ok = true;
         for (int kc = ks0; kc < ks1 && ok; kc += p.chunk) {
@@ -472,6 +473,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
     } else if (warp == 1) {
         if (leader) {
             int stage = 0, buf = 0; uint32_t phase = 0, bphase = 0;
+            griddep_wait();
             const uint32_t idesc = p.idesc | ((uint32_t)(C::TC >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
             bool ok = true;
             for (long long w = unit; w < tiles && ok; w += units)
@@ -826,6 +828,12 @@ fmm_status_t launch_empty(const ProductParams& p, cudaStream_t st)
     return cudaGetLastError() == cudaSuccess ? FMM_OK : FMM_ERR_CUDA;
 }
 
+// whether a gradient's workspace has a size that can be had at all (and that 64 bits hold)
+bool grad_dims_ok(int64_t M, int64_t N, int64_t K)
+{
+    if (!(M >= 0 && M < INT8_MAX_DIM && N >= 0 && N < INT8_MAX_DIM && K >= 0 && K < INT8_MAX_DIM)) return false;
+    return 2.0 * ((double)std::max(M, N) * (K + 8) + (double)M * (N + 8)) < 0x1p46;
+}
 bool dim_ok(int64_t n) { return n >= 0 && n < INT8_MAX_DIM; }
 int64_t up_to(int64_t n, int64_t a) { return ceil_div(n, a) * a; }
 
@@ -843,7 +851,7 @@ GradWorkspace grad_workspace(int64_t code_rows, int64_t K, int64_t M, int64_t N,
 template <int KIND> fmm_status_t grad_workspace_bytes(const fmm_int8_grad_t* a, size_t* bytes)
 {
     if (!a || !bytes) return FMM_ERR_INVALID_ARG;
-    if (!dim_ok(a->M) || !dim_ok(a->N) || !dim_ok(a->K)) return FMM_ERR_SHAPE;
+    if (!grad_dims_ok(a->M, a->N, a->K)) return FMM_ERR_SHAPE;
     *bytes = grad_workspace(KIND == GRAD_W ? a->M : a->N, a->K, a->M, a->N, int8_aligned(a->dy, a->ldy * 2, 16)).total;
     return FMM_OK;
 }
@@ -858,7 +866,7 @@ fmm_status_t grad(const fmm_int8_grad_t* a, void* workspace, size_t workspace_by
     const void* dY = a->dy;
     const int8_t* codes = a->codes;
     const float* scales = a->scales;
-    if (!dim_ok(M) || !dim_ok(N) || !dim_ok(K)) return FMM_ERR_SHAPE;
+    if (!grad_dims_ok(M, N, K)) return FMM_ERR_SHAPE;
     const int64_t code_rows = KIND == GRAD_W ? M : N, contraction = code_rows, cols = KIND == GRAD_W ? N : M;
     if (K == 0 || cols == 0) return FMM_OK;
     const int eo = int8_type_bytes(out_type);

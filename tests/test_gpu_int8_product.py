@@ -190,6 +190,18 @@ def test_weight_gradient_accumulates(M, N, K, out_type):
     check_grad(d.t() @ v, d.abs().t() @ v.abs(), d.abs().t() @ off, got, M, out_type, old.cuda().double())
 
 
+@pytest.mark.parametrize("out_type", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(70, 130, 200), (2100, 500, 2200)])
+def test_input_gradient_accumulates(M, N, K, out_type):
+    gen = torch.Generator().manual_seed(7)
+    dy = torch.randn(M, N, generator=gen).bfloat16()
+    w, sw = codes_of(N, K, 1), scales_of(N, 1, True)
+    old = torch.randn(M, K, generator=gen).to(out_type)
+    got = int8.grad_input(dy.cuda(), padded(w), torch.from_numpy(sw).cuda(), out=old.cuda(), accumulate=True)
+    d, (v, off) = dy.cuda().double(), restored(w, sw, torch.bfloat16)
+    check_grad(d @ v, d.abs() @ v.abs(), d.abs() @ off, got, N, out_type, old.cuda().double())
+
+
 def test_gradients_of_nothing():
     dy = torch.empty(0, 24, dtype=torch.bfloat16, device="cuda")
     x = torch.empty(0, 40, dtype=torch.int8, device="cuda")

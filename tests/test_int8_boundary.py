@@ -44,7 +44,7 @@ def test_quantize_refusals(lib):
     for bad in (dict(x=None), dict(codes=None), dict(scales=None), dict(type=3), dict(block=64), dict(scale_mode=2), dict(ldx=63), dict(ldc=63),
                 dict(x=P + 2), dict(x=P + 1, type=1), dict(scales=P + 2)):
         assert call(**bad) == INVALID, bad
-    for bad in (dict(rows=-1), dict(cols=-1), dict(rows=1 << 31), dict(cols=1 << 40), dict(rows=(1 << 62) + 1, cols=8)):
+    for bad in (dict(rows=-1), dict(cols=-1), dict(rows=1 << 31), dict(cols=(1 << 31) - 16384, ldx=1 << 31, ldc=1 << 31), dict(cols=1 << 40), dict(rows=(1 << 62) + 1, cols=8)):
         assert call(**bad) == SHAPE, bad
     assert call(rows=0, x=None, codes=None, scales=None) == OK
     assert call(cols=0, block=32, x=None, codes=None, scales=None) == OK
@@ -133,6 +133,10 @@ def test_grad_refusals(lib, which):
     assert call(K=0, out=None) == OK
     assert ask(filled(int8.GradArgs, base, {}), None) == INVALID and ask(None, C.byref(need)) == INVALID
     assert ask(filled(int8.GradArgs, base, dict(K=-1)), C.byref(need)) == SHAPE
+    # sizes whose workspace no 64 bits hold
+    big = dict(M=(1 << 31) - 20000, N=(1 << 31) - 20000, K=(1 << 31) - 20000)
+    big.update(ldy=big["N"], ldc=big["K"], ldo=big["K"])
+    assert ask(filled(int8.GradArgs, base, big), C.byref(need)) == SHAPE and call(**big) == SHAPE
 
 
 def test_binding_wants_cuda_tensors_of_the_right_type():
