@@ -67,7 +67,7 @@ fmm_status_t fmm_int8_dequantize(const fmm_int8_dequantize_t* p, void* cuda_stre
  *   x, residual, gain (cols), hidden: of `type`.  residual == NULL: no addition; hidden is then not written and may be
  *   NULL.  hidden receives h rounded to `type`; it may be the same matrix as x or as residual (same pointer and
  *   distance between rows).  rstd (rows) may be NULL.  checkpoint_block 0: no checkpoint, checkpoint and
- *   checkpoint_scales are not used.  eps finite, >= 0. */
+ *   checkpoint_scales are not used.  eps finite, >= 0.  Of rows without columns nothing is written. */
 typedef struct {
     fmm_type_t type;
     fmm_int8_scale_t scale_mode;

@@ -195,6 +195,11 @@ def _new_codes(rows, cols, like):
     return like.new_empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8)[:, :cols]
 
 
+def _new_like(t):
+    """A dense matrix of t's shape and type (0.5 us less where t is dense itself)."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _call(status, what):
     if status:
         fmm._check(status, what)
@@ -288,7 +293,7 @@ def rms_norm(x, gain, residual=None, eps=1e-6, pow2=False, checkpoint=0, hidden=
     if residual is not None:
         ldr = _matrix(residual, "residual", dtype, device, (rows, cols))
         if hidden is None:
-            hidden, ldh = x.new_empty((rows, cols)), cols
+            hidden, ldh = _new_like(x), cols
         else:
             ldh = _matrix(hidden, "hidden", dtype, device, (rows, cols))
         at_residual, at_hidden = residual.data_ptr(), hidden.data_ptr()
@@ -327,7 +332,7 @@ def rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block=128, 
     if dresidual is not None:
         ldr, at_dresidual = _matrix(dresidual, "dresidual", dtype, device, (rows, cols)), dresidual.data_ptr()
     if dx is None:
-        dx, ldx = dy.new_empty((rows, cols)), cols
+        dx, ldx = _new_like(dy), cols
     else:
         ldx = _matrix(dx, "dx", dtype, device, (rows, cols))
     dgain = dy.new_empty((cols,), dtype=torch.float32)
