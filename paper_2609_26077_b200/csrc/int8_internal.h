@@ -73,3 +73,5 @@ template <> __device__ __forceinline__ uint32_t pack_two<__half>(float a, float 
 
 // int8_rows.cu: the status word of its store checks (FMM_DEBUG build; 0 otherwise)
 fmm_status_t int8_rows_guard_read(int* code, bool clear);
+// 16-bit rows copied to rows on 16-byte boundaries, ldy a multiple of 8
+fmm_status_t int8_realign(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int64_t cols, cudaStream_t st);

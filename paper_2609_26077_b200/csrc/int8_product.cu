@@ -684,13 +684,6 @@ __global__ void __launch_bounds__(256) empty_sum_kernel(const ProductParams p)
     }
 }
 
-// 16-bit rows of any alignment, copied to rows that a tensor map can read
-__global__ void __launch_bounds__(256) realign_kernel(const uint16_t* x, long long ldx, uint16_t* y, long long ldy, int rows, int cols)
-{
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x)
-        for (int c = threadIdx.x; c < cols; c += 256) y[row * ldy + c] = x[row * ldx + c];
-}
-
 // ------------------------------------------------------------------------------------------------ host side
 struct Operand { const void* p; int64_t rows, cols, ld; };        // row-major, cols contiguous; ld in elements
 
@@ -886,9 +879,9 @@ fmm_status_t grad(const fmm_int8_grad_t* a, void* workspace, size_t workspace_by
     if (s != FMM_OK) return s;
     Operand dy = {dY, M, N, ldy};
     if (!dy_aligned) {
-        uint16_t* copy = reinterpret_cast<uint16_t*>(static_cast<char*>(workspace) + w.dy);
-        realign_kernel<<<(unsigned)std::min<int64_t>(M, (int64_t)int8_sm_count() * 8), 256, 0, st>>>(static_cast<const uint16_t*>(dY), ldy, copy, w.ld_dy, (int)M, (int)N);
-        if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;
+        void* copy = static_cast<char*>(workspace) + w.dy;
+        s = int8_realign(dY, ldy, copy, w.ld_dy, M, N, st);
+        if (s != FMM_OK) return s;
         dy = {copy, M, N, w.ld_dy};
     }
     p.behind = 1;
