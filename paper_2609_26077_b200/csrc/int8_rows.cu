@@ -8,6 +8,7 @@
 #include <type_traits>
 #include "fmm_ptx.cuh"
 #include "int8_internal.h"
+#include "int8_shapes.h"
 
 namespace {
 
@@ -415,6 +416,13 @@ __global__ void __launch_bounds__(SHORT ? 128 : 512, !SHORT && AL && sizeof(T) =
     if (t == 0 && ROW_STORE_OK(p.scales + row, 4, 2106)) p.scales[row] = s.scale;
 }
 
+// Rows without columns: the scale of nothing, 1e-12 / 127 or the power of two above it
+__global__ void __launch_bounds__(256) no_columns_kernel(const RowsParams p)
+{
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (row < p.rows && ROW_STORE_OK(p.scales + row, 4, 2107)) p.scales[row] = block_scale(0u, p.pow2).scale;
+}
+
 // Rows that do not fit registers: read again for each pass (from L2, mostly).  hidden may be x or residual, so it is written in the
 // last pass.  Every lane goes round as often, as lanes exchange numbers.
 template <typename T, bool NORM, int AL>
@@ -798,10 +806,9 @@ template <typename T, bool NORM> fmm_status_t launch_rows(const RowsParams& p, c
 {
     const int groups = (p.cols + 7) / 8;
     const unsigned rows = (unsigned)p.rows;
-    // Two groups of eight columns a thread up to 512 columns, four up to 16384; a warp a row up to 1024.  (Two groups a thread up to 4096
-    // columns: 16384 x 4096 bf16 in 98.5 instead of 74.3 us, 8192 x 2048 in 25.2 instead of 21.7.)
-    const int vpt = groups <= 64 ? 2 : 4, threads = (groups + 32 * vpt - 1) / (32 * vpt) * 32;
-    const bool full = p.aligned && groups == vpt * threads && p.vc && (!p.block || p.vk);
+    const Int8RowForm form = int8_row_form(p.cols);
+    const int threads = form.threads;
+    const bool full = p.aligned && form.whole && p.vc && (!p.block || p.vk);
     auto launch = [&](auto al) {
         constexpr int AL = decltype(al)::value;
         if (groups <= 64) rows_kernel<T, NORM, AL, 2, true><<<(rows + 3) / 4, dim3(32, 4), 0, st>>>(p);
@@ -938,6 +945,10 @@ fmm_status_t fmm_int8_quantize(const fmm_int8_quantize_t* a, void* stream)
     RowsParams p = {};
     p.x = X; p.ldx = ldx; p.codes = codes; p.ldc = ldc; p.scales = scales;
     p.rows = (int)rows; p.cols = (int)cols; p.pow2 = pow2; p.aligned = vx; p.vc = vc; p.ranges = ranges;
+    if (cols == 0) {
+        no_columns_kernel<<<(unsigned)((rows + 255) / 256), 256, 0, st>>>(p);
+        return launched();
+    }
     if (type == FMM_TYPE_F32) return launch_rows<float, false>(p, st);
     if (type == FMM_TYPE_BF16) return launch_rows<__nv_bfloat16, false>(p, st);
     return launch_rows<__half, false>(p, st);

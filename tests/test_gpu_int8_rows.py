@@ -109,6 +109,27 @@ def test_empty_matrices():
     assert dx.shape == (0, 64) and not dgain.any()
 
 
+@pytest.mark.parametrize("pow2", [False, True])
+@pytest.mark.parametrize("dtype", O.TYPES)
+def test_rows_without_columns_touch_nothing(dtype, pow2):
+    """Views of no columns in aligned buffers whose rows are 64 and 512 elements apart: the scales of nothing, the buffers as they were."""
+    for ld in (64, 512):
+        x, codes = torch.full((5, ld), float("nan"), dtype=dtype, device="cuda"), torch.full((5, ld), 77, dtype=torch.int8, device="cuda")
+        scales = torch.full((7,), -1.0, device="cuda")
+        want = O.quantize(np.zeros((5, 1), np.float32), 0, pow2)[1]          # a row of zeros has the same scale
+        got = int8.quantize(x[:, :0], pow2=pow2, out=(codes[:, :0], scales[:5]))
+        assert got[0].shape == (5, 0)
+        assert np.array_equal(O.host(scales[:5]), want) and (scales[5:] == -1).all()
+        assert (codes == 77).all() and torch.isnan(x).all()
+        # by addresses, as a C caller has them: present, and absent
+        for at_x, at_codes in ((x.data_ptr(), codes.data_ptr()), (0, 0)):
+            a = int8._quantize_args(int8._TYPES[dtype], 0, int8.POW2 if pow2 else int8.AMAX_DIV_127, 5, 0, at_x, 0, at_codes, 0, scales.data_ptr())
+            scales.fill_(-1.0)
+            assert int8.lib().fmm_int8_quantize(a, torch.cuda.current_stream().cuda_stream) == 0
+            assert np.array_equal(O.host(scales[:5]), want) and (scales[5:] == -1).all()
+            assert (codes == 77).all()
+
+
 # ------------------------------------------------------------------------------------------------ norm
 def norm_case(rows, cols, dtype, seed, residual=True):
     g = torch.Generator().manual_seed(1000 + seed)
