@@ -390,7 +390,8 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
 template <int KIND>
 struct PairCfg {
     static constexpr int TC = 256, R_BYTES = 128 * 128, S_BYTES = 128 * 128, STAGE_BYTES = R_BYTES + S_BYTES, STAGES = 6;
-    static constexpr int OFF_SCALES = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALES + 2 * TC * 4, NUM_BARS = 2 * STAGES + 4;
+    // (scales: every output warp has its own copy of its columns')
+    static constexpr int OFF_SCALES = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALES + 8 * (TC / 2) * 4, NUM_BARS = 2 * STAGES + 4;
     static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;
     // warp 0 TMA producer, warp 1 MMA issuer, warps 4..11 output: a TMEM lane quadrant and half of the columns each, the gradients' sums
     // in registers
@@ -515,13 +516,12 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
             const int row = (2 * tr + rank) * 128 + quadrant * 32 + lane, col0 = tc * C::TC + half * COLS;
             const int valid = min(COLS, p.cols - col0);
             if constexpr (KIND == INT8) {
-                // (a warp is at most one tile behind the others, and the scales of two tiles are kept)
-                const uint32_t tile_scales = base + C::OFF_SCALES + buf * C::TC * 4, scales = tile_scales + half * COLS * 4;
-                for (int i = threadIdx.x - C::OUT_WARP0 * 32; i < C::TC; i += C::OUT_WARPS * 32) {
-                    const int col = tc * C::TC + i;
-                    sts32u(tile_scales + 4 * i, col < p.cols ? __float_as_uint(p.c_scales[col]) : 0u);
-                }
-                asm volatile("bar.sync 1, %0;" ::"n"(C::OUT_WARPS * 32) : "memory");
+                // (No warp waits here for another: one whose wait below has run out leaves the loop, and a barrier among the output
+                // warps would then have no limit for those whose wait has not.)
+                const uint32_t scales = base + C::OFF_SCALES + (warp - C::OUT_WARP0) * COLS * 4;
+                __syncwarp();                                // the tile before is out
+                for (int i = lane; i < COLS; i += 32) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
+                __syncwarp();
                 float r_scale = 0.0f, bias = 0.0f;
                 if (row < p.rows) { r_scale = p.r_scales[row]; bias = load_bias(p, row); }
                 if (!mbar_wait_warp(bar_tfull(buf), bphase, ctl, 2314)) break;

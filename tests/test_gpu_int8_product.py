@@ -59,6 +59,11 @@ def test_matmul(M, N, K):
     check_matmul(M, N, K, bias=(M + N) % 2 == 0, seed=M + N)
 
 
+def test_matmul_of_many_tiles_a_pair():
+    """17 x 17 tiles of 256 x 256 among 74 pairs: both accumulators, every tile with the scales of its own columns."""
+    check_matmul(4100, 4100, 2050, bias=True, seed=3)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("M,N,K", [(1, 300, 512), (50, 70, 90), (200, 333, 1024), (2300, 2100, 256)])
 def test_matmul_types(M, N, K, dtype):
