@@ -11,21 +11,32 @@
 //
 //               rows operand ("R")                  columns operand ("S")
 //   INT8        B (N x K), K-major                  A (M x K), K-major
-//   GRAD_W      X restored (M x K), row-major       dY (M x N), row-major     contraction over the rows of both
-//   GRAD_X      W restored (N x K), row-major       dY (M x N), K-major
+//   GRAD_W      values of X (M x K), row-major      dY (M x N), row-major     contraction over the rows of both
+//   GRAD_X      values of W (N x K), row-major      dY (M x N), K-major
 //
 // An operand whose contraction runs over its rows is loaded as it lies, in boxes of 64 rows x 128 bytes, and handed to the tensor
 // cores as MN-major; nothing is transposed in memory.  One pipeline stage is 128 bytes of contraction on both sides (128 codes, 64
 // 16-bit numbers), four MMAs.
+//
+// What a gradient multiplies is in the workspace in 16 bits, but not rounded to them where the output can show it:
+//   - The values code * scale, fp32 numbers, are taken apart into 16-bit parts that are multiplied one after the other: three of
+//     bf16 (nothing is lost) or two of fp16 (2^-22) for an fp32 output, two for a 16-bit one (bf16: 2^-16).  Where the scales of all 64
+//     rows of a stage are powers of two the first part is the value, and the others are left out: such a product takes a third or half of the
+//     others' MMAs (weight gradient in fp32, 8192 cubed: 781 and 2170 us).  fp16 parts carry a power of two that keeps them in range,
+//     which the output takes out again.
+//   - The input gradient of a bf16 dY with a 16-bit output contracts over the scales of W, so that these can go to dY instead: the product of
+//     the codes, exact in fp16, and of dY * scale, which fp16 holds to 2^-12 of a number, or 2^-39 of its row's largest.  An eighth of the
+//     output's own rounding, in one pass (8192 cubed: 800 us, 1514 with two parts, 759 with values rounded to bf16).
+//   - A caller who wants one pass in any case gets values rounded once to dY's type (`rounded`).
 //
 // The tensor cores add in fp32 by cutting off what does not fit, so the sums of a gradient drift towards zero as the contraction
 // grows: 2.4e-6 of their size over 8192 terms, 6e-6 over 16384.  Where the output is fp32 they are therefore taken out of the
 // accumulator every CHUNK stages (1024 terms) and added up in registers, rounded to nearest: 1.9e-7 for both.  An output of 16 bits has no
 // use for that.
 //
-// The 8-bit operand of a gradient is restored to 16 bits by fmm_int8_dequantize into the workspace before the product: 3 bytes a code
-// once, against 2 M N K operations.  Restoring it tile by tile on the way into the tensor cores would take two more passes
-// through shared memory per tile (codes in, 16-bit values out), which the product's own operand traffic already fills.
+// The 8-bit operand is taken to 16 bits in the workspace before the product: 3 bytes a code and part once, against 2 M N K operations.  Doing
+// so tile by tile on the way into the tensor cores would take two more passes through shared memory per tile (codes in, 16-bit values
+// out), which the product's own operand traffic already fills where the product is large.
 #include <math.h>
 #include <algorithm>
 #include "fmm_gemm_common.cuh"
@@ -78,7 +89,9 @@ struct ProductParams {
     int k_shares;                   // cluster kernel
     int chunk;                      // gradients: stages after which the sums leave the tensor cores' accumulator (see below)
     uint32_t idesc;                 // without the tile's dimensions
-    const float* r_scales; const float* c_scales; const void* bias;      // INT8
+    const float* r_scales; const float* c_scales; const void* bias;      // INT8; c_scales: gradients too, or null
+    const uint8_t* flags; int parts;                // gradients: which stages have `parts` parts (of int8_values; null: none), the others one
+    const uint32_t* maxima; int maxima_count;       // fp16 parts: of matrix_exponent, or null
     void* out; long long ldo;
     int out_type, accumulate;
     int behind;                     // launched behind a kernel of the same call: may be set up while that one drains
@@ -101,6 +114,63 @@ __device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* tm
         for (int b = 0; b < N / 64; ++b) tma_load_2d<NCTA>(dst + b * MN_BOX, tm, first + 64 * b, ks * ELEMENTS, bar);
     } else tma_load_2d<NCTA>(dst, tm, ks * ELEMENTS, first, bar);
 }
+// the rows operand: codes, or a part of a gradient's values
+template <int KIND, int NCTA>
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* tm, int first, int ks, int part, uint32_t bar)
+{
+    if constexpr (KIND == INT8) load_operand<false, STAGE_ELEMENTS<KIND>, 128, NCTA>(dst, tm, first, ks, bar);
+    else {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) tma_load_3d<NCTA>(dst + b * MN_BOX, tm, first + 64 * b, ks * STAGE_ELEMENTS<KIND>, part, bar);
+    }
+}
+// Which parts the stages of a walk along the contraction have.  The warp that loads them goes stage by stage; the flags are read 32 at a
+// time, a window ahead.  Warp-collective.
+template <int KIND> struct StageParts {
+    static_assert(KIND == INT8 || STAGE_ELEMENTS<KIND> == INT8_PART_ROWS, "values_kernel goes by the same stages");
+    const ProductParams& p;
+    int window = -1;
+    uint32_t mask = 0, next = 0;
+    // the first stage of the walk
+    __device__ __forceinline__ void begin(int ks) { if (KIND != INT8 && p.flags) fetch(ks >> 5); }
+    __device__ __forceinline__ void fetch(int w)
+    {
+        const int ks = 32 * w + (threadIdx.x & 31);
+        next = ks < p.kstages ? p.flags[ks] : 0u;
+    }
+    // parts of stage ks; stages are asked for in order, the first one again behind the last
+    __device__ __forceinline__ int of(int ks)
+    {
+        if (KIND == INT8 || !p.flags) return 1;
+        if (ks >> 5 != window) {
+            window = ks >> 5;
+            mask = warp_uniform(__ballot_sync(0xffffffffu, next));
+            fetch(32 * (window + 1) < p.kstages ? window + 1 : 0);
+        }
+        return mask >> (ks & 31) & 1 ? p.parts : 1;
+    }
+};
+// The warp that multiplies them need not tell parts apart: it is told how many pipeline stages a chunk of the walk has, and counts the next
+// chunk's while this one's are on their way.  (With the parts in its loop it issues the MMAs more slowly, whatever their number: 8192 cubed in
+// 856 instead of 764 us.)  Warp-collective.
+template <int KIND> struct ChunkStages {
+    const ProductParams& p;
+    uint32_t inexact = 0;
+    __device__ __forceinline__ void look(int from, int to)
+    {
+        if (KIND == INT8 || !p.flags) return;
+        inexact = 0;
+        for (int ks = from + (threadIdx.x & 31); ks < to; ks += 32) inexact += p.flags[ks];
+    }
+    // of the chunk that was looked at last
+    __device__ __forceinline__ int count(int stages)
+    {
+        if (KIND == INT8 || !p.flags) return stages;
+        return (int)warp_uniform(stages + (p.parts - 1) * __reduce_add_sync(0xffffffffu, inexact));
+    }
+};
+// what the sums of fp16 parts are multiplied by
+__device__ __forceinline__ float part_inverse(const ProductParams& p) { return p.maxima ? power_of_two(-matrix_exponent(p.maxima, p.maxima_count)) : 1.0f; }
 // the four MMAs of a stage
 template <int KIND, int NCTA>
 __device__ __forceinline__ void mma_stage(uint32_t d, uint32_t r_addr, uint32_t s_addr, uint32_t idesc, bool first)
@@ -133,14 +203,14 @@ __device__ __forceinline__ float load_bias(const ProductParams& p, int row)
     return to_float(static_cast<const __half*>(p.bias)[row]);
 }
 // N columns from col0 of one row of the output, from a thread's registers, `valid` of which exist.  c_scale: shared address of column
-// col0's scale.  All of them are computed before the first is stored, and whole groups without a test in between: with one the
+// col0's scale (gradients: if there are any; r_scale: their sums' factor, a power of two).  All of them are computed before the first is stored, and whole groups without a test in between: with one the
 // columns came one after the other, 75 cycles each (4096 x 4096 x 128: 47.6 us a call, 19.4 without).
 template <int KIND, int N>
 __device__ __forceinline__ void put_columns(const ProductParams& p, const uint32_t (&v)[N], int row, int col0, int valid, float r_scale, float bias, uint32_t c_scale)
 {
     if (row >= p.rows) return;
     float x[N];
-    if constexpr (KIND == INT8) {
+    if (KIND == INT8 || p.c_scales) {
         float s[N];
         if constexpr (N % 4 == 0) {
 #pragma unroll
@@ -150,10 +220,10 @@ __device__ __forceinline__ void put_columns(const ProductParams& p, const uint32
             for (int j = 0; j < N; ++j) s[j] = lds32f(c_scale + 4 * j);
         }
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = scaled(v[j], r_scale, s[j]) + bias;
+        for (int j = 0; j < N; ++j) x[j] = KIND == INT8 ? scaled(v[j], r_scale, s[j]) + bias : __uint_as_float(v[j]) * s[j];
     } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = __uint_as_float(v[j]);
+        for (int j = 0; j < N; ++j) x[j] = __uint_as_float(v[j]) * r_scale;
     }
     auto each = [&](auto type) {
         using T = decltype(type);
@@ -241,31 +311,39 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
 
     if (warp == C::OUT_WARPS) {
         int stage = 0; uint32_t phase = 0;
+        StageParts<KIND> stage_parts{p};
+        bool ok = true;
         griddep_wait();
-        for (int ks = ks0; ks < ks1; ++ks) {
-            if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2301)) break;
-            if (elect_one()) {
-                const uint32_t s = base + stage * C::STAGE_BYTES;
-                mbar_expect_tx(bar_full(stage), C::STAGE_BYTES);
-                load_operand<R_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 1>(s, &tmR, row0, ks, bar_full(stage));
-                load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, TC, 1>(s + C::R_BYTES, &tmS, col0, ks, bar_full(stage));
+        stage_parts.begin(ks0);
+        for (int ks = ks0; ks < ks1 && ok; ++ks) {
+            for (int part = 0; part == 0 || part < stage_parts.of(ks); ++part) {
+                if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2301)) { ok = false; break; }
+                if (elect_one()) {
+                    const uint32_t s = base + stage * C::STAGE_BYTES;
+                    mbar_expect_tx(bar_full(stage), C::STAGE_BYTES);
+                    load_rows<KIND, 1>(s, &tmR, row0, ks, part, bar_full(stage));
+                    load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, TC, 1>(s + C::R_BYTES, &tmS, col0, ks, bar_full(stage));
+                }
+                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
             }
-            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
         }
     } else if (warp == C::OUT_WARPS + 1) {
         int stage = 0, buf = 0; uint32_t phase = 0, bphase = 0;
         griddep_wait();                                      // (the limit of the waits counts from here)
         const uint32_t idesc = p.idesc | ((uint32_t)(TC >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
         bool ok = true;
+        ChunkStages<KIND> chunk{p};
+        chunk.look(ks0, min(ks0 + p.chunk, ks1));
         for (int kc = ks0; kc < ks1 && ok; kc += p.chunk) {
             if (!mbar_wait_warp(bar_tempty(buf), bphase ^ 1u, ctl, 2304)) break;
             tc_fence_after();
-            const int end = min(kc + p.chunk, ks1);
-            for (int ks = kc; ks < end; ++ks) {
+            const int end = min(kc + p.chunk, ks1), stages = chunk.count(end - kc);
+            chunk.look(end, min(end + p.chunk, ks1));
+            for (int i = 0; i < stages; ++i) {
                 if (!mbar_wait_warp(bar_full(stage), phase, ctl, 2302)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t s = base + stage * C::STAGE_BYTES;
-                mma_stage<KIND, 1>(tmem_base + buf * TC, s, s + C::R_BYTES, idesc, ks == kc);
+                mma_stage<KIND, 1>(tmem_base + buf * TC, s, s + C::R_BYTES, idesc, i == 0);
                 tc_commit<1>(bar_empty(stage));
                 if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
             }
@@ -275,9 +353,9 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
     } else {
         griddep_wait();
         const uint32_t scales = base + C::OFF_SCALES;
-        if constexpr (KIND == INT8) {
-            for (int i = threadIdx.x; i < TC; i += 128) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (KIND == INT8 || p.c_scales) {
+            for (int i = threadIdx.x; i < TC; i += C::OUT_WARPS * 32) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
+            asm volatile("bar.sync 1, %0;" ::"n"(C::OUT_WARPS * 32) : "memory");
         }
         constexpr int CH = TC < 32 ? TC : 32, COLS = TC * 4 / C::OUT_WARPS;      // columns of a warp
         const int quadrant = warp & 3, first = (warp >> 2) * COLS;
@@ -306,6 +384,7 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
             }
         } else {
             float sum[COLS / CH][CH];
+            const float inverse = part_inverse(p);
             int buf = 0; uint32_t bphase = 0;
             bool ok = true;
             for (int kc = ks0; kc < ks1; kc += p.chunk) {
@@ -332,7 +411,7 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
                 uint32_t v[CH];
 #pragma unroll
                 for (int j = 0; j < CH; ++j) v[j] = __float_as_uint(sum[i][j]);
-                if (ok && first + i * CH < valid) put(v, first + i * CH, 0.0f, 0.0f);
+                if (ok && first + i * CH < valid) put(v, first + i * CH, inverse, 0.0f);
             }
         }
     }
@@ -345,7 +424,7 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
             if constexpr (KIND == INT8) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) if (row + i < p.rows) { r_scale[i] = p.r_scales[row + i]; bias[i] = load_bias(p, row + i); }
-            }
+            } else r_scale[0] = r_scale[1] = r_scale[2] = r_scale[3] = part_inverse(p);
             // the tile's columns are dealt out to the cluster's output warps
             for (int c = rank * C::OUT_WARPS + warp; c < valid; c += C::OUT_WARPS * shares) {
                 uint4 x[8];
@@ -454,21 +533,25 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
     if (warp == 0) {
         int stage = 0; uint32_t phase = 0;
         bool ok = true;
+        StageParts<KIND> stage_parts{p};
         griddep_wait();
+        stage_parts.begin(0);
         for (long long w = unit; w < tiles && ok; w += units) {
             int tr, tc;
             place(w, tr, tc);
-            for (int ks = 0; ks < p.kstages; ++ks) {
-                if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2311)) { ok = false; break; }
-                // completion is counted on the even CTA's barrier; only that CTA arms it
-                const uint32_t fb = bar_full(stage) & PEER_BIT_MASK;
-                if (elect_one()) {
-                    const uint32_t s = base + stage * C::STAGE_BYTES;
-                    if (leader) mbar_expect_tx(bar_full(stage), 2 * C::STAGE_BYTES);
-                    load_operand<R_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 2>(s, &tmR, (2 * tr + rank) * 128, ks, fb);
-                    load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 2>(s + C::R_BYTES, &tmS, (2 * tc + rank) * 128, ks, fb);
+            for (int ks = 0; ks < p.kstages && ok; ++ks) {
+                for (int part = 0; part == 0 || part < stage_parts.of(ks); ++part) {
+                    if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2311)) { ok = false; break; }
+                    // completion is counted on the even CTA's barrier; only that CTA arms it
+                    const uint32_t fb = bar_full(stage) & PEER_BIT_MASK;
+                    if (elect_one()) {
+                        const uint32_t s = base + stage * C::STAGE_BYTES;
+                        if (leader) mbar_expect_tx(bar_full(stage), 2 * C::STAGE_BYTES);
+                        load_rows<KIND, 2>(s, &tmR, (2 * tr + rank) * 128, ks, part, fb);
+                        load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 2>(s + C::R_BYTES, &tmS, (2 * tc + rank) * 128, ks, fb);
+                    }
+                    if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
                 }
-                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
             }
         }
     } else if (warp == 1) {
@@ -477,16 +560,19 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
             griddep_wait();
             const uint32_t idesc = p.idesc | ((uint32_t)(C::TC >> 3) << 17) | ((uint32_t)(256 >> 4) << 24);
             bool ok = true;
+            ChunkStages<KIND> chunk{p};
+            chunk.look(0, min(p.chunk, p.kstages));
             for (long long w = unit; w < tiles && ok; w += units)
                 for (int kc = 0; kc < p.kstages && ok; kc += p.chunk) {
                     if (!mbar_wait_warp(bar_tempty(buf), bphase ^ 1u, ctl, 2312)) { ok = false; break; }
                     tc_fence_after();
-                    const int end = min(kc + p.chunk, p.kstages);
-                    for (int ks = kc; ks < end; ++ks) {
+                    const int end = min(kc + p.chunk, p.kstages), stages = chunk.count(end - kc), from = end < p.kstages ? end : 0;
+                    chunk.look(from, min(from + p.chunk, p.kstages));
+                    for (int i = 0; i < stages; ++i) {
                         if (!mbar_wait_warp(bar_full(stage), phase, ctl, 2313)) { ok = false; break; }
                         tc_fence_after();
                         const uint32_t s = base + stage * C::STAGE_BYTES;
-                        mma_stage<KIND, 2>(tmem_base + buf * C::TC, s, s + C::R_BYTES, idesc, ks == kc);
+                        mma_stage<KIND, 2>(tmem_base + buf * C::TC, s, s + C::R_BYTES, idesc, i == 0);
                         tc_commit<2>(bar_empty(stage));
                         if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
                     }
@@ -504,6 +590,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
         int buf = 0; uint32_t bphase = 0;
         bool ok = true;
         griddep_wait();
+        const float inverse = KIND == INT8 ? 1.0f : part_inverse(p);
         auto release = [&] {
             tc_fence_before();
             __syncwarp();
@@ -515,13 +602,15 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
             place(w, tr, tc);
             const int row = (2 * tr + rank) * 128 + quadrant * 32 + lane, col0 = tc * C::TC + half * COLS;
             const int valid = min(COLS, p.cols - col0);
-            if constexpr (KIND == INT8) {
+            const uint32_t scales = base + C::OFF_SCALES + (warp - C::OUT_WARP0) * COLS * 4;
+            if (KIND == INT8 || p.c_scales) {
                 // (No warp waits here for another: one whose wait below has run out leaves the loop, and a barrier among the output
                 // warps would then have no limit for those whose wait has not.)
-                const uint32_t scales = base + C::OFF_SCALES + (warp - C::OUT_WARP0) * COLS * 4;
                 __syncwarp();                                // the tile before is out
                 for (int i = lane; i < COLS; i += 32) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
                 __syncwarp();
+            }
+            if constexpr (KIND == INT8) {
                 float r_scale = 0.0f, bias = 0.0f;
                 if (row < p.rows) { r_scale = p.r_scales[row]; bias = load_bias(p, row); }
                 if (!mbar_wait_warp(bar_tfull(buf), bphase, ctl, 2314)) break;
@@ -558,7 +647,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
                     uint32_t v[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(sum[i][j]);
-                    if (32 * i < valid) put_columns<KIND, 32>(p, v, row, col0 + 32 * i, valid - 32 * i, 0.0f, 0.0f, 0);
+                    if (32 * i < valid) put_columns<KIND, 32>(p, v, row, col0 + 32 * i, valid - 32 * i, inverse, 0.0f, scales + 128 * i);
                 }
             }
         }
@@ -685,7 +774,7 @@ __global__ void __launch_bounds__(256) empty_sum_kernel(const ProductParams p)
 }
 
 // ------------------------------------------------------------------------------------------------ host side
-struct Operand { const void* p; int64_t rows, cols, ld; };        // row-major, cols contiguous; ld in elements
+struct Operand { const void* p; int64_t rows, cols, ld, parts = 1, step = 0; };        // row-major, cols contiguous; ld and step in elements
 
 template <int KIND, bool MN>
 bool make_operand_map(CUtensorMap* tm, const Operand& o, int n)
@@ -693,6 +782,18 @@ bool make_operand_map(CUtensorMap* tm, const Operand& o, int n)
     const CUtensorMapDataType dt = KIND == INT8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
     const int e = KIND == INT8 ? 1 : 2;
     return make_map_2d(tm, dt, e, o.p, (uint64_t)o.cols, (uint64_t)o.rows, MN ? 64 : 128 / e, MN ? 64 : n, CU_TENSOR_MAP_SWIZZLE_128B, (uint64_t)o.ld);
+}
+
+// the rows operand: codes, or the parts of a gradient's values
+template <int KIND> bool make_rows_map(CUtensorMap* tm, const Operand& o)
+{
+    if constexpr (KIND == INT8) return make_operand_map<KIND, false>(tm, o, 128);
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.parts}, strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)o.step * 2};
+    const cuuint32_t box[3] = {64, 64, 1}, steps[3] = {1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, const_cast<void*>(o.p), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The kernel's shared memory limit, raised once per device.
@@ -730,7 +831,7 @@ fmm_status_t launch_pair(ProductParams p, const Operand& r, const Operand& s, cu
     using C = PairCfg<KIND>;
     static std::atomic<bool> done[64];
     CUtensorMap tmR, tmS;
-    if (!make_operand_map<KIND, R_MN<KIND>>(&tmR, r, 128) || !make_operand_map<KIND, S_MN<KIND>>(&tmS, s, 128) ||
+    if (!make_rows_map<KIND>(&tmR, r) || !make_operand_map<KIND, S_MN<KIND>>(&tmS, s, 128) ||
         !raise_smem(int8_pair_kernel<KIND>, C::SMEM_BYTES, done)) return FMM_ERR_CUDA;
     p.tiles_r = (p.rows + 255) / 256; p.tiles_c = (p.cols + 255) / 256; p.k_shares = 1;
     // as few pairs as finish in the same number of waves
@@ -744,7 +845,7 @@ fmm_status_t launch_cluster(ProductParams p, const Operand& r, const Operand& s,
     using C = ClusterCfg<KIND, TC>;
     static std::atomic<bool> done[64];
     CUtensorMap tmR, tmS;
-    if (!make_operand_map<KIND, R_MN<KIND>>(&tmR, r, 128) || !make_operand_map<KIND, S_MN<KIND>>(&tmS, s, TC) ||
+    if (!make_rows_map<KIND>(&tmR, r) || !make_operand_map<KIND, S_MN<KIND>>(&tmS, s, TC) ||
         !raise_smem(int8_cluster_kernel<KIND, TC>, C::SMEM_BYTES, done)) return FMM_ERR_CUDA;
     p.tiles_r = (p.rows + 127) / 128; p.tiles_c = (p.cols + TC - 1) / TC; p.k_shares = shares;
     const int64_t grid = (int64_t)p.tiles_r * p.tiles_c * shares;
@@ -825,19 +926,32 @@ fmm_status_t launch_empty(const ProductParams& p, cudaStream_t st)
 bool grad_dims_ok(int64_t M, int64_t N, int64_t K)
 {
     if (!(M >= 0 && M < INT8_MAX_DIM && N >= 0 && N < INT8_MAX_DIM && K >= 0 && K < INT8_MAX_DIM)) return false;
-    return 2.0 * ((double)std::max(M, N) * (K + 8) + (double)M * (N + 8)) < 0x1p46;
+    return 2.0 * (3.0 * std::max(M, N) * (K + 8) + (double)M * (N + 8)) < 0x1p46;
 }
 bool dim_ok(int64_t n) { return n >= 0 && n < INT8_MAX_DIM; }
 int64_t up_to(int64_t n, int64_t a) { return ceil_div(n, a) * a; }
 
-struct GradWorkspace { int64_t ld_codes, ld_dy; size_t dy, total; };       // elements, elements, bytes, bytes
-GradWorkspace grad_workspace(int64_t code_rows, int64_t K, int64_t M, int64_t N, bool dy_aligned)
+// What a gradient's product reads and where it lies in the workspace: the values' parts (or codes), what belongs to them (maxima of the scales
+// and a flag for each stage, or a factor for each row of dY), and dY where it is not read as it lies.
+struct GradPlan {
+    bool scaled;                            // the scales go to dY (see the top)
+    int parts;
+    fmm_type_t operands;                    // type of what is multiplied
+    int64_t ld_values, ld_dy;               // elements
+    size_t extra, dy, total;                // bytes
+};
+template <int KIND> GradPlan grad_plan(const fmm_int8_grad_t* a)
 {
-    GradWorkspace w;
-    w.ld_codes = up_to(K, 8);
-    w.ld_dy = up_to(N, 8);
-    w.dy = (size_t)up_to(code_rows * w.ld_codes * 2, 256);
-    w.total = w.dy + (dy_aligned ? 0 : (size_t)up_to(M * w.ld_dy * 2, 256));
+    const int64_t code_rows = KIND == GRAD_W ? a->M : a->N;
+    GradPlan w;
+    w.scaled = KIND == GRAD_X && a->type == FMM_TYPE_BF16 && a->out_type == FMM_TYPE_BF16 && !a->rounded;
+    w.parts = w.scaled || a->rounded ? 1 : a->type == FMM_TYPE_BF16 && a->out_type == FMM_TYPE_F32 ? 3 : 2;
+    w.operands = w.scaled ? FMM_TYPE_F16 : a->type;
+    w.ld_values = up_to(a->K, 8);
+    w.ld_dy = up_to(a->N, 8);
+    w.extra = (size_t)up_to(code_rows * w.ld_values * 2 * w.parts, 256);
+    w.dy = w.extra + (size_t)up_to(w.scaled ? a->M * 4 : INT8_MAXIMA * 4 + ceil_div(code_rows, INT8_PART_ROWS), 256);
+    w.total = w.dy + (!w.scaled && int8_aligned(a->dy, a->ldy * 2, 16) ? 0 : (size_t)up_to(a->M * w.ld_dy * 2, 256));
     return w;
 }
 
@@ -845,11 +959,11 @@ template <int KIND> fmm_status_t grad_workspace_bytes(const fmm_int8_grad_t* a, 
 {
     if (!a || !bytes) return FMM_ERR_INVALID_ARG;
     if (!grad_dims_ok(a->M, a->N, a->K)) return FMM_ERR_SHAPE;
-    *bytes = grad_workspace(KIND == GRAD_W ? a->M : a->N, a->K, a->M, a->N, int8_aligned(a->dy, a->ldy * 2, 16)).total;
+    *bytes = grad_plan<KIND>(a).total;
     return FMM_OK;
 }
 
-// Both gradients: the codes restored to dy's type in the workspace, dy realigned there if it has to be, one product.
+// Both gradients: what the product reads into the workspace, one product.
 template <int KIND>
 fmm_status_t grad(const fmm_int8_grad_t* a, void* workspace, size_t workspace_bytes, void* stream)
 {
@@ -871,25 +985,37 @@ fmm_status_t grad(const fmm_int8_grad_t* a, void* workspace, size_t workspace_by
     int8_add_range(p.ranges, a->out, cols, K, ldo, eo);
     if (contraction == 0) return a->accumulate ? FMM_OK : launch_empty(p, st);
     if (!dY || ldy < N || ((uintptr_t)dY & 1) || !codes || ldc < K || !scales || ((uintptr_t)scales & 3)) return FMM_ERR_INVALID_ARG;
-    const bool dy_aligned = int8_aligned(dY, ldy * 2, 16);
-    const GradWorkspace w = grad_workspace(code_rows, K, M, N, dy_aligned);
+    const GradPlan w = grad_plan<KIND>(a);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < w.total) return FMM_ERR_WORKSPACE;
-    const fmm_int8_dequantize_t restore = {type, 0, code_rows, K, codes, ldc, scales, workspace, w.ld_codes};
-    fmm_status_t s = fmm_int8_dequantize(&restore, stream);
-    if (s != FMM_OK) return s;
+    char* base = static_cast<char*>(workspace);
+    const int64_t step = code_rows * w.ld_values;
     Operand dy = {dY, M, N, ldy};
-    if (!dy_aligned) {
-        void* copy = static_cast<char*>(workspace) + w.dy;
-        s = int8_realign(dY, ldy, copy, w.ld_dy, M, N, st);
-        if (s != FMM_OK) return s;
-        dy = {copy, M, N, w.ld_dy};
+    fmm_status_t s = FMM_OK;
+    if (w.scaled) {
+        float* inverse = reinterpret_cast<float*>(base + w.extra);
+        s = int8_values(w.operands, 1, codes, ldc, nullptr, nullptr, nullptr, base, w.ld_values, step, code_rows, K, st);
+        if (s == FMM_OK) s = int8_scaled_rows(dY, ldy, scales, base + w.dy, w.ld_dy, inverse, M, N, st);
+        dy = {base + w.dy, M, N, w.ld_dy};
+        p.c_scales = inverse;
+    } else {
+        uint32_t* maxima = type == FMM_TYPE_F16 ? reinterpret_cast<uint32_t*>(base + w.extra) : nullptr;
+        uint8_t* flags = w.parts > 1 ? reinterpret_cast<uint8_t*>(base + w.extra) + INT8_MAXIMA * 4 : nullptr;
+        if (maxima) s = int8_scale_maxima(scales, code_rows, maxima, st);
+        if (s == FMM_OK) s = int8_values(w.operands, w.parts, codes, ldc, scales, maxima, flags, base, w.ld_values, step, code_rows, K, st);
+        if (s == FMM_OK && !int8_aligned(dY, ldy * 2, 16)) {
+            s = int8_realign(dY, ldy, base + w.dy, w.ld_dy, M, N, st);
+            dy = {base + w.dy, M, N, w.ld_dy};
+        }
+        p.flags = flags; p.maxima = maxima; p.maxima_count = int8_scale_maxima_count(code_rows);
     }
+    if (s != FMM_OK) return s;
+    p.parts = w.parts;
     p.behind = 1;
-    const uint32_t format = type == FMM_TYPE_BF16 ? 1u : 0u;
+    const uint32_t format = w.operands == FMM_TYPE_BF16 ? 1u : 0u;
     p.kstages = (int)ceil_div(contraction, 64);
     p.chunk = out_type == FMM_TYPE_F32 ? CHUNK : p.kstages;
     p.idesc = (1u << 4) | (format << 7) | (format << 10) | (1u << 15) | ((KIND == GRAD_W ? 1u : 0u) << 16);
-    return launch_product<KIND>(p, {workspace, code_rows, K, w.ld_codes}, dy, st);
+    return launch_product<KIND>(p, {base, code_rows, K, w.ld_values, w.parts, step}, dy, st);
 }
 
 }  // namespace

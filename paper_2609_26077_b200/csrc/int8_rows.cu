@@ -5,6 +5,7 @@
 // A thread owns groups of eight consecutive columns (16 bytes of a 16-bit type), a warp N * 256 consecutive columns: group i of lane l are
 // columns 256 i + 8 l and on, so that a block of 32 (128) columns is 4 (16) neighbouring lanes and its maximum takes 2 (4) shuffles.
 #include <math.h>
+#include <algorithm>
 #include <type_traits>
 #include "fmm_ptx.cuh"
 #include "int8_internal.h"
@@ -543,7 +544,6 @@ template <typename T, int AL>
 __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
 {
     constexpr int VPT = FLAT_VPT;
-    fmmptx::griddep_launch_dependents();                      // (the product of a gradient, which waits for this grid to end)
     const int per_row = p.block ? (p.cols + p.block - 1) / p.block : 1, shift = p.block == 32 ? 5 : 7;
     for (int64_t row = (int64_t)blockIdx.x * blockDim.z + threadIdx.z; row < p.rows; row += (int64_t)gridDim.x * blockDim.z) {
         const int8_t* codes = p.codes + row * p.ldc;
@@ -570,6 +570,210 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
             store_groups<AL>(x, col, p.cols - col, f, p, 2131);
         }
     }
+}
+
+// ---------------------------------------------------------------------------------------- what the product of a gradient reads
+// Maxima of the finite scales' magnitudes, one a block
+__global__ void __launch_bounds__(1024) scale_maxima_kernel(const float* __restrict__ scales, int rows, uint32_t* __restrict__ maxima)
+{
+    __shared__ uint32_t red[32];
+    fmmptx::griddep_launch_dependents();
+    uint32_t m = 0;
+    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < rows; i += (int64_t)gridDim.x * 1024) {
+        const uint32_t b = __float_as_uint(scales[i]) & 0x7FFFFFFFu;
+        if (b < 0x7F800000u) m = max(m, b);
+    }
+    m = row_max(m, red, 32);
+    if (threadIdx.x == 0) maxima[blockIdx.x] = m;
+}
+
+// A part of a number that others follow: cut off towards zero and never the whole of it, so that what is left has its sign and is not zero.
+// (An infinity of dY times a part of 0, or minus an infinity from a part of the other sign, would be NaN.)  Infinities and NaN as they are.
+template <typename T> __device__ __forceinline__ uint16_t part_below(float v);
+template <> __device__ __forceinline__ uint16_t part_below<__nv_bfloat16>(float v)
+{
+    const uint32_t b = __float_as_uint(v);
+    return (uint16_t)((b - ((b & 0x7FFFFFFFu) - 1u < 0x7F7FFFFFu ? 1u : 0u)) >> 16);
+}
+template <> __device__ __forceinline__ uint16_t part_below<__half>(float v)
+{
+    const uint16_t h = __half_as_ushort(__float2half_rz(v));
+    return (uint16_t)(h - (__half2float(__ushort_as_half(h)) == v && (uint16_t)((h & 0x7FFFu) - 1u) < 0x7BFFu ? 1u : 0u));
+}
+
+// A row's pieces as those of dequantize_kernel.  The values are those of fp32; a part is what the parts before it leave, the last one rounded
+// to nearest: two of bf16 are 2^-16 off at most, three exact, two of fp16 2^-22 (or 2^-25 in the units that matrix_exponent sets).
+// Where the stage needs one part the others are neither written nor read.
+struct ValuesParams {
+    const int8_t* codes; const float* scales; const uint32_t* maxima; uint8_t* flags; void* x;
+    int64_t ldc, ldx, step;
+    int rows, cols, parts, maxima_count;
+    bool vc;
+    Int8Ranges ranges;
+};
+// whether a scale of a row's stage is no power of two (warp-collective, two rows a lane)
+__device__ __forceinline__ bool inexact_stage(const float* scales, int rows, int64_t row)
+{
+    const int64_t r = row / INT8_PART_ROWS * INT8_PART_ROWS + (threadIdx.x & 31);
+    uint32_t bits = 0;
+    if (r < rows) bits = __float_as_uint(scales[r]);
+    if (r + 32 < rows) bits |= __float_as_uint(scales[r + 32]);
+    return __any_sync(0xffffffffu, bits & 0x007FFFFFu);
+}
+template <typename T>
+__global__ void __launch_bounds__(256) values_kernel(const ValuesParams p)
+{
+    constexpr int VPT = FLAT_VPT;
+    fmmptx::griddep_launch_dependents();                      // (the product, which waits for this grid to end)
+    float factor = 1.0f;
+    if (p.maxima) {
+        fmmptx::griddep_wait();
+        factor = power_of_two(matrix_exponent(p.maxima, p.maxima_count));
+    }
+    for (int64_t row = (int64_t)blockIdx.x * blockDim.z + threadIdx.z; row < p.rows; row += (int64_t)gridDim.x * blockDim.z) {
+        const int8_t* codes = p.codes + row * p.ldc;
+        const float scale = p.scales ? p.scales[row] * factor : 1.0f;
+        const bool inexact = p.parts > 1 && inexact_stage(p.scales, p.rows, row);
+        const int parts = inexact ? p.parts : 1;
+        if (p.flags && row % INT8_PART_ROWS == 0 && threadIdx.x == 0 && threadIdx.y == 0) {
+            uint8_t* flag = p.flags + row / INT8_PART_ROWS;
+            if (ROW_STORE_OK(flag, 1, 2183)) *flag = inexact;
+        }
+        T* x = static_cast<T*>(p.x) + row * p.ldx;
+        for (int piece = threadIdx.y * FLAT_PIECE; piece < p.cols; piece += blockDim.y * FLAT_PIECE) {
+            const int col = piece + 8 * threadIdx.x;
+            uint2 c[VPT];
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) c[i] = load_codes8(codes + col + i * GROUP, p.cols - (col + i * GROUP), p.vc);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                if (col + i * GROUP >= p.cols) continue;
+                float f[8];
+                codes_to_float(c[i], f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], scale);
+                T* q = x + col + i * GROUP;
+                for (int part = 1; part < parts; ++part, q += p.step) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint16_t h = part_below<T>(f[j]);
+                        w[j / 2] = j & 1 ? w[j / 2] | (uint32_t)h << 16 : h;
+                        const float held = to_float(*reinterpret_cast<const T*>(&h));
+                        if (isfinite(held)) f[j] -= held;
+                    }
+                    // (columns behind the last, up to a multiple of eight, belong to the row and are not read)
+                    if (ROW_STORE_OK(q, 16, 2181)) *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = pack_two<T>(f[2 * j], f[2 * j + 1]);
+                if (ROW_STORE_OK(q, 16, 2182)) *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+    }
+}
+
+// The largest finite number of a row comes to lie in [2^14, 2^15) (within what powers of two fp32 holds on both sides).
+struct ScaledParams {
+    const __nv_bfloat16* x; const float* scales; __half* y; float* inverse;
+    int64_t ldx, ldy;
+    int rows, cols;
+    Int8Ranges ranges;
+};
+__device__ __forceinline__ uint32_t finite_max8(const float (&f)[8], uint32_t m)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t b = __float_as_uint(f[j]) & 0x7FFFFFFFu;
+        m = max(m, b < 0x7F800000u ? b : 0u);
+    }
+    return m;
+}
+__device__ __forceinline__ int scaled_exponent(uint32_t most) { return most == 0 ? 0 : min(14 - ((int)(most >> 23) - 127), 126); }
+__device__ __forceinline__ void store_scaled8(const ScaledParams& p, int64_t row, int col, const float (&f)[8], float factor)
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = pack_two<__half>(__fmul_rn(f[2 * j], factor), __fmul_rn(f[2 * j + 1], factor));
+    uint4* q = reinterpret_cast<uint4*>(p.y + row * p.ldy + col);
+    if (ROW_STORE_OK(q, 16, 2191)) *q = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A row per block at a time, two groups of eight columns a thread, whose scales stay in registers; the next row is on its way while this one's
+// maximum is found.  (8192 x 8192: 43 us, 152 with the scales loaded for every row.)
+template <int AL>
+__global__ void __launch_bounds__(1024) scaled_rows_kernel(const ScaledParams p)
+{
+    using T = __nv_bfloat16;
+    constexpr int VPT = 2;
+    __shared__ uint32_t red[2][32];
+    fmmptx::griddep_launch_dependents();
+    const int t = threadIdx.x, warps = blockDim.x / 32, first = ((t >> 5) * VPT * 32 + (t & 31)) * 8;
+    auto left = [&](int i) { return p.cols - (first + i * GROUP); };
+    float scale[VPT][8];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) scale[i][j] = j < left(i) ? p.scales[first + i * GROUP + j] : 0.0f;
+    Raw8<T, AL> raw[VPT];
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(p.x + row * p.ldx, first + i * GROUP, left(i));
+    };
+    int parity = 0;
+    fetch(blockIdx.x);
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+        const int m = AL ? 0 : row_offset(p.x + row * p.ldx);
+        float f[VPT][8];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            unpack8<T, AL>(raw[i], m, left(i), f[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[i][j] = __fmul_rn(f[i][j], scale[i][j]);
+            most = finite_max8(f[i], most);
+        }
+        if (row + gridDim.x < p.rows) fetch(row + gridDim.x);
+        const int e = scaled_exponent(row_max(most, red[parity], warps));
+        if (t == 0 && ROW_STORE_OK(p.inverse + row, 4, 2192)) p.inverse[row] = power_of_two(-e);
+        const float factor = power_of_two(e);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) if (left(i) > 0) store_scaled8(p, row, first + i * GROUP, f[i], factor);
+    }
+    fmmptx::griddep_wait();                                   // what waits for this grid waits for the one before it too
+}
+// rows that do not fit registers: read twice, the second time from L2, mostly
+__global__ void __launch_bounds__(1024) scaled_long_kernel(const ScaledParams p)
+{
+    using T = __nv_bfloat16;
+    __shared__ uint32_t red[2][32];
+    fmmptx::griddep_launch_dependents();
+    int parity = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+        const T* x = p.x + row * p.ldx;
+        const int m = row_offset(x);
+        auto scaled8 = [&](int col, float (&f)[8]) {
+            const int n = p.cols - col;
+            unpack8<T, 0>(load8<T, 0>(x, col, n), m, n, f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = j < n ? __fmul_rn(f[j], p.scales[col + j]) : 0.0f;
+        };
+        uint32_t most = 0;
+        for (int col = 8 * threadIdx.x; col < p.cols; col += 8 * 1024) {
+            float f[8];
+            scaled8(col, f);
+            most = finite_max8(f, most);
+        }
+        const int e = scaled_exponent(row_max(most, red[parity], 32));
+        if (threadIdx.x == 0 && ROW_STORE_OK(p.inverse + row, 4, 2194)) p.inverse[row] = power_of_two(-e);
+        for (int col = 8 * threadIdx.x; col < p.cols; col += 8 * 1024) {
+            float f[8];
+            scaled8(col, f);
+            store_scaled8(p, row, col, f, power_of_two(e));
+        }
+    }
+    fmmptx::griddep_wait();
 }
 
 // 16-bit rows of any alignment, copied to rows that a tensor map can read (ldy a multiple of 8, y on a 16-byte boundary); what lies
@@ -802,6 +1006,19 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const BackParams p)
 // ---------------------------------------------------------------------------------------- launches
 fmm_status_t launched() { return cudaGetLastError() == cudaSuccess ? FMM_OK : FMM_ERR_CUDA; }
 
+// behind: set up while the kernel before drains, for which it waits itself
+template <typename P> fmm_status_t launch_behind(void (*kernel)(P), unsigned grid, dim3 block, bool behind, const P& p, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid); cfg.blockDim = block; cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = behind ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) { cudaGetLastError(); return FMM_ERR_CUDA; }
+    return FMM_OK;
+}
+
 template <typename T, bool NORM> fmm_status_t launch_rows(const RowsParams& p, cudaStream_t st)
 {
     const int groups = (p.cols + 7) / 8;
@@ -851,14 +1068,7 @@ template <typename T> fmm_status_t launch_back(const BackParams& p, int threads,
     else launch(std::integral_constant<int, 0>{});
     if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;
     // set up while the rows are dealt with; it waits for them before its first load
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.cols + 31) / 32); cfg.blockDim = dim3(1024); cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, column_sum_kernel, p) != cudaSuccess) { cudaGetLastError(); return FMM_ERR_CUDA; }
-    return FMM_OK;
+    return launch_behind(column_sum_kernel, (unsigned)(p.cols + 31) / 32, dim3(1024), true, p, st);
 }
 
 // eight warps of a block without a reduction: pieces of a row along y, rows along z
@@ -882,6 +1092,37 @@ bool block_ok(int block) { return block == 0 || block == 32 || block == 128; }
 bool matrix_ok(const void* p, int64_t cols, int64_t ld, int element) { return p && ld >= cols && !((uintptr_t)p & (element - 1)); }
 
 }  // namespace
+
+int int8_scale_maxima_count(int64_t rows) { return (int)(rows < 1024 * INT8_MAXIMA ? (rows + 1023) / 1024 : INT8_MAXIMA); }
+
+fmm_status_t int8_scale_maxima(const float* scales, int64_t rows, uint32_t* maxima, cudaStream_t st)
+{
+    scale_maxima_kernel<<<(unsigned)int8_scale_maxima_count(rows), 1024, 0, st>>>(scales, (int)rows, maxima);
+    return launched();
+}
+
+fmm_status_t int8_values(fmm_type_t type, int parts, const int8_t* codes, int64_t ldc, const float* scales, const uint32_t* maxima, uint8_t* flags, void* x, int64_t ldx,
+                         int64_t step, int64_t rows, int64_t cols, cudaStream_t st)
+{
+    ValuesParams p = {codes, scales, maxima, flags, x, ldc, ldx, step, (int)rows, (int)cols, parts, int8_scale_maxima_count(rows), int8_aligned(codes, ldc, 8), {}};
+    for (int i = 0; i < parts; ++i) int8_add_range(p.ranges, static_cast<char*>(x) + 2 * i * step, rows, ldx, ldx, 2);
+    int8_add_range(p.ranges, flags, 1, (rows + INT8_PART_ROWS - 1) / INT8_PART_ROWS, rows, 1);
+    const dim3 b = flat_block((int)cols);
+    const unsigned grid = flat_grid((int)rows, b);
+    return launch_behind(type == FMM_TYPE_BF16 ? values_kernel<__nv_bfloat16> : values_kernel<__half>, grid, b, maxima != nullptr, p, st);
+}
+
+fmm_status_t int8_scaled_rows(const void* x, int64_t ldx, const float* scales, void* y, int64_t ldy, float* inverse, int64_t rows, int64_t cols, cudaStream_t st)
+{
+    ScaledParams p = {static_cast<const __nv_bfloat16*>(x), scales, static_cast<__half*>(y), inverse, ldx, ldy, (int)rows, (int)cols, {}};
+    int8_add_range(p.ranges, y, rows, ldy, ldy, 2);
+    int8_add_range(p.ranges, inverse, 1, rows, rows, 4);
+    const int64_t threads = (cols + 511) / 512 * 32;          // two groups of eight columns each
+    const bool fits = threads <= 1024;
+    const int64_t resident = (int64_t)int8_sm_count() * (fits ? std::min<int64_t>(16, 1024 / threads) : 1);
+    return launch_behind(!fits ? scaled_long_kernel : cols % 8 == 0 && int8_aligned(x, ldx * 2, 16) ? scaled_rows_kernel<1> : scaled_rows_kernel<0>,
+                         (unsigned)std::min(rows, resident), dim3((unsigned)(fits ? threads : 1024)), true, p, st);
+}
 
 fmm_status_t int8_realign(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int64_t cols, cudaStream_t st)
 {

@@ -4,7 +4,7 @@ every step runs in the CUDA kernels).
 A forward and backward pass of one layer, everything that is kept for the backward pass in 8 bits:
 
     w, ws = int8.quantize(weight)                                   # (N, K): one scale per output channel
-    n = int8.rms_norm(x, gain, residual=r, checkpoint=128)          # hidden rows, their 8-bit norm, a checkpoint
+    n = int8.rms_norm(x, gain, residual=r, pow2=True, checkpoint=128)    # hidden rows, their 8-bit norm, a checkpoint
     z = int8.matmul(n.codes, n.scales, w, ws)                       # (M, N)
     ...
     dw = int8.grad_weight(dz, n.codes, n.scales)                    # (N, K)
@@ -56,7 +56,7 @@ class MatmulArgs(C.Structure):
 
 class GradArgs(C.Structure):
     """fmm_int8_grad_t"""
-    _fields_ = [("type", C.c_int), ("out_type", C.c_int), ("accumulate", C.c_int), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64),
+    _fields_ = [("type", C.c_int), ("out_type", C.c_int), ("accumulate", C.c_int), ("rounded", C.c_int), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64),
                 ("dy", C.c_void_p), ("ldy", C.c_int64), ("codes", C.c_void_p), ("ldc", C.c_int64), ("scales", C.c_void_p), ("out", C.c_void_p),
                 ("ldo", C.c_int64)]
 
@@ -382,7 +382,7 @@ def matmul(a, a_scales, b, b_scales, bias=None, dtype=torch.bfloat16, out=None, 
     return out
 
 
-def _grad(what, device, dy, codes, scales, shape, dtype, out, accumulate):
+def _grad(what, device, dy, codes, scales, shape, dtype, out, accumulate, rounded):
     kind = dy.dtype
     if kind is not torch.bfloat16 and kind is not torch.float16:
         raise TypeError(f"dy: bfloat16 or float16 is needed, not {kind}")
@@ -404,38 +404,44 @@ def _grad(what, device, dy, codes, scales, shape, dtype, out, accumulate):
             raise TypeError(f"the gradient is float32 or of dy's type, not {dtype}")
         ldo = _matrix(out, "out", dtype, device, shape)
     at = dy.data_ptr()
-    a = _grad_args(_TYPES[kind], _TYPES[dtype], int(accumulate), M, N, K, at, ldy, codes.data_ptr(), ldc, scales.data_ptr(), out.data_ptr(), ldo)
-    need = _need(what + "_workspace_bytes", (M, N, K, not (at & 15 or ldy & 7)), a)
+    rounded = bool(rounded)
+    a = _grad_args(_TYPES[kind], _TYPES[dtype], bool(accumulate), rounded, M, N, K, at, ldy, codes.data_ptr(), ldc, scales.data_ptr(), out.data_ptr(), ldo)
+    need = _need(what + "_workspace_bytes", (M, N, K, not (at & 15 or ldy & 7), kind, dtype, rounded), a)
     workspace = dy.new_empty((need,), dtype=torch.uint8)
     call = (_lib or lib()).fmm_int8_grad_weight if what == "fmm_int8_grad_weight" else (_lib or lib()).fmm_int8_grad_input
     _call(call(a, workspace.data_ptr(), need, _stream(device)), what)
     return out
 
 
-def grad_weight(dy, codes, scales, dtype=torch.float32, out=None, accumulate=False, stream=None):
+def grad_weight(dy, codes, scales, dtype=torch.float32, out=None, accumulate=False, stream=None, rounded=False):
     """Gradient of matmul's b: dy^T (M x N, 16-bit) times the activations that codes (M x K) and scales stand for: N x K in
-    `dtype` (float32 or dy's type).  With accumulate it is added to out."""
+    `dtype` (float32 or dy's type).  With accumulate it is added to out.
+
+    The activations count as the numbers of fp32 that they are.  With scales that are powers of two (quantize, rms_norm with
+    pow2=True) 16 bits hold them; with others they are multiplied in two or three 16-bit parts, which takes as many times as long.
+    With `rounded` in one part, rounded to dy's type: 2^-9 of each for bfloat16, 2^-12 for float16."""
     device = _device(dy)
     where = _elsewhere(device, stream)
     if where is not None:
         with where:
-            return grad_weight(dy, codes, scales, dtype, out, accumulate)
+            return grad_weight(dy, codes, scales, dtype, out, accumulate, rounded=rounded)
     if dy.dim() != 2 or codes.dim() != 2 or codes.shape[0] != dy.shape[0]:
         raise ValueError(f"dy and codes: two dimensions and as many rows are needed, not {tuple(dy.shape)} and {tuple(codes.shape)}")
-    return _grad("fmm_int8_grad_weight", device, dy, codes, scales, (dy.shape[1], codes.shape[1]), dtype, out, accumulate)
+    return _grad("fmm_int8_grad_weight", device, dy, codes, scales, (dy.shape[1], codes.shape[1]), dtype, out, accumulate, rounded)
 
 
-def grad_input(dy, codes, scales, dtype=None, out=None, accumulate=False, stream=None):
+def grad_input(dy, codes, scales, dtype=None, out=None, accumulate=False, stream=None, rounded=False):
     """Gradient of matmul's a: dy (M x N, 16-bit) times the weight that codes (N x K) and scales stand for: M x K in `dtype`
-    (float32 or dy's type, the default).  With accumulate it is added to out."""
+    (float32 or dy's type, the default).  With accumulate it is added to out.  Values and `rounded` as for grad_weight; the
+    bfloat16 gradient of a bfloat16 dy takes one pass whatever the scales."""
     device = _device(dy)
     where = _elsewhere(device, stream)
     if where is not None:
         with where:
-            return grad_input(dy, codes, scales, dtype, out, accumulate)
+            return grad_input(dy, codes, scales, dtype, out, accumulate, rounded=rounded)
     if dy.dim() != 2 or codes.dim() != 2 or codes.shape[0] != dy.shape[1]:
         raise ValueError(f"dy and codes: two dimensions and dy's columns as codes' rows are needed, not {tuple(dy.shape)} and {tuple(codes.shape)}")
-    return _grad("fmm_int8_grad_input", device, dy, codes, scales, (dy.shape[0], codes.shape[1]), dtype, out, accumulate)
+    return _grad("fmm_int8_grad_input", device, dy, codes, scales, (dy.shape[0], codes.shape[1]), dtype, out, accumulate, rounded)
 
 
 def status():
