@@ -157,6 +157,21 @@ fmm_status_t fmm_int8_grad_input_workspace_bytes(const fmm_int8_grad_t* p, size_
 fmm_status_t fmm_int8_grad_weight(const fmm_int8_grad_t* p, void* workspace, size_t workspace_bytes, void* cuda_stream);
 fmm_status_t fmm_int8_grad_input(const fmm_int8_grad_t* p, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* How a product or gradient is multiplied, for tests and measurements. */
+typedef struct {
+    int kernel;                  /* 1: persistent CTA pairs (columns 256, k_shares 1); 2: a cluster of k_shares CTAs a tile;
+                                    3: few tokens (products of up to eight; columns 8, k_shares 1) */
+    int columns;                 /* cluster: of a tile: products 16, 32, 64, 128; gradients 64, 128 */
+    int k_shares;                /* cluster: CTAs that share the contraction, 1 to 8, each a stage (128 codes, 64 numbers) at least */
+} fmm_int8_product_shape_t;
+typedef enum { FMM_INT8_MATMUL = 0, FMM_INT8_GRAD_WEIGHT = 1, FMM_INT8_GRAD_INPUT = 2 } fmm_int8_product_t;
+/* The shape that a call of this size takes on the current device (M, N, K > 0, as the call has them; out_type: of its output). */
+fmm_status_t fmm_int8_product_shape(fmm_int8_product_t which, int64_t M, int64_t N, int64_t K, fmm_type_t out_type, fmm_int8_product_shape_t* shape);
+/* From now on every call of the calling host thread takes `shape` instead of the one that the library expects to be fastest; NULL: the
+ * library chooses again.  FMM_ERR_INVALID_ARG for a shape that does not exist; a call that cannot be multiplied that way (more tokens
+ * than few, more shares than stages, columns that its kind does not have) returns FMM_ERR_SHAPE. */
+fmm_status_t fmm_int8_force_product_shape(const fmm_int8_product_shape_t* shape);
+
 /* Status of the product kernels on the current device, read after cudaDeviceSynchronize: *code == 0, or the location of
  * the first bounded device-side wait that gave up (FMM_ERR_DEVICE_TIMEOUT; the results of that call are invalid).
  * Debug build (fmm_debug_build): also the first store outside the ranges that a launch was given. */

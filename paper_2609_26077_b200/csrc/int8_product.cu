@@ -901,19 +901,35 @@ ProductChoice choose_product(const ProductModel& m, const ProductParams& p, doub
     return choice;
 }
 
-template <int KIND>
-fmm_status_t launch_product(const ProductParams& p, const Operand& r, const Operand& s, cudaStream_t st)
+// what fmm_int8_force_product_shape set for this host thread; kernel 0: nothing
+thread_local fmm_int8_product_shape_t forced_shape;
+enum { SHAPE_PAIRS = 1, SHAPE_CLUSTER = 2, SHAPE_FEW = 3 };
+constexpr int FEW_SHAPE_COLUMNS = FEW_TOKENS;
+
+template <int KIND> fmm_int8_product_shape_t product_shape(const ProductParams& p, const Operand& r, const Operand& s)
 {
+    if (forced_shape.kernel) return forced_shape;
+    if (KIND == INT8 && p.cols <= FEW_TOKENS) return {SHAPE_FEW, FEW_SHAPE_COLUMNS, 1};
     const int e = KIND == INT8 ? 1 : 2;
     const double bytes = (double)e * ((double)r.rows * r.cols + (double)s.rows * s.cols) + (double)p.rows * p.cols * int8_type_bytes((fmm_type_t)p.out_type);
     const ProductChoice c = choose_product(KIND == INT8 ? MODEL_INT8 : MODEL_GRAD, p, bytes, int8_sm_count());
+    return {c.columns == 256 ? SHAPE_PAIRS : SHAPE_CLUSTER, c.columns, c.shares};
+}
+template <int KIND>
+fmm_status_t launch_product(const ProductParams& p, const Operand& r, const Operand& s, cudaStream_t st)
+{
+    const fmm_int8_product_shape_t c = product_shape<KIND>(p, r, s);
+    if (c.kernel == SHAPE_PAIRS) return launch_pair<KIND>(p, r, s, st);
     if constexpr (KIND == INT8) {
-        if (c.columns == 16) return launch_cluster<KIND, 16>(p, r, s, c.shares, st);
-        if (c.columns == 32) return launch_cluster<KIND, 32>(p, r, s, c.shares, st);
+        if (c.kernel == SHAPE_FEW) return p.cols <= FEW_TOKENS ? launch_few_tokens(p, r, s, st) : FMM_ERR_SHAPE;
     }
-    if (c.columns == 64) return launch_cluster<KIND, 64>(p, r, s, c.shares, st);
-    if (c.columns == 128) return launch_cluster<KIND, 128>(p, r, s, c.shares, st);
-    return launch_pair<KIND>(p, r, s, st);
+    if (c.kernel != SHAPE_CLUSTER || c.k_shares > p.kstages) return FMM_ERR_SHAPE;
+    if constexpr (KIND == INT8) {
+        if (c.columns == 16) return launch_cluster<KIND, 16>(p, r, s, c.k_shares, st);
+        if (c.columns == 32) return launch_cluster<KIND, 32>(p, r, s, c.k_shares, st);
+    }
+    if (c.columns == 64) return launch_cluster<KIND, 64>(p, r, s, c.k_shares, st);
+    return c.columns == 128 ? launch_cluster<KIND, 128>(p, r, s, c.k_shares, st) : FMM_ERR_SHAPE;
 }
 
 fmm_status_t launch_empty(const ProductParams& p, cudaStream_t st)
@@ -1040,7 +1056,6 @@ fmm_status_t fmm_int8_matmul(const fmm_int8_matmul_t* a, void* stream)
     if (!a->a || !a->b || !a->a_scales || !a->b_scales || (((uintptr_t)a->a_scales | (uintptr_t)a->b_scales) & 3) || a->lda < K || a->ldb < K ||
         !int8_aligned(a->a, a->lda, 16) || !int8_aligned(a->b, a->ldb, 16)) return FMM_ERR_INVALID_ARG;
     p.kstages = p.chunk = (int)ceil_div(K, 128);
-    if (M <= FEW_TOKENS) return launch_few_tokens(p, {a->b, N, K, a->ldb}, {a->a, M, K, a->lda}, st);
     p.idesc = (2u << 4) | (1u << 7) | (1u << 10);
     return launch_product<INT8>(p, {a->b, N, K, a->ldb}, {a->a, M, K, a->lda}, st);
 }
@@ -1054,6 +1069,36 @@ fmm_status_t fmm_int8_grad_weight(const fmm_int8_grad_t* p, void* workspace, siz
 fmm_status_t fmm_int8_grad_input(const fmm_int8_grad_t* p, void* workspace, size_t workspace_bytes, void* stream)
 {
     return grad<GRAD_X>(p, workspace, workspace_bytes, stream);
+}
+
+fmm_status_t fmm_int8_product_shape(fmm_int8_product_t which, int64_t M, int64_t N, int64_t K, fmm_type_t out_type, fmm_int8_product_shape_t* shape)
+{
+    if (!shape || which < FMM_INT8_MATMUL || which > FMM_INT8_GRAD_INPUT || !int8_type_ok(out_type)) return FMM_ERR_INVALID_ARG;
+    if (M <= 0 || N <= 0 || K <= 0 || (which == FMM_INT8_MATMUL ? !dim_ok(M) || !dim_ok(N) || K > 131071 : !grad_dims_ok(M, N, K))) return FMM_ERR_SHAPE;
+    ProductParams p = {};
+    p.out_type = out_type;
+    if (which == FMM_INT8_MATMUL) {
+        p.rows = (int)N; p.cols = (int)M; p.kstages = (int)ceil_div(K, 128);
+        *shape = product_shape<INT8>(p, {nullptr, N, K, K}, {nullptr, M, K, K});
+    } else {
+        const int64_t contraction = which == FMM_INT8_GRAD_WEIGHT ? M : N;
+        p.rows = (int)K; p.cols = (int)(which == FMM_INT8_GRAD_WEIGHT ? N : M); p.kstages = (int)ceil_div(contraction, 64);
+        const Operand values = {nullptr, contraction, K, K}, dy = {nullptr, M, N, N};
+        *shape = which == FMM_INT8_GRAD_WEIGHT ? product_shape<GRAD_W>(p, values, dy) : product_shape<GRAD_X>(p, values, dy);
+    }
+    return FMM_OK;
+}
+
+fmm_status_t fmm_int8_force_product_shape(const fmm_int8_product_shape_t* shape)
+{
+    if (!shape) { forced_shape = {}; return FMM_OK; }
+    const int c = shape->columns, n = shape->k_shares;
+    const bool ok = shape->kernel == SHAPE_PAIRS     ? c == 256 && n == 1
+                    : shape->kernel == SHAPE_CLUSTER ? (c == 16 || c == 32 || c == 64 || c == 128) && n >= 1 && n <= 8
+                                                     : shape->kernel == SHAPE_FEW && c == FEW_SHAPE_COLUMNS && n == 1;
+    if (!ok) return FMM_ERR_INVALID_ARG;
+    forced_shape = *shape;
+    return FMM_OK;
 }
 
 fmm_status_t fmm_int8_status(int* code)

@@ -33,7 +33,8 @@ _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 EXPORTS = ["fmm_int8_quantize", "fmm_int8_dequantize", "fmm_int8_rms_norm", "fmm_int8_rms_norm_backward_workspace_bytes",
            "fmm_int8_rms_norm_backward", "fmm_int8_matmul", "fmm_int8_grad_weight_workspace_bytes",
-           "fmm_int8_grad_input_workspace_bytes", "fmm_int8_grad_weight", "fmm_int8_grad_input", "fmm_int8_status", "fmm_int8_status_clear", "fmm_int8_selftest_bounded_wait"]
+           "fmm_int8_grad_input_workspace_bytes", "fmm_int8_grad_weight", "fmm_int8_grad_input", "fmm_int8_product_shape",
+           "fmm_int8_force_product_shape", "fmm_int8_status", "fmm_int8_status_clear", "fmm_int8_selftest_bounded_wait"]
 
 
 class QuantizeArgs(C.Structure):
@@ -78,6 +79,18 @@ class RmsNormBackwardArgs(C.Structure):
                 ("dgain", C.c_void_p)]
 
 
+class ProductShape(C.Structure):
+    """fmm_int8_product_shape_t; iterates as (kernel, columns, k_shares)."""
+    _fields_ = [("kernel", C.c_int), ("columns", C.c_int), ("k_shares", C.c_int)]
+
+    def __iter__(self):
+        return iter((self.kernel, self.columns, self.k_shares))
+
+
+KERNEL_PAIRS, KERNEL_CLUSTER, KERNEL_FEW_TOKENS = 1, 2, 3
+MATMUL, GRAD_WEIGHT, GRAD_INPUT = 0, 1, 2
+
+
 def _packer(kind):
     """pack() of the same bytes as kind(*fields): a quarter of the time that filling a ctypes structure takes, and a new object
     for every call, so that threads do not share one.  Addresses are 0, not None."""
@@ -104,6 +117,8 @@ def lib():
             getattr(L, "fmm_int8_" + name).argtypes = [ptr, ptr, size, ptr]
         L.fmm_int8_rms_norm_backward_workspace_bytes.argtypes = [i64, i64, ptr]
         L.fmm_int8_status.argtypes = [ptr]
+        L.fmm_int8_product_shape.argtypes = [C.c_int, i64, i64, i64, C.c_int, ptr]
+        L.fmm_int8_force_product_shape.argtypes = [ptr]
         L.fmm_int8_selftest_bounded_wait.argtypes = [i64, ptr]
         _lib = L
     return _lib
@@ -442,6 +457,19 @@ def grad_input(dy, codes, scales, dtype=None, out=None, accumulate=False, stream
     if dy.dim() != 2 or codes.dim() != 2 or codes.shape[0] != dy.shape[1]:
         raise ValueError(f"dy and codes: two dimensions and dy's columns as codes' rows are needed, not {tuple(dy.shape)} and {tuple(codes.shape)}")
     return _grad("fmm_int8_grad_input", device, dy, codes, scales, (dy.shape[0], codes.shape[1]), dtype, out, accumulate, rounded)
+
+
+def product_shape(which, M, N, K, dtype=torch.float32):
+    """The ProductShape that MATMUL, GRAD_WEIGHT or GRAD_INPUT takes on the current device for this size and output type."""
+    s = ProductShape()
+    _call(lib().fmm_int8_product_shape(which, M, N, K, _float_type(dtype, "dtype"), C.byref(s)), "fmm_int8_product_shape")
+    return s
+
+
+def force_product_shape(kernel=None, columns=256, k_shares=1):
+    """Every later call of this host thread takes this shape; without arguments: the library chooses again."""
+    s = None if kernel is None else C.byref(ProductShape(kernel, columns, k_shares))
+    _call(lib().fmm_int8_force_product_shape(s), "fmm_int8_force_product_shape")
 
 
 def status():

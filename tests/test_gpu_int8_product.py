@@ -48,7 +48,7 @@ def check_matmul(M, N, K, dtype=torch.float32, bias=False, seed=0, extreme=True,
     return c
 
 
-# every kernel: few tokens, tiles of 16, 32, 64 and 128 columns with and without shares of K, and pairs; edges on each side
+# as the library chooses by size (each kernel form by name: test_gpu_int8_forms.py); edges on each side
 SHAPES = [(1, 1, 1), (1, 17, 31), (3, 100, 77), (5, 4737, 129), (8, 4800, 1000), (8, 15, 4100), (7, 2048, 2047), (9, 300, 300), (1, 8192, 8192), (1, 130, 64), (2, 257, 1000), (15, 513, 2048), (16, 128, 128), (17, 1024, 4096), (32, 640, 96), (33, 129, 257),
           (64, 4096, 512), (65, 200, 4095), (100, 3000, 200), (128, 128, 8192), (129, 127, 129), (300, 777, 640), (777, 2047, 2048), (1000, 33, 5000),
           (2048, 2048, 1024), (1500, 2500, 100), (2049, 1793, 384), (5000, 16, 256), (4097, 65, 64), (8192, 1, 130)]

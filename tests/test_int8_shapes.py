@@ -40,3 +40,22 @@ def test_untested_kernels_have_a_column_for_every_thread(lib):
 
 def test_rows_without_columns_take_no_untested_kernel(lib):
     assert not row_form(lib, 0)[2]
+
+
+def test_product_shapes_are_refused_on_the_host():
+    B.build()
+    from paper_2609_26077_b200 import int8
+    lib, s = int8.lib(), int8.ProductShape()
+    ask = lambda *a: lib.fmm_int8_product_shape(*a, C.byref(s))
+    assert lib.fmm_int8_product_shape(0, 1, 1, 1, 0, None) == 1
+    for bad in ((3, 1, 1, 1, 0), (-1, 1, 1, 1, 0), (0, 1, 1, 1, 3)):
+        assert ask(*bad) == 1, bad
+    for bad in ((0, 0, 1, 1, 0), (0, 1, 1, 131072, 0), (1, 1, 0, 1, 0), (2, 1, 1, 1 << 31, 0), (0, 1 << 31, 1, 1, 0)):
+        assert ask(*bad) == 2, bad
+    for form in ((1, 256, 1), (2, 16, 8), (3, 8, 1)):
+        assert lib.fmm_int8_force_product_shape(C.byref(int8.ProductShape(*form))) == 0
+        assert ask(0, 5, 5, 5, 0) == 0 and tuple(s) == form
+    for form in ((0, 0, 0), (1, 256, 2), (2, 16, 9), (2, 256, 1), (3, 16, 1)):
+        assert lib.fmm_int8_force_product_shape(C.byref(int8.ProductShape(*form))) == 1
+        assert ask(0, 5, 5, 5, 0) == 0 and tuple(s) == (3, 8, 1)
+    assert lib.fmm_int8_force_product_shape(None) == 0
