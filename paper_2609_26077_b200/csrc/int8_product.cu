@@ -29,10 +29,10 @@
 //     output's own rounding, in one pass (8192 cubed: 800 us, 1514 with two parts, 759 with values rounded to bf16).
 //   - A caller who wants one pass in any case gets values rounded once to dY's type (`rounded`).
 //
-// The tensor cores add in fp32 by cutting off what does not fit, so the sums of a gradient drift towards zero as the contraction
-// grows: 2.4e-6 of their size over 8192 terms, 6e-6 over 16384.  Where the output is fp32 they are therefore taken out of the
-// accumulator every CHUNK stages (1024 terms) and added up in registers, rounded to nearest: 1.9e-7 for both.  An output of 16 bits has no
-// use for that.
+// The tensor cores add in fp32 by cutting off what does not fit, so the sums of a gradient drift towards zero as the contraction grows: sums of
+// positive terms by 2.2e-5 of their size over 8192 terms, 5.7e-5 over 16384, a 16-bit output's rounding over 2^20.  They are therefore
+// taken out of the accumulator and added up in registers, rounded to nearest: every CHUNK stages (1024 terms) where the output is fp32
+// (below 3.8e-6; of both signs 1.9e-7 instead of 2.4e-6 and 6e-6), every CHUNK_SHORT (8192 terms, below 3.1e-5) where it has 16 bits.
 //
 // The 8-bit operand is taken to 16 bits in the workspace before the product: 3 bytes a code and part once, against 2 M N K operations.  Doing
 // so tile by tile on the way into the tensor cores would take two more passes through shared memory per tile (codes in, 16-bit values
@@ -87,7 +87,7 @@ struct ProductParams {
     int kstages;                    // 128-byte stages of the contraction
     int tiles_r, tiles_c;
     int k_shares;                   // cluster kernel
-    int chunk;                      // gradients: stages after which the sums leave the tensor cores' accumulator (see below)
+    int chunk;                      // gradients: stages after which the sums leave the tensor cores' accumulator
     uint32_t idesc;                 // without the tile's dimensions
     const float* r_scales; const float* c_scales; const void* bias;      // INT8; c_scales: gradients too, or null
     const uint8_t* flags; int parts;                // gradients: which stages have `parts` parts (of int8_values; null: none), the others one
@@ -98,7 +98,7 @@ struct ProductParams {
     Int8Ranges ranges;
 };
 
-constexpr int CHUNK = 16;
+constexpr int CHUNK = 16, CHUNK_SHORT = 128;
 // contraction elements per stage
 template <int KIND> constexpr int STAGE_ELEMENTS = KIND == INT8 ? 128 : 64;
 template <int KIND> constexpr bool R_MN = KIND != INT8;
@@ -861,7 +861,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // holds (`shared` each), + what the exchange takes; a share more leaves 2 % more places in the GPCs empty.  CTAs without an exchange
 // make room one by one, so their rounds are a fraction.  Pairs: lat + waves of stages, + what a tile's output costs beyond the next
 // tile's stages.  The choice takes 1.1 % (gradients 0.1 %) more time than the fastest of these in the mean, at worst 1.31 times it (2048 x
-// 512 x 8192: 22.9, 17.4 us).
+// 512 x 8192: 22.9, 17.4 us).  Beyond the calls of the fit: gradients of 64 to 8192 tokens and 128 to 4096 channels 2.5 % in the mean, at worst 1.38
+// times (weight, 6192 x 1656 x 3128: 136, 99 us).  The models know one part a stage; weight gradients of three take 6.5 % more in the mean.
 struct ClusterModel { int columns; float lat, stage, shared, fixed; };
 struct ProductModel { float pair_lat, pair_stage, pair_tile, exchange, exchange_share; int per_sm, widths; ClusterModel cluster[4]; };
 constexpr ProductModel MODEL_INT8 = {6.544f, 0.277f, 2.584f, 2.365f, 0.022f, 2, 4,
@@ -1029,7 +1030,7 @@ fmm_status_t grad(const fmm_int8_grad_t* a, void* workspace, size_t workspace_by
     p.behind = 1;
     const uint32_t format = w.operands == FMM_TYPE_BF16 ? 1u : 0u;
     p.kstages = (int)ceil_div(contraction, 64);
-    p.chunk = out_type == FMM_TYPE_F32 ? CHUNK : p.kstages;
+    p.chunk = out_type == FMM_TYPE_F32 ? CHUNK : CHUNK_SHORT;
     p.idesc = (1u << 4) | (format << 7) | (format << 10) | (1u << 15) | ((KIND == GRAD_W ? 1u : 0u) << 16);
     return launch_product<KIND>(p, {base, code_rows, K, w.ld_values, w.parts, step}, dy, st);
 }

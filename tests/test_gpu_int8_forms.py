@@ -170,6 +170,25 @@ def test_sums_leave_the_accumulator_in_time(which, form, contraction):
     assert abs(off.mean().item()) <= 4e-6, off.mean().item()
 
 
+@pytest.mark.parametrize("form", [None, PAIRS, (int8.KERNEL_CLUSTER, 64, 1)])
+def test_sums_of_a_16_bit_output_too(form):
+    """A million tokens: 65536 additions of 16 positive terms each, which an accumulator that cuts off would lose up to 3.9e-3 of; of
+    8192 terms at a time 512 * 2^-24 = 3.1e-5.  fp16's rounding, 2.1e-4 in the mean and independent from column to column of dY (their factors
+    differ), leaves 2.6e-5 in the mean of 64 of them, of which four times are allowed."""
+    if form:
+        force(form)
+    M, N, K = (1 << 20) + 100, 64, 64
+    g = torch.Generator(device="cuda").manual_seed(1)
+    factor = torch.exp(torch.randn(N, device="cuda", generator=g)) * 2.0 ** -13
+    dy = ((torch.rand(M, N, device="cuda", generator=g) + 0.5) * factor).half()
+    codes = torch.randint(1, 128, (M, K), device="cuda", generator=g, dtype=torch.int8)
+    scales = torch.full((M,), 2.0 ** -6, device="cuda")
+    got = int8.grad_weight(dy, codes, scales, dtype=torch.float16)
+    want = dy.double().t() @ (codes.double() * 2.0 ** -6)
+    off = (got.double() - want) / want
+    assert abs(off.mean().item()) <= 3.1e-5 + 4 * 2.6e-5, off.mean().item()
+
+
 # ------------------------------------------------------------------------------------------------ choice and refusals
 def test_choice():
     shape = lambda *a, **k: tuple(int8.product_shape(*a, **k))
