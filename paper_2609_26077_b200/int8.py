@@ -14,13 +14,15 @@ A forward and backward pass of one layer, everything that is kept for the backwa
 Matrices are 2-D CUDA tensors whose columns are contiguous (rows may lie any distance apart); scales and gains are
 contiguous.  All tensors of a call are on one device, on whose current stream the work is enqueued, or on `stream`; nothing
 is synchronised, and calls may be captured into CUDA graphs.  Outputs are allocated unless they are given; codes get rows
-that are a multiple of 16 bytes apart, as `matmul` wants them.  Unsuitable tensors raise TypeError (types, devices) or
-ValueError (shapes, strides), anything that the library refuses raises fmm.FmmError.
+that are a multiple of 16 bytes apart, as `matmul` wants them.  Unsuitable arguments raise TypeError (types, devices) or
+ValueError (shapes, strides, blocks), anything that the library refuses raises fmm.FmmError.  Nothing is recorded for autograd,
+also of tensors that require a gradient: the gradients are calls of their own.
 """
 from __future__ import annotations
 
 import collections
 import ctypes as C
+import operator
 import struct
 
 import torch
@@ -180,9 +182,20 @@ def _float_type(dtype, name):
 
 
 def _block(block, name="block"):
+    try:
+        block = operator.index(block)
+    except TypeError:
+        raise TypeError(f"{name}: 0, 32 or 128 is needed, not {block!r}") from None
     if block not in (0, 32, 128):
-        raise ValueError(f"{name}: 0, 32 or 128 is needed, not {block!r}")
+        raise ValueError(f"{name}: 0, 32 or 128 is needed, not {block}")
     return block
+
+
+def _number(x, name):
+    try:
+        return float(x)
+    except (TypeError, ValueError):
+        raise TypeError(f"{name}: a number is needed, not {x!r}") from None
 
 
 def _scale_shape(rows, cols, block):
@@ -192,6 +205,8 @@ def _scale_shape(rows, cols, block):
 def _elsewhere(device, stream):
     """None where a call can run on the current device and stream, else the context in which it can."""
     if stream is not None:
+        if not isinstance(stream, torch.cuda.Stream):
+            raise TypeError(f"stream: a torch.cuda.Stream is needed, not {stream!r}")
         if stream.device.index != device:
             raise TypeError(f"a stream of {stream.device} for tensors on cuda:{device}")
         return torch.cuda.stream(stream)
@@ -248,7 +263,8 @@ def quantize(x, block=0, pow2=False, out=None, stream=None):
     kind = _float_type(x.dtype, "x")
     ldx = _matrix(x, "x", x.dtype, device)
     rows, cols = x.shape
-    shape = _scale_shape(rows, cols, _block(block))
+    block = _block(block)
+    shape = _scale_shape(rows, cols, block)
     if out is None:
         codes, scales = _new_codes(rows, cols, x), x.new_empty(shape, dtype=torch.float32)
         ldc = codes.stride(0) or 1
@@ -270,7 +286,8 @@ def dequantize(codes, scales, block=0, dtype=torch.bfloat16, out=None, stream=No
             return dequantize(codes, scales, block, dtype, out)
     ldc = _matrix(codes, "codes", torch.int8, device)
     rows, cols = codes.shape
-    _vector(scales, "scales", torch.float32, device, _scale_shape(rows, cols, _block(block)))
+    block = _block(block)
+    _vector(scales, "scales", torch.float32, device, _scale_shape(rows, cols, block))
     if out is None:
         kind, out, ldx = _float_type(dtype, "dtype"), codes.new_empty((rows, cols), dtype=dtype), cols
     else:
@@ -303,6 +320,7 @@ def rms_norm(x, gain, residual=None, eps=1e-6, pow2=False, checkpoint=0, hidden=
     ldx = _matrix(x, "x", dtype, device)
     rows, cols = x.shape
     _vector(gain, "gain", dtype, device, (cols,))
+    eps, checkpoint = _number(eps, "eps"), _block(checkpoint, "checkpoint")
     ldr = ldh = ldk = 0
     at_residual = at_hidden = at_kept = at_kept_scales = 0
     if residual is not None:
@@ -319,7 +337,7 @@ def rms_norm(x, gain, residual=None, eps=1e-6, pow2=False, checkpoint=0, hidden=
     kept = kept_scales = None
     if checkpoint:
         kept = _new_codes(rows, cols, x)
-        kept_scales = x.new_empty(_scale_shape(rows, cols, _block(checkpoint, "checkpoint")), dtype=torch.float32)
+        kept_scales = x.new_empty(_scale_shape(rows, cols, checkpoint), dtype=torch.float32)
         at_kept, ldk, at_kept_scales = kept.data_ptr(), kept.stride(0), kept_scales.data_ptr()
     a = _norm_args(kind, POW2 if pow2 else AMAX_DIV_127, checkpoint, rows, cols, eps, x.data_ptr(), ldx, at_residual, ldr, gain.data_ptr(),
                     at_hidden, ldh, codes.data_ptr(), codes.stride(0), scales.data_ptr(), rstd.data_ptr(), at_kept, ldk, at_kept_scales)
@@ -340,7 +358,8 @@ def rms_norm_backward(dy, checkpoint, checkpoint_scales, rstd, gain, block=128, 
     ldy = _matrix(dy, "dy", dtype, device)
     rows, cols = dy.shape
     ldk = _matrix(checkpoint, "checkpoint", torch.int8, device, (rows, cols))
-    _vector(checkpoint_scales, "checkpoint_scales", torch.float32, device, _scale_shape(rows, cols, _block(block)))
+    block = _block(block)
+    _vector(checkpoint_scales, "checkpoint_scales", torch.float32, device, _scale_shape(rows, cols, block))
     _vector(rstd, "rstd", torch.float32, device, (rows,))
     _vector(gain, "gain", dtype, device, (cols,))
     ldr = at_dresidual = 0

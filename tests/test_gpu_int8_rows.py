@@ -294,3 +294,29 @@ def test_refusals():
             call()
     with pytest.raises(fmm.FmmError):
         int8.rms_norm(x, x[0], eps=-1.0)
+
+
+def test_refusals_of_numbers_and_streams():
+    """Arguments that are no tensors: the errors that the binding states, not those of its packing."""
+    x = torch.zeros(4, 64, device="cuda")
+    codes, scales = int8.quantize(x)
+    for call in (lambda: int8.rms_norm(x, x[0], checkpoint=None), lambda: int8.rms_norm(x, x[0], checkpoint=32.0), lambda: int8.rms_norm(x, x[0], eps=None),
+                 lambda: int8.rms_norm(x, x[0], eps="small"), lambda: int8.quantize(x, block=None), lambda: int8.quantize(x, block=32.0),
+                 lambda: int8.dequantize(codes, scales, block="32"), lambda: int8.rms_norm_backward(x, codes, scales, scales, x[0], block=None),
+                 lambda: int8.quantize(x, stream=0), lambda: int8.dequantize(codes, scales, dtype=None), lambda: int8.matmul(codes, scales, codes, scales, stream="s")):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: int8.rms_norm(x, x[0], checkpoint=64), lambda: int8.rms_norm_backward(x, codes, scales, scales, x[0], block=-1)):
+        with pytest.raises(ValueError):
+            call()
+    for eps in (float("nan"), float("inf"), -1):
+        with pytest.raises(fmm.FmmError):
+            int8.rms_norm(x, x[0], eps=eps)
+    n = int8.rms_norm(x, x[0], eps=np.float32(1e-6), checkpoint=np.int64(32))
+    assert n.checkpoint_scales.shape == (4, 2)
+
+
+def test_nothing_is_recorded_for_autograd():
+    w = torch.nn.Parameter(torch.randn(4, 64, device="cuda"))
+    codes, scales = int8.quantize(w)
+    assert not scales.requires_grad and not int8.dequantize(codes, scales).requires_grad
