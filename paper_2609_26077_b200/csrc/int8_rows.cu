@@ -1081,7 +1081,7 @@ dim3 flat_block(int cols)
 // (a block per row instead of 32 blocks an SM: 16384 x 8192 bf16 quantized in 77.7 instead of 74.2 us, restored in 68.0 instead of 63.8)
 unsigned flat_grid(int rows, dim3 block)
 {
-    constexpr int64_t most = 148 * 32;
+    const int64_t most = (int64_t)int8_sm_count() * 32;
     const int64_t need = ((int64_t)rows + block.z - 1) / block.z;
     return (unsigned)(need < most ? need : most);
 }
