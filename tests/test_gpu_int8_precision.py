@@ -1,5 +1,11 @@
 """How exactly the gradients of the 8-bit product hold what the 8-bit forms stand for: fp32 gradients in fp32 whatever the scales, 16-bit
 ones up to their own rounding, fp16 values without leaving its range."""
+import json
+import os
+import subprocess
+import sys
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -10,6 +16,7 @@ from test_gpu_int8_product import codes_of, padded, scales_of
 
 pytestmark = pytest.mark.gpu
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 MAX_PARTS = 3
 
 
@@ -182,3 +189,126 @@ def test_rounded_values_on_request(dtype, out_type):
                 if dtype is torch.float16:
                     bound = bound + 2.0 ** -25 * 1.01 * (d.abs().sum(0)[:, None] if got is dw else d.abs().sum(1)[:, None])
                 O.close(O.host(got), want.cpu().numpy(), bound.cpu().numpy())
+
+
+# ------------------------------------------------------------------------------------------------ the chains of kernels
+CHAINS = [(torch.bfloat16, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32), (torch.float16, torch.float16)]
+
+
+def both(dy, x, sx, w, sw, out_type, **how):
+    return int8.grad_weight(dy, x, sx, dtype=out_type, **how), int8.grad_input(dy, w, sw, dtype=out_type, **how)
+
+
+def case(M, N, K, dtype, seed, pow2=False, dy_offset=0):
+    dy = torch.randn(M, N, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+    return [O.strided(dy, 3, dy_offset) if dy_offset else dy, padded(codes_of(M, K, seed)), cuda(scales_of(M, seed, pow2)),
+            padded(codes_of(N, K, seed + 1)), cuda(scales_of(N, seed + 1, pow2))]
+
+
+@pytest.mark.parametrize("dy_offset", [0, 1])
+@pytest.mark.parametrize("dtype,out_type", CHAINS)
+def test_captured_and_replayed(dtype, out_type, dy_offset):
+    """Two graphs of the same calls, replayed on inputs that change in between (default scales, powers of two, others), eager calls on the same
+    stream between them: the bits of eager calls."""
+    M, N, K = 300, 520, 384
+    sources = [case(M, N, K, dtype, 1, False, dy_offset), case(M, N, K, dtype, 2, True, dy_offset), case(M, N, K, dtype, 3, False, dy_offset)]
+    want = [both(*c, out_type) for c in sources]
+    held = case(M, N, K, dtype, 4, False, dy_offset)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        both(*held, out_type)
+    torch.cuda.current_stream().wait_stream(s)
+    graphs, outs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            outs.append(both(*held, out_type))
+    for i in (0, 1, 2, 0):
+        for t, src in zip(held, sources[i]):
+            t.copy_(src)
+        graphs[0].replay()
+        both(*sources[1], out_type)
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for got in outs:
+            assert torch.equal(got[0], want[i][0]) and torch.equal(got[1], want[i][1])
+    assert int8.status() == (0, 0)
+
+
+def test_threads_and_streams_at_once():
+    cases = [(case(300 + 64 * i, 520, 384 + 8 * i, dtype, i, pow2, offset), out_type)
+             for i, ((dtype, out_type), pow2, offset) in enumerate(zip(CHAINS, (False, True, False, False), (0, 1, 1, 0)))]
+    want = [both(*c, t) for c, t in cases]
+    torch.cuda.synchronize()
+    bad = []
+
+    def run(i):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            for _ in range(30):
+                got = both(*cases[i][0], cases[i][1])
+                s.synchronize()
+                if not (torch.equal(got[0], want[i][0]) and torch.equal(got[1], want[i][1])):
+                    bad.append(i)
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(len(cases))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad and int8.status() == (0, 0)
+
+
+def test_alignment_of_dy_leaves_no_trace():
+    for dtype, out_type in CHAINS:
+        aligned = case(140, 203, 150, dtype, 5)
+        want = both(*aligned, out_type)
+        for extra, offset in ((3, 1), (5, 2), (8, 0)):
+            got = both(O.strided(aligned[0], extra, offset), *aligned[1:], out_type)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_rows_of_dy_that_fit_no_registers():
+    """Rows of more than 16384 columns are read twice: the same numbers as those of short rows, whose products they are sums of."""
+    M, N, K = 3, 16384 + 40, 24
+    dy, _, _, w, sw = case(M, N, K, torch.bfloat16, 6)
+    v = w.double() * sw.double()[:, None]
+    for offset in (0, 1):
+        dx = int8.grad_input(O.strided(dy, 3, offset) if offset else dy, w, sw)
+        want, size = dy.double() @ v, dy.double().abs() @ v.abs()
+        floor = (dy.double() * sw.double()).abs().max(1).values[:, None] * 2.0 ** -39 * w.double().abs().sum(0)
+        bound = (2.0 ** -12 + 8192 * 2 * O.U32 + 4 * O.U32) * size + floor + 1.01 * O.U[torch.bfloat16] * want.abs()
+        O.close(O.host(dx), want.cpu().numpy(), bound.cpu().numpy())
+        assert (dx.double() - want).norm() <= 1.03 * (want.bfloat16().double() - want).norm()
+
+
+CHILD = r"""
+import json, sys
+import torch
+sys.path[:0] = [%(root)r, %(root)r + "/tests"]
+from paper_2609_26077_b200 import build, fmm, int8
+build.build(debug=True)
+import test_gpu_int8_forms as F
+import test_gpu_int8_precision as P
+import test_gpu_int8_rows as R
+assert fmm.lib().fmm_debug_build() == 1
+P.test_fp32_gradients_are_fp32(65, 63, 129, "mixed", torch.float16)
+P.test_fp32_gradients_are_fp32(300, 290, 257, "default", torch.bfloat16)
+P.test_16_bit_gradients_up_to_their_rounding(257, 512, 1000, torch.bfloat16)
+P.test_16_bit_gradients_up_to_their_rounding(257, 512, 1000, torch.float16)
+P.test_alignment_of_dy_leaves_no_trace()
+P.test_rows_of_dy_that_fit_no_registers()
+R.test_rows_without_columns_touch_nothing(torch.bfloat16, True)
+for form in F.GRAD_FORMS:
+    F.test_gradient(form, int8.GRAD_WEIGHT)
+    F.test_gradient(form, int8.GRAD_INPUT)
+for form in F.PRODUCT_FORMS:
+    F.test_product(form)
+print("RESULT", json.dumps(int8.status()))
+"""
+
+
+def test_no_store_outside_its_range():
+    r = subprocess.run([sys.executable, "-c", CHILD % {"root": ROOT}], capture_output=True, text=True, timeout=900, env=dict(os.environ, FMM_B200_DEBUG="1"))
+    assert r.returncode == 0, r.stderr[-3000:]
+    line = [ln for ln in r.stdout.splitlines() if ln.startswith("RESULT ")][-1]
+    assert json.loads(line[len("RESULT "):]) == [0, 0]
