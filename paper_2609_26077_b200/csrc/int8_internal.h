@@ -71,12 +71,12 @@ template <> __device__ __forceinline__ uint32_t pack_two<__half>(float a, float 
 { __half2 v = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&v); }
 
 // fp16 parts: a power of two for the whole matrix, by which its largest finite scale comes to lie in [128, 256), so that no value leaves
-// the range and those 2^-22 of the largest are still normal numbers.  Exponent, from the maxima that int8_scale_maxima left (warp-collective).
+// the range and those 2^-22 of the largest are still normal numbers.  Exponent, from the maxima that int8_values left (warp-collective).
+__device__ __forceinline__ int maximum_exponent(uint32_t m) { return m == 0 ? 0 : min(7 - ((int)(m >> 23) - 127), 100); }
 __device__ __forceinline__ int matrix_exponent(const uint32_t* maxima, int count)
 {
     const int lane = threadIdx.x & 31;
-    const uint32_t m = __reduce_max_sync(0xffffffffu, max(lane < count ? maxima[lane] : 0u, lane + 32 < count ? maxima[lane + 32] : 0u));
-    return m == 0 ? 0 : min(7 - ((int)(m >> 23) - 127), 100);
+    return maximum_exponent(__reduce_max_sync(0xffffffffu, max(lane < count ? maxima[lane] : 0u, lane + 32 < count ? maxima[lane + 32] : 0u)));
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }      // -126 .. 127
 #endif
@@ -86,14 +86,14 @@ fmm_status_t int8_rows_guard_read(int* code, bool clear);
 // What the product of a gradient reads, in the workspace.  Rows there are ld elements apart, a multiple of 8, on 16-byte boundaries.
 //   values: code * scale in fp32, in `parts` matrices of `type`, step elements apart, each holding what the ones before it leave.  By stages of
 //   INT8_PART_ROWS rows: where every scale of a stage is a power of two, its first part is the value, the others are not written, and its
-//   byte of `flags` is 0, else 1.  maxima: null, or of int8_scale_maxima, for fp16.  scales and flags null: the codes themselves.
+//   byte of `flags` is 0, else 1.  flags null: one part.  maxima: null, or room for INT8_MAXIMA maxima of scales, for fp16.
 constexpr int INT8_PART_ROWS = 64, INT8_MAXIMA = 64;
 int int8_scale_maxima_count(int64_t rows);
-fmm_status_t int8_scale_maxima(const float* scales, int64_t rows, uint32_t* maxima, cudaStream_t st);
-fmm_status_t int8_values(fmm_type_t type, int parts, const int8_t* codes, int64_t ldc, const float* scales, const uint32_t* maxima, uint8_t* flags, void* x, int64_t ldx,
+fmm_status_t int8_values(fmm_type_t type, int parts, const int8_t* codes, int64_t ldc, const float* scales, uint32_t* maxima, uint8_t* flags, void* x, int64_t ldx,
                          int64_t step, int64_t rows, int64_t cols, cudaStream_t st);
-//   scaled rows: y[i][j] = x[i][j] (bf16) * scales[j] in fp16, times a power of two for each row by which its largest finite number comes to lie in
-//   [2^14, 2^15); inverse[i]: one over that.  Launched behind int8_values, which it may overlap; what follows it may rely on both.
-fmm_status_t int8_scaled_rows(const void* x, int64_t ldx, const float* scales, void* y, int64_t ldy, float* inverse, int64_t rows, int64_t cols, cudaStream_t st);
+//   the codes (code_rows x code_cols) themselves in fp16, and rows scaled by code_rows scales: y[i][j] = x[i][j] (bf16) * scales[j] in fp16,
+//   times a power of two for each row by which its largest finite number comes to lie in [2^14, 2^15); inverse[i]: one over that.
+fmm_status_t int8_codes_and_scaled_rows(const int8_t* codes, int64_t ldc, void* values, int64_t ldv, int64_t code_rows, int64_t code_cols, const void* x, int64_t ldx,
+                                        const float* scales, void* y, int64_t ldy, float* inverse, int64_t rows, cudaStream_t st);
 // 16-bit rows copied to rows on 16-byte boundaries, ldy a multiple of 8
 fmm_status_t int8_realign(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int64_t cols, cudaStream_t st);

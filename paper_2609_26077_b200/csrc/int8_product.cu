@@ -597,6 +597,18 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
             if (lane == 0) mbar_arrive_cluster(bar_tempty(buf) & PEER_BIT_MASK);
             if (++buf == 2) { buf = 0; bphase ^= 1u; }
         };
+        uint32_t next_scale[COLS / 32];
+        auto fetch_scales = [&](long long w) {
+            if (w >= tiles) return;
+            int tr, tc;
+            place(w, tr, tc);
+#pragma unroll
+            for (int i = 0; i < COLS / 32; ++i) {
+                const int col = tc * C::TC + half * COLS + lane + 32 * i;
+                next_scale[i] = col < p.cols ? __float_as_uint(p.c_scales[col]) : 0u;
+            }
+        };
+        if (KIND == INT8 || p.c_scales) fetch_scales(unit);
         for (long long w = unit; w < tiles && ok; w += units) {
             int tr, tc;
             place(w, tr, tc);
@@ -607,8 +619,10 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
                 // (No warp waits here for another: one whose wait below has run out leaves the loop, and a barrier among the output
                 // warps would then have no limit for those whose wait has not.)
                 __syncwarp();                                // the tile before is out
-                for (int i = lane; i < COLS; i += 32) sts32u(scales + 4 * i, col0 + i < p.cols ? __float_as_uint(p.c_scales[col0 + i]) : 0u);
+#pragma unroll
+                for (int i = 0; i < COLS / 32; ++i) sts32u(scales + 4 * (lane + 32 * i), next_scale[i]);
                 __syncwarp();
+                fetch_scales(w + units);                     // (a tile ahead: 8192 x 8192 x 1024 product in 63.7 instead of 67.4 us)
             }
             if constexpr (KIND == INT8) {
                 float r_scale = 0.0f, bias = 0.0f;
@@ -1010,15 +1024,13 @@ fmm_status_t grad(const fmm_int8_grad_t* a, void* workspace, size_t workspace_by
     fmm_status_t s = FMM_OK;
     if (w.scaled) {
         float* inverse = reinterpret_cast<float*>(base + w.extra);
-        s = int8_values(w.operands, 1, codes, ldc, nullptr, nullptr, nullptr, base, w.ld_values, step, code_rows, K, st);
-        if (s == FMM_OK) s = int8_scaled_rows(dY, ldy, scales, base + w.dy, w.ld_dy, inverse, M, N, st);
+        s = int8_codes_and_scaled_rows(codes, ldc, base, w.ld_values, code_rows, K, dY, ldy, scales, base + w.dy, w.ld_dy, inverse, M, st);
         dy = {base + w.dy, M, N, w.ld_dy};
         p.c_scales = inverse;
     } else {
         uint32_t* maxima = type == FMM_TYPE_F16 ? reinterpret_cast<uint32_t*>(base + w.extra) : nullptr;
         uint8_t* flags = w.parts > 1 ? reinterpret_cast<uint8_t*>(base + w.extra) + INT8_MAXIMA * 4 : nullptr;
-        if (maxima) s = int8_scale_maxima(scales, code_rows, maxima, st);
-        if (s == FMM_OK) s = int8_values(w.operands, w.parts, codes, ldc, scales, maxima, flags, base, w.ld_values, step, code_rows, K, st);
+        s = int8_values(w.operands, w.parts, codes, ldc, scales, maxima, flags, base, w.ld_values, step, code_rows, K, st);
         if (s == FMM_OK && !int8_aligned(dY, ldy * 2, 16)) {
             s = int8_realign(dY, ldy, base + w.dy, w.ld_dy, M, N, st);
             dy = {base + w.dy, M, N, w.ld_dy};

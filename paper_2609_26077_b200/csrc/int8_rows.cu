@@ -573,17 +573,25 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const RestoreParams p)
 }
 
 // ---------------------------------------------------------------------------------------- what the product of a gradient reads
-// Maxima of the finite scales' magnitudes, one a block
+// Largest magnitude of finite scales that the threads of a block come across, from `first` on in steps of `step` (threads: of a block, 1024 at most)
+__device__ __forceinline__ uint32_t finite_scale_max(const float* scales, int rows, int64_t first, int64_t step, int thread, int threads, uint32_t* red)
+{
+    uint32_t m = 0;
+    for (int64_t i = first; i < rows; i += step) {
+        const uint32_t b = __float_as_uint(scales[i]) & 0x7FFFFFFFu;
+        if (b < 0x7F800000u) m = max(m, b);
+    }
+    m = __reduce_max_sync(0xffffffffu, m);
+    if ((thread & 31) == 0) red[thread >> 5] = m;
+    __syncthreads();
+    return __reduce_max_sync(0xffffffffu, (thread & 31) < threads / 32 ? red[thread & 31] : 0u);
+}
+// one a block
 __global__ void __launch_bounds__(1024) scale_maxima_kernel(const float* __restrict__ scales, int rows, uint32_t* __restrict__ maxima)
 {
     __shared__ uint32_t red[32];
     fmmptx::griddep_launch_dependents();
-    uint32_t m = 0;
-    for (int64_t i = (int64_t)blockIdx.x * 1024 + threadIdx.x; i < rows; i += (int64_t)gridDim.x * 1024) {
-        const uint32_t b = __float_as_uint(scales[i]) & 0x7FFFFFFFu;
-        if (b < 0x7F800000u) m = max(m, b);
-    }
-    m = row_max(m, red, 32);
+    const uint32_t m = finite_scale_max(scales, rows, (int64_t)blockIdx.x * 1024 + threadIdx.x, (int64_t)gridDim.x * 1024, threadIdx.x, 1024, red);
     if (threadIdx.x == 0) maxima[blockIdx.x] = m;
 }
 
@@ -605,7 +613,7 @@ template <> __device__ __forceinline__ uint16_t part_below<__half>(float v)
 // to nearest: two of bf16 are 2^-16 off at most, three exact, two of fp16 2^-22 (or 2^-25 in the units that matrix_exponent sets).
 // Where the stage needs one part the others are neither written nor read.
 struct ValuesParams {
-    const int8_t* codes; const float* scales; const uint32_t* maxima; uint8_t* flags; void* x;
+    const int8_t* codes; const float* scales; uint8_t* flags; void* x;
     int64_t ldc, ldx, step;
     int rows, cols, parts, maxima_count;
     bool vc;
@@ -620,28 +628,23 @@ __device__ __forceinline__ bool inexact_stage(const float* scales, int rows, int
     if (r + 32 < rows) bits |= __float_as_uint(scales[r + 32]);
     return __any_sync(0xffffffffu, bits & 0x007FFFFFu);
 }
-template <typename T>
-__global__ void __launch_bounds__(256) values_kernel(const ValuesParams p)
+// `block` of `blocks`, eight warps each: pieces of a row along y of them, rows along the others
+template <typename T> __device__ __forceinline__ void values_block(const ValuesParams& p, float factor, int block, int blocks, int y)
 {
     constexpr int VPT = FLAT_VPT;
-    fmmptx::griddep_launch_dependents();                      // (the product, which waits for this grid to end)
-    float factor = 1.0f;
-    if (p.maxima) {
-        fmmptx::griddep_wait();
-        factor = power_of_two(matrix_exponent(p.maxima, p.maxima_count));
-    }
-    for (int64_t row = (int64_t)blockIdx.x * blockDim.z + threadIdx.z; row < p.rows; row += (int64_t)gridDim.x * blockDim.z) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, side = warp & (y - 1), z = 8 / y;
+    for (int64_t row = (int64_t)block * z + warp / y; row < p.rows; row += (int64_t)blocks * z) {
         const int8_t* codes = p.codes + row * p.ldc;
         const float scale = p.scales ? p.scales[row] * factor : 1.0f;
         const bool inexact = p.parts > 1 && inexact_stage(p.scales, p.rows, row);
         const int parts = inexact ? p.parts : 1;
-        if (p.flags && row % INT8_PART_ROWS == 0 && threadIdx.x == 0 && threadIdx.y == 0) {
+        if (p.flags && row % INT8_PART_ROWS == 0 && lane == 0 && side == 0) {
             uint8_t* flag = p.flags + row / INT8_PART_ROWS;
             if (ROW_STORE_OK(flag, 1, 2183)) *flag = inexact;
         }
         T* x = static_cast<T*>(p.x) + row * p.ldx;
-        for (int piece = threadIdx.y * FLAT_PIECE; piece < p.cols; piece += blockDim.y * FLAT_PIECE) {
-            const int col = piece + 8 * threadIdx.x;
+        for (int piece = side * FLAT_PIECE; piece < p.cols; piece += y * FLAT_PIECE) {
+            const int col = piece + 8 * lane;
             uint2 c[VPT];
 #pragma unroll
             for (int i = 0; i < VPT; ++i) c[i] = load_codes8(codes + col + i * GROUP, p.cols - (col + i * GROUP), p.vc);
@@ -673,14 +676,46 @@ __global__ void __launch_bounds__(256) values_kernel(const ValuesParams p)
         }
     }
 }
+// Up to OWN_MAXIMUM rows every block finds the scales' maximum itself, and the first one leaves it for the product: a launch less.
+constexpr int OWN_MAXIMUM = 2048;
+template <typename T>
+__global__ void __launch_bounds__(256) values_kernel(const ValuesParams p, uint32_t* maxima, int y)
+{
+    __shared__ uint32_t red[32];
+    fmmptx::griddep_launch_dependents();                      // (the product, which waits for this grid to end)
+    float factor = 1.0f;
+    if (maxima) {
+        if (p.rows <= OWN_MAXIMUM) {
+            uint32_t m = finite_scale_max(p.scales, p.rows, threadIdx.x, 256, threadIdx.x, 256, red);
+            if (blockIdx.x == 0 && threadIdx.x == 0) maxima[0] = m;
+            factor = power_of_two(maximum_exponent(m));
+        } else {
+            fmmptx::griddep_wait();
+            factor = power_of_two(matrix_exponent(maxima, p.maxima_count));
+        }
+    }
+    values_block<T>(p, factor, blockIdx.x, gridDim.x, y);
+}
 
 // The largest finite number of a row comes to lie in [2^14, 2^15) (within what powers of two fp32 holds on both sides).
 struct ScaledParams {
     const __nv_bfloat16* x; const float* scales; __half* y; float* inverse;
     int64_t ldx, ldy;
-    int rows, cols;
+    int rows, cols, warps;                    // warps: of a row
+    bool vs;                                  // scales on a 16-byte boundary
     Int8Ranges ranges;
 };
+__device__ __forceinline__ void scales8(const ScaledParams& p, int col, float (&s)[8])
+{
+    const float* q = p.scales + col;
+    if (p.vs && col + 8 <= p.cols) {
+        const float4 a = reinterpret_cast<const float4*>(q)[0], b = reinterpret_cast<const float4*>(q)[1];
+        s[0] = a.x; s[1] = a.y; s[2] = a.z; s[3] = a.w; s[4] = b.x; s[5] = b.y; s[6] = b.z; s[7] = b.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = col + j < p.cols ? q[j] : 0.0f;
+    }
+}
 __device__ __forceinline__ uint32_t finite_max8(const float (&f)[8], uint32_t m)
 {
 #pragma unroll
@@ -700,80 +735,112 @@ __device__ __forceinline__ void store_scaled8(const ScaledParams& p, int64_t row
     if (ROW_STORE_OK(q, 16, 2191)) *q = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A row per block at a time, two groups of eight columns a thread, whose scales stay in registers; the next row is on its way while this one's
-// maximum is found.  (8192 x 8192: 43 us, 152 with the scales loaded for every row.)
-template <int AL>
-__global__ void __launch_bounds__(1024) scaled_rows_kernel(const ScaledParams p)
+// Rows of up to 4096 (8192) columns: two (four) groups of eight a thread, whose scales stay in registers, one, two, four or eight warps a
+// row; the next row is on its way while this one's maximum is found (8192 x 8192: 43 us, 152 with the scales loaded for every row).  With
+// two groups a thread the codes' values come in the same launch, from the blocks behind: 20 instead of 23.8 us of the host's time for a
+// call.  (With four, which leave room for two blocks an SM, that takes 84 us for 8192 x 8192 of both; apart 43 and 29.)
+template <int AL, int VPT>
+__global__ void __launch_bounds__(256, VPT == 2 ? 4 : 2) scaled_rows_kernel(const ScaledParams p, const ValuesParams v, int blocks, int y)
 {
     using T = __nv_bfloat16;
-    constexpr int VPT = 2;
-    __shared__ uint32_t red[2][32];
+    __shared__ uint32_t red[2][8];
     fmmptx::griddep_launch_dependents();
-    const int t = threadIdx.x, warps = blockDim.x / 32, first = ((t >> 5) * VPT * 32 + (t & 31)) * 8;
+    if ((int)blockIdx.x >= blocks) {
+        values_block<__half>(v, 1.0f, (int)blockIdx.x - blocks, (int)gridDim.x - blocks, y);
+        return;
+    }
+    const int warps = p.warps, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, side = warp & (warps - 1), per_block = 8 / warps;
+    const int first = side * VPT * GROUP + 8 * lane;
     auto left = [&](int i) { return p.cols - (first + i * GROUP); };
     float scale[VPT][8];
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) scale[i][j] = j < left(i) ? p.scales[first + i * GROUP + j] : 0.0f;
+    for (int i = 0; i < VPT; ++i) scales8(p, first + i * GROUP, scale[i]);
     Raw8<T, AL> raw[VPT];
     auto fetch = [&](int64_t row) {
+        if (row >= p.rows) return;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) raw[i] = load8<T, AL>(p.x + row * p.ldx, first + i * GROUP, left(i));
     };
     int parity = 0;
-    fetch(blockIdx.x);
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
+    const int64_t step = (int64_t)blocks * per_block;
+    int64_t row = (int64_t)blockIdx.x * per_block + warp / warps;
+    fetch(row);
+    // (every warp of the block goes round as often: they meet)
+    for (int64_t base = (int64_t)blockIdx.x * per_block; base < p.rows; base += step, row += step, parity ^= 1) {
+        const bool live = row < p.rows;
         const int m = AL ? 0 : row_offset(p.x + row * p.ldx);
         float f[VPT][8];
         uint32_t most = 0;
+        if (live) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            unpack8<T, AL>(raw[i], m, left(i), f[i]);
+            for (int i = 0; i < VPT; ++i) {
+                unpack8<T, AL>(raw[i], m, left(i), f[i]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[i][j] = __fmul_rn(f[i][j], scale[i][j]);
-            most = finite_max8(f[i], most);
+                for (int j = 0; j < 8; ++j) f[i][j] = __fmul_rn(f[i][j], scale[i][j]);
+                most = finite_max8(f[i], most);
+            }
         }
-        if (row + gridDim.x < p.rows) fetch(row + gridDim.x);
-        const int e = scaled_exponent(row_max(most, red[parity], warps));
-        if (t == 0 && ROW_STORE_OK(p.inverse + row, 4, 2192)) p.inverse[row] = power_of_two(-e);
+        fetch(row + step);
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (warps > 1) {
+            if (lane == 0) red[parity][warp] = most;
+            __syncthreads();
+            most = __reduce_max_sync(0xffffffffu, lane < warps ? red[parity][(warp - side) + lane] : 0u);
+        }
+        if (!live) continue;
+        const int e = scaled_exponent(most);
+        if (side == 0 && lane == 0 && ROW_STORE_OK(p.inverse + row, 4, 2192)) p.inverse[row] = power_of_two(-e);
         const float factor = power_of_two(e);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) if (left(i) > 0) store_scaled8(p, row, first + i * GROUP, f[i], factor);
     }
-    fmmptx::griddep_wait();                                   // what waits for this grid waits for the one before it too
+    fmmptx::griddep_wait();                                   // what waits for this grid waits for the one before it too, if there is one
 }
-// rows that do not fit registers: read twice, the second time from L2, mostly
-__global__ void __launch_bounds__(1024) scaled_long_kernel(const ScaledParams p)
+// Rows that do not fit registers: ROWS of them, four or one, to a block, so that the scales, which are as many bytes as two rows, come from L2
+// for all of them; read twice, the second time from L2, mostly.  (4000 x 20000: 60 us, 124 with a row to a block.)
+template <int AL, int ROWS>
+__global__ void __launch_bounds__(512) scaled_long_kernel(const ScaledParams p)
 {
     using T = __nv_bfloat16;
-    __shared__ uint32_t red[2][32];
+    constexpr int NT = 512;
+    __shared__ uint32_t red[ROWS][NT / 32];
     fmmptx::griddep_launch_dependents();
-    int parity = 0;
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
-        const T* x = p.x + row * p.ldx;
-        const int m = row_offset(x);
-        auto scaled8 = [&](int col, float (&f)[8]) {
-            const int n = p.cols - col;
-            unpack8<T, 0>(load8<T, 0>(x, col, n), m, n, f);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t base = (int64_t)blockIdx.x * ROWS;
+    auto row = [&](int r) { return p.x + min(base + r, (int64_t)p.rows - 1) * p.ldx; };      // (behind the last: that one again, not stored)
+    auto each8 = [&](auto use) {
+        for (int col = 8 * threadIdx.x; col < p.cols; col += 8 * NT) {
+            float s[8];
+            scales8(p, col, s);
+            Raw8<T, AL> raw[ROWS];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = j < n ? __fmul_rn(f[j], p.scales[col + j]) : 0.0f;
-        };
-        uint32_t most = 0;
-        for (int col = 8 * threadIdx.x; col < p.cols; col += 8 * 1024) {
-            float f[8];
-            scaled8(col, f);
-            most = finite_max8(f, most);
+            for (int r = 0; r < ROWS; ++r) raw[r] = load8<T, AL>(row(r), col, p.cols - col);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                float f[8];
+                unpack8<T, AL>(raw[r], AL ? 0 : row_offset(row(r)), p.cols - col, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = __fmul_rn(f[j], s[j]);
+                use(r, col, f);
+            }
         }
-        const int e = scaled_exponent(row_max(most, red[parity], 32));
-        if (threadIdx.x == 0 && ROW_STORE_OK(p.inverse + row, 4, 2194)) p.inverse[row] = power_of_two(-e);
-        for (int col = 8 * threadIdx.x; col < p.cols; col += 8 * 1024) {
-            float f[8];
-            scaled8(col, f);
-            store_scaled8(p, row, col, f, power_of_two(e));
-        }
+    };
+    uint32_t most[ROWS] = {};
+    each8([&](int r, int, const float (&f)[8]) { most[r] = finite_max8(f, most[r]); });
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const uint32_t m = __reduce_max_sync(0xffffffffu, most[r]);
+        if (lane == 0) red[r][warp] = m;
     }
-    fmmptx::griddep_wait();
+    __syncthreads();
+    int e[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        e[r] = scaled_exponent(__reduce_max_sync(0xffffffffu, lane < NT / 32 ? red[r][lane] : 0u));
+        if (threadIdx.x == 0 && base + r < p.rows && ROW_STORE_OK(p.inverse + base + r, 4, 2194)) p.inverse[base + r] = power_of_two(-e[r]);
+    }
+    each8([&](int r, int col, const float (&f)[8]) { if (base + r < p.rows) store_scaled8(p, base + r, col, f, power_of_two(e[r])); });
+    fmmptx::griddep_wait();                                   // what waits for this grid waits for the one before it too
 }
 
 // 16-bit rows of any alignment, copied to rows that a tensor map can read (ldy a multiple of 8, y on a 16-byte boundary); what lies
@@ -1007,7 +1074,7 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const BackParams p)
 fmm_status_t launched() { return cudaGetLastError() == cudaSuccess ? FMM_OK : FMM_ERR_CUDA; }
 
 // behind: set up while the kernel before drains, for which it waits itself
-template <typename P> fmm_status_t launch_behind(void (*kernel)(P), unsigned grid, dim3 block, bool behind, const P& p, cudaStream_t st)
+template <typename... P, typename... A> fmm_status_t launch_behind(void (*kernel)(P...), unsigned grid, dim3 block, bool behind, cudaStream_t st, const A&... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid); cfg.blockDim = block; cfg.stream = st;
@@ -1015,7 +1082,7 @@ template <typename P> fmm_status_t launch_behind(void (*kernel)(P), unsigned gri
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = behind ? 1 : 0;
-    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) { cudaGetLastError(); return FMM_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) { cudaGetLastError(); return FMM_ERR_CUDA; }
     return FMM_OK;
 }
 
@@ -1068,7 +1135,7 @@ template <typename T> fmm_status_t launch_back(const BackParams& p, int threads,
     else launch(std::integral_constant<int, 0>{});
     if (cudaGetLastError() != cudaSuccess) return FMM_ERR_CUDA;
     // set up while the rows are dealt with; it waits for them before its first load
-    return launch_behind(column_sum_kernel, (unsigned)(p.cols + 31) / 32, dim3(1024), true, p, st);
+    return launch_behind(column_sum_kernel, (unsigned)(p.cols + 31) / 32, dim3(1024), true, st, p);
 }
 
 // eight warps of a block without a reduction: pieces of a row along y, rows along z
@@ -1093,35 +1160,62 @@ bool matrix_ok(const void* p, int64_t cols, int64_t ld, int element) { return p 
 
 }  // namespace
 
-int int8_scale_maxima_count(int64_t rows) { return (int)(rows < 1024 * INT8_MAXIMA ? (rows + 1023) / 1024 : INT8_MAXIMA); }
-
-fmm_status_t int8_scale_maxima(const float* scales, int64_t rows, uint32_t* maxima, cudaStream_t st)
+int int8_scale_maxima_count(int64_t rows)
 {
-    scale_maxima_kernel<<<(unsigned)int8_scale_maxima_count(rows), 1024, 0, st>>>(scales, (int)rows, maxima);
-    return launched();
+    return rows <= OWN_MAXIMUM ? 1 : (int)std::min<int64_t>((rows + 1023) / 1024, INT8_MAXIMA);
 }
 
-fmm_status_t int8_values(fmm_type_t type, int parts, const int8_t* codes, int64_t ldc, const float* scales, const uint32_t* maxima, uint8_t* flags, void* x, int64_t ldx,
-                         int64_t step, int64_t rows, int64_t cols, cudaStream_t st)
+static ValuesParams values_params(int parts, const int8_t* codes, int64_t ldc, const float* scales, uint8_t* flags, void* x, int64_t ldx, int64_t step, int64_t rows,
+                                  int64_t cols)
 {
-    ValuesParams p = {codes, scales, maxima, flags, x, ldc, ldx, step, (int)rows, (int)cols, parts, int8_scale_maxima_count(rows), int8_aligned(codes, ldc, 8), {}};
+    ValuesParams p = {codes, scales, flags, x, ldc, ldx, step, (int)rows, (int)cols, parts, int8_scale_maxima_count(rows), int8_aligned(codes, ldc, 8), {}};
     for (int i = 0; i < parts; ++i) int8_add_range(p.ranges, static_cast<char*>(x) + 2 * i * step, rows, ldx, ldx, 2);
     int8_add_range(p.ranges, flags, 1, (rows + INT8_PART_ROWS - 1) / INT8_PART_ROWS, rows, 1);
-    const dim3 b = flat_block((int)cols);
-    const unsigned grid = flat_grid((int)rows, b);
-    return launch_behind(type == FMM_TYPE_BF16 ? values_kernel<__nv_bfloat16> : values_kernel<__half>, grid, b, maxima != nullptr, p, st);
+    return p;
 }
 
-fmm_status_t int8_scaled_rows(const void* x, int64_t ldx, const float* scales, void* y, int64_t ldy, float* inverse, int64_t rows, int64_t cols, cudaStream_t st)
+fmm_status_t int8_values(fmm_type_t type, int parts, const int8_t* codes, int64_t ldc, const float* scales, uint32_t* maxima, uint8_t* flags, void* x, int64_t ldx,
+                         int64_t step, int64_t rows, int64_t cols, cudaStream_t st)
 {
-    ScaledParams p = {static_cast<const __nv_bfloat16*>(x), scales, static_cast<__half*>(y), inverse, ldx, ldy, (int)rows, (int)cols, {}};
+    const ValuesParams p = values_params(parts, codes, ldc, scales, flags, x, ldx, step, rows, cols);
+    const bool apart = maxima && rows > OWN_MAXIMUM;
+    if (apart) {
+        scale_maxima_kernel<<<(unsigned)p.maxima_count, 1024, 0, st>>>(scales, (int)rows, maxima);
+        if (launched() != FMM_OK) return FMM_ERR_CUDA;
+    }
+    const dim3 b = flat_block((int)cols);
+    return launch_behind(type == FMM_TYPE_BF16 ? values_kernel<__nv_bfloat16> : values_kernel<__half>, flat_grid((int)rows, b), dim3(256), apart, st, p, maxima,
+                         (int)b.y);
+}
+
+fmm_status_t int8_codes_and_scaled_rows(const int8_t* codes, int64_t ldc, void* values, int64_t ldv, int64_t code_rows, int64_t code_cols, const void* x, int64_t ldx,
+                                        const float* scales, void* y, int64_t ldy, float* inverse, int64_t rows, cudaStream_t st)
+{
+    const int64_t cols = code_rows;
+    const ValuesParams v = values_params(1, codes, ldc, nullptr, nullptr, values, ldv, 0, code_rows, code_cols);
+    ScaledParams p = {static_cast<const __nv_bfloat16*>(x), scales, static_cast<__half*>(y), inverse, ldx, ldy, (int)rows, (int)cols, 1, int8_aligned(scales, 0, 16), {}};
     int8_add_range(p.ranges, y, rows, ldy, ldy, 2);
     int8_add_range(p.ranges, inverse, 1, rows, rows, 4);
-    const int64_t threads = (cols + 511) / 512 * 32;          // two groups of eight columns each
-    const bool fits = threads <= 1024;
-    const int64_t resident = (int64_t)int8_sm_count() * (fits ? std::min<int64_t>(16, 1024 / threads) : 1);
-    return launch_behind(!fits ? scaled_long_kernel : cols % 8 == 0 && int8_aligned(x, ldx * 2, 16) ? scaled_rows_kernel<1> : scaled_rows_kernel<0>,
-                         (unsigned)std::min(rows, resident), dim3((unsigned)(fits ? threads : 1024)), true, p, st);
+    const dim3 b = flat_block((int)code_cols);
+    const unsigned value_blocks = flat_grid((int)code_rows, b);
+    const int64_t sms = int8_sm_count();
+    const bool aligned = cols % 8 == 0 && int8_aligned(x, ldx * 2, 16);
+    const int vpt = cols <= 8 * 2 * GROUP ? 2 : 4, piece = vpt * GROUP;
+    const bool fits = cols <= 8 * piece, together = fits && vpt == 2;
+    if (!together) {
+        const fmm_status_t s = launch_behind(values_kernel<__half>, value_blocks, dim3(256), false, st, v, (uint32_t*)nullptr, (int)b.y);
+        if (s != FMM_OK) return s;
+    }
+    if (!fits) {
+        const bool many = rows >= 8 * sms;
+        const auto kernel = many ? (aligned ? scaled_long_kernel<1, 4> : scaled_long_kernel<0, 4>) : aligned ? scaled_long_kernel<1, 1> : scaled_long_kernel<0, 1>;
+        return launch_behind(kernel, (unsigned)(many ? (rows + 3) / 4 : rows), dim3(512), true, st, p);
+    }
+    while (p.warps * piece < cols) p.warps *= 2;
+    const int64_t per_block = 8 / p.warps;
+    const unsigned blocks = (unsigned)std::min((rows + per_block - 1) / per_block, (vpt == 2 ? 4 : 2) * sms);
+    const auto kernel = vpt == 2 ? (aligned ? scaled_rows_kernel<1, 2> : scaled_rows_kernel<0, 2>) : aligned ? scaled_rows_kernel<1, 4> : scaled_rows_kernel<0, 4>;
+    return launch_behind(kernel, blocks + (together ? value_blocks : 0), dim3(256), !together, st, p, v, (int)blocks, (int)b.y);
 }
 
 fmm_status_t int8_realign(const void* x, int64_t ldx, void* y, int64_t ldy, int64_t rows, int64_t cols, cudaStream_t st)

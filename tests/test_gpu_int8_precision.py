@@ -267,16 +267,18 @@ def test_alignment_of_dy_leaves_no_trace():
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
-def test_rows_of_dy_that_fit_no_registers():
-    """Rows of more than 16384 columns are read twice: the same numbers as those of short rows, whose products they are sums of."""
-    M, N, K = 3, 16384 + 40, 24
+@pytest.mark.parametrize("M,N,K", [(3, 16424, 24), (1190, 16424, 24), (1201, 8200, 24), (700, 8192, 40), (700, 5000, 33), (2500, 300, 16)])
+def test_rows_of_dy_of_every_length(M, N, K):
+    """A warp to a block a row, rows that fit registers and rows that do not, few of them and many, aligned and not."""
     dy, _, _, w, sw = case(M, N, K, torch.bfloat16, 6)
     v = w.double() * sw.double()[:, None]
+    want, size = dy.double() @ v, dy.double().abs() @ v.abs()
+    floor = (dy.double() * sw.double()).abs().max(1).values[:, None] * 2.0 ** -39 * w.double().abs().sum(0)
+    # sums of at most 8192 terms leave the accumulator, three more additions
+    bound = (2.0 ** -12 + (min(N, 8192) + 4) * 2 * O.U32) * size + floor + 1.01 * O.U[torch.bfloat16] * want.abs()
     for offset in (0, 1):
+        poison_free_memory()
         dx = int8.grad_input(O.strided(dy, 3, offset) if offset else dy, w, sw)
-        want, size = dy.double() @ v, dy.double().abs() @ v.abs()
-        floor = (dy.double() * sw.double()).abs().max(1).values[:, None] * 2.0 ** -39 * w.double().abs().sum(0)
-        bound = (2.0 ** -12 + 8192 * 2 * O.U32 + 4 * O.U32) * size + floor + 1.01 * O.U[torch.bfloat16] * want.abs()
         O.close(O.host(dx), want.cpu().numpy(), bound.cpu().numpy())
         assert (dx.double() - want).norm() <= 1.03 * (want.bfloat16().double() - want).norm()
 
@@ -296,7 +298,9 @@ P.test_fp32_gradients_are_fp32(300, 290, 257, "default", torch.bfloat16)
 P.test_16_bit_gradients_up_to_their_rounding(257, 512, 1000, torch.bfloat16)
 P.test_16_bit_gradients_up_to_their_rounding(257, 512, 1000, torch.float16)
 P.test_alignment_of_dy_leaves_no_trace()
-P.test_rows_of_dy_that_fit_no_registers()
+P.test_rows_of_dy_of_every_length(1190, 16424, 24)
+P.test_rows_of_dy_of_every_length(3, 16424, 24)
+P.test_rows_of_dy_of_every_length(700, 5000, 33)
 R.test_rows_without_columns_touch_nothing(torch.bfloat16, True)
 for form in F.GRAD_FORMS:
     F.test_gradient(form, int8.GRAD_WEIGHT)
