@@ -31,8 +31,9 @@
 //
 // The tensor cores add in fp32 by cutting off what does not fit, so the sums of a gradient drift towards zero as the contraction grows: sums of
 // positive terms by 2.2e-5 of their size over 8192 terms, 5.7e-5 over 16384, a 16-bit output's rounding over 2^20.  They are therefore
-// taken out of the accumulator and added up in registers, rounded to nearest: every CHUNK stages (1024 terms) where the output is fp32
-// (below 3.8e-6; of both signs 1.9e-7 instead of 2.4e-6 and 6e-6), every CHUNK_SHORT (8192 terms, below 3.1e-5) where it has 16 bits.
+// taken out of the accumulator and added up in registers, rounded to nearest: every CHUNK stages (512 terms) where the output is fp32
+// (positive terms: below 1.9e-6; 256 terms would cost powers of two 12 %, 1024 save 1 %), every CHUNK_SHORT (8192 terms, below 3.1e-5)
+// where it has 16 bits.
 //
 // The 8-bit operand is taken to 16 bits in the workspace before the product: 3 bytes a code and part once, against 2 M N K operations.  Doing
 // so tile by tile on the way into the tensor cores would take two more passes through shared memory per tile (codes in, 16-bit values
@@ -98,7 +99,7 @@ struct ProductParams {
     Int8Ranges ranges;
 };
 
-constexpr int CHUNK = 16, CHUNK_SHORT = 128;
+constexpr int CHUNK = 8, CHUNK_SHORT = 128;
 // contraction elements per stage
 template <int KIND> constexpr int STAGE_ELEMENTS = KIND == INT8 ? 128 : 64;
 template <int KIND> constexpr bool R_MN = KIND != INT8;
@@ -124,30 +125,39 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* tm, i
         for (int b = 0; b < 2; ++b) tma_load_3d<NCTA>(dst + b * MN_BOX, tm, first + 64 * b, ks * STAGE_ELEMENTS<KIND>, part, bar);
     }
 }
-// Which parts the stages of a walk along the contraction have.  The warp that loads them goes stage by stage; the flags are read 32 at a
-// time, a window ahead.  Warp-collective.
-template <int KIND> struct StageParts {
+// The loads of stages [ks0, ks1) of the contraction, load(stage, part) each, until one says false.  Groups of PART_GROUP stages: the small parts
+// of all of them come before the first, so that what the tensor cores cut off at each addition is a unit of the whole sum in the last pass
+// only (fp32 weight gradient, default scales, 8192 terms: 3.8e-6 off with the parts stage by stage in chunks of 16, 4.4e-7 this way).  Flags are
+// read a group ahead; `next`: the group's that follows these stages.  Warp-collective.
+constexpr int PART_GROUP = 8;
+static_assert(CHUNK % PART_GROUP == 0 && CHUNK_SHORT % PART_GROUP == 0, "all parts of a stage are in one chunk");
+template <int KIND> struct StageWalk {
     static_assert(KIND == INT8 || STAGE_ELEMENTS<KIND> == INT8_PART_ROWS, "values_kernel goes by the same stages");
     const ProductParams& p;
-    int window = -1;
-    uint32_t mask = 0, next = 0;
-    // the first stage of the walk
-    __device__ __forceinline__ void begin(int ks) { if (KIND != INT8 && p.flags) fetch(ks >> 5); }
-    __device__ __forceinline__ void fetch(int w)
+    uint32_t ahead = 0;
+    __device__ __forceinline__ void fetch(int group)
     {
-        const int ks = 32 * w + (threadIdx.x & 31);
-        next = ks < p.kstages ? p.flags[ks] : 0u;
+        if (KIND == INT8 || !p.flags) return;
+        const int lane = threadIdx.x & 31;
+        ahead = lane < PART_GROUP && group + lane < p.kstages ? p.flags[group + lane] : 0u;
     }
-    // parts of stage ks; stages are asked for in order, the first one again behind the last
-    __device__ __forceinline__ int of(int ks)
+    template <typename L> __device__ __forceinline__ bool run(int ks0, int ks1, int next, L&& load)
     {
-        if (KIND == INT8 || !p.flags) return 1;
-        if (ks >> 5 != window) {
-            window = ks >> 5;
-            mask = warp_uniform(__ballot_sync(0xffffffffu, next));
-            fetch(32 * (window + 1) < p.kstages ? window + 1 : 0);
+        if constexpr (KIND != INT8) {
+            if (p.flags) {
+                for (int group = ks0; group < ks1; group += PART_GROUP) {
+                    const uint32_t mask = warp_uniform(__ballot_sync(0xffffffffu, ahead));
+                    const int end = min(group + PART_GROUP, ks1);
+                    fetch(end < ks1 ? end : next);
+                    for (int part = mask ? p.parts - 1 : 0; part >= 0; --part)
+                        for (int ks = group; ks < end; ++ks)
+                            if ((part == 0 || (mask >> (ks - group) & 1)) && !load(ks, part)) return false;
+                }
+                return true;
+            }
         }
-        return mask >> (ks & 31) & 1 ? p.parts : 1;
+        for (int ks = ks0; ks < ks1; ++ks) if (!load(ks, 0)) return false;
+        return true;
     }
 };
 // The warp that multiplies them need not tell parts apart: it is told how many pipeline stages a chunk of the walk has, and counts the next
@@ -311,22 +321,20 @@ int8_cluster_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_consta
 
     if (warp == C::OUT_WARPS) {
         int stage = 0; uint32_t phase = 0;
-        StageParts<KIND> stage_parts{p};
-        bool ok = true;
+        StageWalk<KIND> walk{p};
         griddep_wait();
-        stage_parts.begin(ks0);
-        for (int ks = ks0; ks < ks1 && ok; ++ks) {
-            for (int part = 0; part == 0 || part < stage_parts.of(ks); ++part) {
-                if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2301)) { ok = false; break; }
-                if (elect_one()) {
-                    const uint32_t s = base + stage * C::STAGE_BYTES;
-                    mbar_expect_tx(bar_full(stage), C::STAGE_BYTES);
-                    load_rows<KIND, 1>(s, &tmR, row0, ks, part, bar_full(stage));
-                    load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, TC, 1>(s + C::R_BYTES, &tmS, col0, ks, bar_full(stage));
-                }
-                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        walk.fetch(ks0);
+        walk.run(ks0, ks1, ks0, [&](int ks, int part) {
+            if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2301)) return false;
+            if (elect_one()) {
+                const uint32_t s = base + stage * C::STAGE_BYTES;
+                mbar_expect_tx(bar_full(stage), C::STAGE_BYTES);
+                load_rows<KIND, 1>(s, &tmR, row0, ks, part, bar_full(stage));
+                load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, TC, 1>(s + C::R_BYTES, &tmS, col0, ks, bar_full(stage));
             }
-        }
+            if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            return true;
+        });
     } else if (warp == C::OUT_WARPS + 1) {
         int stage = 0, buf = 0; uint32_t phase = 0, bphase = 0;
         griddep_wait();                                      // (the limit of the waits counts from here)
@@ -533,26 +541,25 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap tmR, const __grid_constant_
     if (warp == 0) {
         int stage = 0; uint32_t phase = 0;
         bool ok = true;
-        StageParts<KIND> stage_parts{p};
+        StageWalk<KIND> walk{p};
         griddep_wait();
-        stage_parts.begin(0);
+        walk.fetch(0);
         for (long long w = unit; w < tiles && ok; w += units) {
             int tr, tc;
             place(w, tr, tc);
-            for (int ks = 0; ks < p.kstages && ok; ++ks) {
-                for (int part = 0; part == 0 || part < stage_parts.of(ks); ++part) {
-                    if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2311)) { ok = false; break; }
-                    // completion is counted on the even CTA's barrier; only that CTA arms it
-                    const uint32_t fb = bar_full(stage) & PEER_BIT_MASK;
-                    if (elect_one()) {
-                        const uint32_t s = base + stage * C::STAGE_BYTES;
-                        if (leader) mbar_expect_tx(bar_full(stage), 2 * C::STAGE_BYTES);
-                        load_rows<KIND, 2>(s, &tmR, (2 * tr + rank) * 128, ks, part, fb);
-                        load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 2>(s + C::R_BYTES, &tmS, (2 * tc + rank) * 128, ks, fb);
-                    }
-                    if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+            ok = walk.run(0, p.kstages, 0, [&](int ks, int part) {
+                if (!mbar_wait_warp(bar_empty(stage), phase ^ 1u, ctl, 2311)) return false;
+                // completion is counted on the even CTA's barrier; only that CTA arms it
+                const uint32_t fb = bar_full(stage) & PEER_BIT_MASK;
+                if (elect_one()) {
+                    const uint32_t s = base + stage * C::STAGE_BYTES;
+                    if (leader) mbar_expect_tx(bar_full(stage), 2 * C::STAGE_BYTES);
+                    load_rows<KIND, 2>(s, &tmR, (2 * tr + rank) * 128, ks, part, fb);
+                    load_operand<S_MN<KIND>, STAGE_ELEMENTS<KIND>, 128, 2>(s + C::R_BYTES, &tmS, (2 * tc + rank) * 128, ks, fb);
                 }
-            }
+                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                return true;
+            });
         }
     } else if (warp == 1) {
         if (leader) {
