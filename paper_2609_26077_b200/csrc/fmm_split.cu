@@ -77,8 +77,6 @@ struct SplitCfg {
 
 __device__ __forceinline__ uint32_t cluster_id_x()
 { uint32_t r; asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(r)); return r; }
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t cta)
-{ uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(cta)); return r; }
 __device__ __forceinline__ float4 ld_cluster128(uint32_t addr)
 {
     float4 v;

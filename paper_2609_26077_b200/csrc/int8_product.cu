@@ -50,8 +50,6 @@ enum Kind { INT8 = 0, GRAD_W = 1, GRAD_X = 2 };
 // [0] first bounded wait that gave up, [1] set by the self-test if its wait did not, [2] store outside its range (FMM_DEBUG build)
 __device__ int g_int8_product_status[3];
 
-__device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t cta)
-{ uint32_t r; asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(cta)); return r; }
 __device__ __forceinline__ uint4 ld_cluster128u(uint32_t addr)
 {
     uint4 v;
