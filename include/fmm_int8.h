@@ -132,13 +132,13 @@ fmm_status_t fmm_int8_matmul(const fmm_int8_matmul_t* p, void* cuda_stream);
  *     fmm_int8_grad_input:  out[i][k] (+)= sum_j dy[i][j] * (codes[j][k] * scales[j])      codes N x K, out M x K
  *   out: dev, of out_type, FMM_TYPE_F32 or dy's type; accumulate != 0 adds to what it holds.
  *   Values.  code * scale is a number of fp32.  The tensor cores take 16-bit numbers, so a value is multiplied in parts of dy's type:
- *     out_type FMM_TYPE_F32   bf16: three parts, nothing is lost; fp16: two, 2^-22 of the value (or 2^-32 of the largest scale)
- *     out_type that of dy     two parts: bf16 2^-16, fp16 as above; but fmm_int8_grad_input of bf16 takes the codes, which are exact, and
- *                             dy * scale in half precision: 2^-12 of it, or 2^-39 of the largest in its row (out's rounding: 2^-9)
+ *     out_type FMM_TYPE_F32   bf16: three parts, nothing is lost; fp16: two, 2^-21 of the value (or 2^-32 of the largest scale)
+ *     out_type that of dy     two parts: bf16 2^-15, fp16 as above; but fmm_int8_grad_input of bf16 takes the codes, which are exact, and
+ *                             dy * scale in half precision: 2^-11 of it, or 2^-39 of the largest in its row (out's rounding: 2^-8)
  *   Where the scales of 64 consecutive rows (the first a multiple of 64) are powers of two, one part is the value and the others are left
  *   out: with FMM_INT8_SCALE_POW2 a gradient takes a third (FMM_TYPE_F32, bf16) or half of the time.  fp16 parts carry a power of two
  *   for the whole matrix, so that values beyond fp16's range, as 64 * 1024 for an activation of 65504, do not leave it.
- *   rounded != 0: one part in any case, the value rounded once to dy's type (2^-9 of it for bf16, 2^-12 for fp16).
+ *   rounded != 0: one part in any case, the value rounded once to dy's type (2^-8 of it for bf16, 2^-11 for fp16).
  *   An infinity or NaN, of dy or of a scale, reaches what it is a term of, as in the product of the values.
  *   The workspace holds the values' parts and, where its rows are not 16-byte aligned or it is scaled, a copy of dy (FMM_ERR_SHAPE
  *   where that could be 2^46 bytes or more); its size is asked for with the same arguments (of which the matrices' own addresses but dy's

@@ -71,7 +71,7 @@ template <> __device__ __forceinline__ uint32_t pack_two<__half>(float a, float 
 { __half2 v = __floats2half2_rn(a, b); return *reinterpret_cast<uint32_t*>(&v); }
 
 // fp16 parts: a power of two for the whole matrix, by which its largest finite scale comes to lie in [128, 256), so that no value leaves
-// the range and those 2^-22 of the largest are still normal numbers.  Exponent, from the maxima that int8_values left (warp-collective).
+// the range and those 2^-21 of the largest are still normal numbers.  Exponent, from the maxima that int8_values left (warp-collective).
 __device__ __forceinline__ int maximum_exponent(uint32_t m) { return m == 0 ? 0 : min(7 - ((int)(m >> 23) - 127), 100); }
 __device__ __forceinline__ int matrix_exponent(const uint32_t* maxima, int count)
 {

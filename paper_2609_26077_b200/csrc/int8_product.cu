@@ -20,12 +20,12 @@
 //
 // What a gradient multiplies is in the workspace in 16 bits, but not rounded to them where the output can show it:
 //   - The values code * scale, fp32 numbers, are taken apart into 16-bit parts that are multiplied one after the other: three of
-//     bf16 (nothing is lost) or two of fp16 (2^-22) for an fp32 output, two for a 16-bit one (bf16: 2^-16).  Where the scales of all 64
+//     bf16 (nothing is lost) or two of fp16 (2^-21) for an fp32 output, two for a 16-bit one (bf16: 2^-15).  Where the scales of all 64
 //     rows of a stage are powers of two the first part is the value, and the others are left out: such a product takes a third or half of the
 //     others' MMAs (weight gradient in fp32, 8192 cubed: 781 and 2170 us).  fp16 parts carry a power of two that keeps them in range,
 //     which the output takes out again.
 //   - The input gradient of a bf16 dY with a 16-bit output contracts over the scales of W, so that these can go to dY instead: the product of
-//     the codes, exact in fp16, and of dY * scale, which fp16 holds to 2^-12 of a number, or 2^-39 of its row's largest.  An eighth of the
+//     the codes, exact in fp16, and of dY * scale, which fp16 holds to 2^-11 of a number, or 2^-39 of its row's largest.  An eighth of the
 //     output's own rounding, in one pass (8192 cubed: 800 us, 1514 with two parts, 759 with values rounded to bf16).
 //   - A caller who wants one pass in any case gets values rounded once to dY's type (`rounded`).
 //

@@ -610,7 +610,7 @@ template <> __device__ __forceinline__ uint16_t part_below<__half>(float v)
 }
 
 // A row's pieces as those of dequantize_kernel.  The values are those of fp32; a part is what the parts before it leave, the last one rounded
-// to nearest: two of bf16 are 2^-16 off at most, three exact, two of fp16 2^-22 (or 2^-25 in the units that matrix_exponent sets).
+// to nearest: two of bf16 are 2^-15 off at most, three exact, two of fp16 2^-21 (or 2^-25 in the units that matrix_exponent sets).
 // Where the stage needs one part the others are neither written nor read.
 struct ValuesParams {
     const int8_t* codes; const float* scales; uint8_t* flags; void* x;

@@ -453,7 +453,7 @@ def grad_weight(dy, codes, scales, dtype=torch.float32, out=None, accumulate=Fal
 
     The activations count as the numbers of fp32 that they are.  With scales that are powers of two (quantize, rms_norm with
     pow2=True) 16 bits hold them; with others they are multiplied in two or three 16-bit parts, which takes as many times as long.
-    With `rounded` in one part, rounded to dy's type: 2^-9 of each for bfloat16, 2^-12 for float16."""
+    With `rounded` in one part, rounded to dy's type: 2^-8 of each at most for bfloat16, 2^-11 for float16."""
     device = _device(dy)
     where = _elsewhere(device, stream)
     if where is not None:

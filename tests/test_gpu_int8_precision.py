@@ -69,7 +69,7 @@ def test_fp32_gradients_are_fp32(M, N, K, scales, dtype):
         sw = scales_of(N, 4, pow2=True)         # (a long contraction's bound would not tell 16 bits from 32)
     dw, dx = grads(dy, x, sx, w, sw, torch.float32)
     want_w, size_w, want_x, size_x = exact_grads(dy, x, sx, w, sw)
-    # a unit of 2^-23 for each addition of a product's parts; the values: rounded to fp32 (2^-24) and, of fp16, to two parts (2^-22, or 2^-25
+    # a unit of 2^-23 for each addition of a product's parts; the values: rounded to fp32 (2^-24) and, of fp16, to two parts (2^-21, or 2^-25
     # where the largest scale lies in [128, 256))
     for got, want, size, n, s in ((dw, want_w, size_w, M, sx), (dx, want_x, size_x, N, sw)):
         bound = (MAX_PARTS * n + 2) * 2 * O.U32 * size + 1e-37
@@ -135,7 +135,7 @@ def test_input_gradient_of_rows_far_apart():
         want, size = dy.double() @ v, dy.double().abs() @ v.abs()
         # dY * scale rounded to fp32 and fp16, or to 2^-25 of a unit that is 2^-15 of the row's largest; the sums; the output
         floor = (dy.double() * cuda(sw).double()).abs().max(1).values[:, None] * 2.0 ** -39 * cuda(w).double().abs().sum(0)
-        bound = (2.0 ** -12 + (N + 2) * 2 * O.U32) * size + floor + 1.01 * O.U[torch.bfloat16] * want.abs() + O.TINY[torch.bfloat16]
+        bound = (2.0 ** -11 + (N + 2) * 2 * O.U32) * size + floor + 1.01 * O.U[torch.bfloat16] * want.abs() + O.TINY[torch.bfloat16]
         O.close(O.host(dx), want.cpu().numpy(), bound.cpu().numpy())
         assert not dx[3].any()
 
@@ -205,12 +205,11 @@ def case(M, N, K, dtype, seed, pow2=False, dy_offset=0):
             padded(codes_of(N, K, seed + 1)), cuda(scales_of(N, seed + 1, pow2))]
 
 
-@pytest.mark.parametrize("dy_offset", [0, 1])
+@pytest.mark.parametrize("M,N,K,dy_offset", [(300, 520, 384, 0), (300, 520, 384, 1), (2200, 4200, 130, 0), (40, 8200, 72, 1)])
 @pytest.mark.parametrize("dtype,out_type", CHAINS)
-def test_captured_and_replayed(dtype, out_type, dy_offset):
+def test_captured_and_replayed(dtype, out_type, M, N, K, dy_offset):
     """Two graphs of the same calls, replayed on inputs that change in between (default scales, powers of two, others), eager calls on the same
     stream between them: the bits of eager calls."""
-    M, N, K = 300, 520, 384
     sources = [case(M, N, K, dtype, 1, False, dy_offset), case(M, N, K, dtype, 2, True, dy_offset), case(M, N, K, dtype, 3, False, dy_offset)]
     want = [both(*c, out_type) for c in sources]
     held = case(M, N, K, dtype, 4, False, dy_offset)
@@ -275,7 +274,7 @@ def test_rows_of_dy_of_every_length(M, N, K):
     want, size = dy.double() @ v, dy.double().abs() @ v.abs()
     floor = (dy.double() * sw.double()).abs().max(1).values[:, None] * 2.0 ** -39 * w.double().abs().sum(0)
     # sums of at most 8192 terms leave the accumulator, three more additions
-    bound = (2.0 ** -12 + (min(N, 8192) + 4) * 2 * O.U32) * size + floor + 1.01 * O.U[torch.bfloat16] * want.abs()
+    bound = (2.0 ** -11 + (min(N, 8192) + 4) * 2 * O.U32) * size + floor + 1.01 * O.U[torch.bfloat16] * want.abs()
     for offset in (0, 1):
         poison_free_memory()
         dx = int8.grad_input(O.strided(dy, 3, offset) if offset else dy, w, sw)
