@@ -139,7 +139,8 @@ fmm_status_t fmm_int8_matmul(const fmm_int8_matmul_t* p, void* cuda_stream);
  *   out: with FMM_INT8_SCALE_POW2 a gradient takes a third (FMM_TYPE_F32, bf16) or half of the time.  fp16 parts carry a power of two
  *   for the whole matrix, so that values beyond fp16's range, as 64 * 1024 for an activation of 65504, do not leave it.
  *   rounded != 0: one part in any case, the value rounded once to dy's type (2^-8 of it for bf16, 2^-11 for fp16).
- *   An infinity or NaN, of dy or of a scale, reaches what it is a term of, as in the product of the values.
+ *   An infinity or NaN, of dy or of a scale, reaches what it is a term of, as in the product of the values.  (A dy * scale beyond fp32 counts
+ *   as infinite in the bf16 input gradient.)
  *   The workspace holds the values' parts and, where its rows are not 16-byte aligned or it is scaled, a copy of dy (FMM_ERR_SHAPE
  *   where that could be 2^46 bytes or more); its size is asked for with the same arguments (of which the matrices' own addresses but dy's
  *   do not matter). */
