@@ -282,7 +282,7 @@ __device__ __forceinline__ void put_tile(const ProductParams& p, const CUtensorM
 // Two TMEM accumulators (narrow tiles: four): a block is multiplied while the ones before it leave TMEM.  What issues the MMAs bounds the loop before the tensor pipe
 // does, so it has one barrier to wait for and one to signal for a block: `full` counts the operands of a stage and the warps that have taken the sums
 // of an earlier block out of the accumulator that this one will take; `done` says to those warps that their sums are complete and to the producer that
-// the stage is free.
+// the stage is free.  A block's scales, which those warps read and the MMAs do not, have a slot of their own and a barrier of the CTA that reads them.
 //   warp 0 TMA producer, warp 1 MMA issuer, warp 2 finds the tiles, warps 4 .. 11 sums and output: a TMEM lane quadrant and half of the columns each
 template <int KIND, int NCTA, int TN> struct Cfg {
     static constexpr int TM = 128 * NCTA, A_BYTES = 128 * 128, B_ROWS = TN / NCTA, B_BYTES = B_MN<KIND> ? BOX : B_ROWS * 128, STAGE_BYTES = A_BYTES + B_BYTES;
@@ -296,14 +296,13 @@ template <int KIND, int NCTA, int TN> struct Cfg {
     static constexpr int FIXED = OUT_WARPS * STAGING + SLOTS * SLOT + 512;
     static constexpr int MOST = (232448 - 1024 - FIXED) / STAGE_BYTES, STAGES = MOST < 6 ? MOST : 6;
     static constexpr int OFF_STAGING = STAGES * STAGE_BYTES, OFF_SCALES = OFF_STAGING + OUT_WARPS * STAGING, OFF_BAR = OFF_SCALES + SLOTS * SLOT;
-    // all that a CTA loads for a block
-    static constexpr int LOAD_BYTES = STAGE_BYTES + ROW_SCALES + (KIND == GRAD_W ? TN * 4 : 0);
-    static constexpr int NUM_BARS = 2 * STAGES + 2 * TILE_RING, OFF_RING = 256, SMEM_BYTES = OFF_BAR + 512 + 1024;
+    static constexpr int SCALE_BYTES = ROW_SCALES + (KIND == GRAD_W ? TN * 4 : 0);        // that a CTA loads for a block
+    static constexpr int NUM_BARS = 2 * STAGES + SLOTS + 2 * TILE_RING, OFF_RING = 320, SMEM_BYTES = OFF_BAR + 512 + 1024;
     // accumulators: as many as TMEM holds, four at most (the waits for one that is taken out would bound narrow tiles)
     static constexpr int BUFS = TN == 256 ? 2 : 4, TMEM_COLS = BUFS * TN;
     static_assert(BUFS <= STAGES, "operands of the block that takes an accumulator next are counted by a barrier that has come round");
     // Block b is loaded when block b - STAGES has been multiplied, for which all warps have left the accumulator of block b - STAGES - BUFS; they may be
-    // at its last piece still.
+    // at its last piece still.  So they have seen the slot's barrier come round, too, before it is armed again.
     static_assert(SLOTS > STAGES + BUFS, "scales are not overwritten while they are read");
     static constexpr int REGS_AT_LAUNCH = 168, REGS_CTRL = 56, REGS_OUT = 224;
     static_assert(128 * REGS_CTRL + OUT_WARPS * 32 * REGS_OUT <= THREADS * REGS_AT_LAUNCH, "register pool");
@@ -323,6 +322,8 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const uint32_t bar0 = base + C::OFF_BAR;
     auto bar_full = [&](int s) { return bar0 + 8u * s; };
     auto bar_done = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+    auto bar_scales = [&](int s) { return bar0 + 8u * (2 * C::STAGES + s); };
+    const uint32_t bar_ring = bar0 + 8u * (2 * C::STAGES + C::SLOTS);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + C::OFF_BAR + C::NUM_BARS * 8);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const Ctl ctl{abort_flag, g_fp8_product_status};
@@ -334,8 +335,9 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     if (warp == 2 && elect_one()) { prefetch_map(&tmA); prefetch_map(&tmB); }
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1 + NCTA * C::OUT_WARPS); mbar_init(bar_done(s), 1); }
+        for (int s = 0; s < C::SLOTS; ++s) mbar_init(bar_scales(s), 1);
         // the output warps, the producer, the issuer
-        for (int i = 0; i < TILE_RING; ++i) { mbar_init(bar0 + 8u * (2 * C::STAGES + i), 1); mbar_init(bar0 + 8u * (2 * C::STAGES + TILE_RING + i), C::OUT_WARPS + 1 + leader); }
+        for (int i = 0; i < TILE_RING; ++i) { mbar_init(bar_ring + 8u * i, 1); mbar_init(bar_ring + 8u * (TILE_RING + i), C::OUT_WARPS + 1 + leader); }
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -349,7 +351,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     tc_fence_after();
     const uint32_t tmem_base = warp_uniform(*tmem_slot);
     const int units = gridDim.x / (NCTA * shares), unit = blockIdx.x / (NCTA * shares);
-    TileRing ring = {base + C::OFF_BAR + C::OFF_RING, bar0 + 16u * C::STAGES, bar0 + 16u * C::STAGES + 8u * TILE_RING};
+    TileRing ring = {base + C::OFF_BAR + C::OFF_RING, bar_ring, bar_ring + 8u * TILE_RING};
 
     if (warp < C::OUT_WARP0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_CTRL));
@@ -362,16 +364,17 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             const int row = t.row0 + rank * 128, col = t.col0 + rank * C::B_ROWS;
             for (int kb = t.kb0; kb < t.kb0 + t.kbs; ++kb) {
                 if (!mbar_wait_warp(bar_done(stage), phase ^ 1u, ctl, 2611)) { ok = false; break; }
-                // completion is counted on the even CTA's barrier; only that CTA arms it
+                // completion of operands is counted on the even CTA's barrier; only that CTA arms it
                 const uint32_t fb = NCTA == 2 ? bar_full(stage) & PEER_BIT_MASK : bar_full(stage);
                 if (elect_one()) {
                     const uint32_t s = base + stage * C::STAGE_BYTES;
-                    if (leader) mbar_expect_tx(bar_full(stage), NCTA * C::LOAD_BYTES);
+                    if (leader) mbar_expect_tx(bar_full(stage), NCTA * C::STAGE_BYTES);
                     tma_load_2d<NCTA>(s, &tmA, A_MN<KIND> ? row : kb * 128, A_MN<KIND> ? kb * 128 : row, fb);
                     tma_load_3d<NCTA>(s + C::A_BYTES, &tmB, B_MN<KIND> ? col : kb * 128, B_MN<KIND> ? kb * 128 : col, KIND == GRAD_W ? 0 : t.group, fb);
                     const uint32_t scales = base + C::OFF_SCALES + slot * C::SLOT;
-                    tma_load_2d<NCTA>(scales, &tmRowScales, row & ~3, kb, fb);
-                    if (KIND == GRAD_W) tma_load_2d<NCTA>(scales + 640, &tmColScales, t.col0, kb, fb);
+                    mbar_expect_tx(bar_scales(slot), C::SCALE_BYTES);
+                    tma_load_2d<1>(scales, &tmRowScales, row & ~3, kb, bar_scales(slot));
+                    if (KIND == GRAD_W) tma_load_2d<1>(scales + 640, &tmColScales, t.col0, kb, bar_scales(slot));
                 }
                 if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
                 if (++slot == C::SLOTS) slot = 0;
@@ -434,7 +437,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             const long long blocks_c = (p.cols + 127) / 128, c = min((t.col0 + half * COLS) / 128, (int)blocks_c - 1), all = (p.depth + 127) / 128, b = t.kb0 + kb + lane;
             return __ldg(p.b_scales + t.group * blocks_c * all + (KIND == MATMUL ? c * all + b : b * blocks_c + c));
         };
-        int slot = 0;
+        int slot = 0; uint32_t slot_phase = 0;
         Tile t = ring.get(ctl);
         scales_now = fetch(t, 0);
         float sum[COLS];
@@ -452,8 +455,14 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             auto arrived = [&](uint32_t (&r)[CH]) {
                 if constexpr (CH == 32) tmem_ld_wait32(r); else tmem_ld_wait16(r);
             };
+            // A block's scales and its sums.  (`done` says nothing of the scales: TMA copied them, which these warps see through a barrier that counts its
+            // bytes.  They are there long before the sums, so that their wait is part of that for these.)
+            auto wait_block = [&] {
+                const bool scales = mbar_wait(bar_scales(slot), slot_phase, ctl, 2616);
+                return __all_sync(0xffffffffu, scales && mbar_wait(bar_done(stage), phase, ctl, 2613));
+            };
             if (t.kbs > 0) {
-                if (!mbar_wait_warp(bar_done(stage), phase, ctl, 2613)) { ok = false; break; }
+                if (!wait_block()) { ok = false; break; }
                 tc_fence_after();
                 load(v[0], 0);
             }
@@ -465,7 +474,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 const uint32_t cols_at = base + C::OFF_SCALES + slot * C::SLOT + 640 + half * COLS * 4;
                 const float row_scale = lds32f(base + C::OFF_SCALES + slot * C::SLOT + row_at);
                 const float factor = KIND == GRAD_W ? 0.0f : row_scale * __shfl_sync(0xffffffffu, scales_now, kb & 31);
-                if (++slot == C::SLOTS) slot = 0;
+                if (++slot == C::SLOTS) { slot = 0; slot_phase ^= 1u; }
 #pragma unroll
                 for (int i = 0; i < COLS / CH; ++i) {
                     uint32_t (&now)[CH] = v[i & 1], (&then)[CH] = v[(i + 1) & 1];
@@ -479,7 +488,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                         if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
                         if (++buf == C::BUFS) buf = 0;
                         if (kb + 1 < t.kbs) {
-                            if (!mbar_wait_warp(bar_done(stage), phase, ctl, 2613)) { ok = false; break; }
+                            if (!wait_block()) { ok = false; break; }
                             tc_fence_after();
                             load(then, 0);
                         }
