@@ -28,7 +28,8 @@
  *     into CUDA graphs.  Results do not depend on the run: no floating-point atomics, every sum in a fixed order.
  *   - Matrices are row-major; `ld*` is the distance between rows in elements, at least the number of columns.  Inputs and outputs in
  *     fp32, bf16 and fp16 may have any alignment that their type allows (16-byte aligned rows are fastest).  Codes have 16-byte
- *     aligned rows (ld a multiple of 16), scales of rows and columns too (ld a multiple of 4).  Nothing is written behind the last column of a row,
+ *     aligned rows (ld a multiple of 16), scales of rows and columns too (ld a multiple of 4), unless the call says that they are `loose`: then these may
+ *     lie as fp32 numbers do, rows any distance apart, and products load them without TMA.  Nothing is written behind the last column of a row,
  *     and nothing read but what shares an aligned 16-byte vector with an element of the row.
  *   - Rows, columns and groups may be 0: then nothing is read, and what an empty sum gives is written.  M, N, K and column rows are below
  *     2^31 - 16384 (FMM_ERR_SHAPE).
@@ -51,7 +52,8 @@ fmm_status_t fmm_fp8_column_rows(int64_t rows, int64_t groups, int64_t* column_r
 
 /* Forms of x (dev, rows x cols of `type`) along its rows, along its columns, or both from one pass over x.
  *   codes (rows x cols), scales (ceil(cols / 128) x rows, lds apart): form along the rows; codes NULL: not wanted.
- *   column_codes (fmm_fp8_column_rows x cols), column_scales (a row for each 128 of those): along the columns; NULL: not wanted. */
+ *   column_codes (fmm_fp8_column_rows x cols), column_scales (a row for each 128 of those): along the columns; NULL: not wanted.
+ *   loose != 0: both kinds of scales as any fp32 numbers. */
 typedef struct {
     fmm_type_t type;
     fmm_fp8_scale_t scale_mode;
@@ -62,6 +64,7 @@ typedef struct {
     float* scales;          int64_t lds;
     uint8_t* column_codes;  int64_t ldcc;
     float* column_scales;   int64_t ldcs;
+    int64_t loose;
 } fmm_fp8_quantize_t;
 fmm_status_t fmm_fp8_quantize(const fmm_fp8_quantize_t* p, void* cuda_stream);
 
@@ -83,8 +86,8 @@ fmm_status_t fmm_fp8_quantize_weight(const fmm_fp8_quantize_weight_t* p, void* c
  *     fmm_fp8_grad_weight  out_g[j][k]  (+)= sum_i a[i][j] b[i][k]                  a: M x N (dy) and b: M x K along their columns, out_g N x K
  *   M: tokens; grad_weight: rows of the form along the columns, a multiple of 128 (FMM_ERR_SHAPE).  It does not know the number of tokens, so
  *   that offsets beyond that are not cut to it there as elsewhere: nothing is read outside of the M rows, but that group's gradient is not specified.
- *   a, lda, a_scales, lda_scales; b, ldb, b_scales as the forms have them, ldb_scales: of grad_weight's b only.  step_b: codes from one group's
- *   weight to the next (a multiple of 16), whose scales are dense.  bias: groups x N of `type`, dense, or NULL (gradients: NULL).
+ *   a, lda, a_scales, lda_scales; b, ldb, b_scales as the forms have them, ldb_scales: of grad_weight's b only.  loose != 0: scales along rows and
+ *   columns as any fp32 numbers.  step_b: codes from one group's weight to the next (a multiple of 16), whose scales are dense.  bias: groups x N of `type`, dense, or NULL (gradients: NULL).
  *   out: of `type`; step_out: elements from one group's weight gradient to the next.  accumulate != 0 adds to what it holds; without, a group
  *   without rows has 0 as its weight gradient.
  *   Arithmetic: the products of a block of 128 are summed by the tensor cores in fp32, the blocks' sums, times their two scales (whose product
@@ -100,6 +103,7 @@ typedef struct {
     const float* b_scales;  int64_t ldb_scales;
     const void* bias;
     void* out;              int64_t ldo, step_out;
+    int64_t loose;
 } fmm_fp8_product_t;
 fmm_status_t fmm_fp8_matmul(const fmm_fp8_product_t* p, void* cuda_stream);
 fmm_status_t fmm_fp8_grad_input(const fmm_fp8_product_t* p, void* cuda_stream);

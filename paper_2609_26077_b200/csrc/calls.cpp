@@ -50,6 +50,14 @@ bool matrix(const at::Tensor* t, const Place& p, at::ScalarType type, int64_t ro
     ld = t->stride(0);
     return ld >= cols && ld >= 1 && ld % step == 0 && (step == 1 || ((uintptr_t)t->data_ptr() & 15) == 0);
 }
+// scales along rows or columns, rows x cols; loose: rows that start anywhere but on 16-byte boundaries
+bool scales_of(const at::Tensor* t, const Place& p, int64_t rows, int64_t cols, int64_t& ld, int64_t& loose)
+{
+    if (!matrix(t, p, at::kFloat, rows, cols, 1, ld)) return false;
+    if (rows == 1) ld = up(cols, 4);
+    loose |= (ld & 3) != 0 || ((uintptr_t)t->data_ptr() & 15) != 0;
+    return true;
+}
 bool dense(const at::Tensor* t, const Place& p, at::ScalarType type, at::IntArrayRef shape) { return here(t, p, type) && t->sizes() == shape && t->is_contiguous(); }
 // codes of a weight, or of one for each group
 bool weight(const at::Tensor* t, const Place& p, int64_t groups, int64_t& ld, int64_t& step)
@@ -150,7 +158,7 @@ PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t n)
         const int accumulate = PyObject_IsTrue(args[9]);
         const int64_t groups = groups_of(args[5], p, c.offsets), M = a->size(0), depth = a->size(1);
         NOT_USUAL(accumulate < 0 || (accumulate && args[8] == Py_None) || groups < 0 || M == 0 || depth == 0 || !matrix(a, p, CODES, M, depth, 16, c.lda) ||
-                  !matrix(as, p, at::kFloat, blocks(depth), M, 4, c.lda_scales) || !weight(b, p, groups, c.ldb, c.step_b));
+                  !scales_of(as, p, blocks(depth), M, c.lda_scales, c.loose) || !weight(b, p, groups, c.ldb, c.step_b));
         const int64_t N = b->size(-2), K = b->size(-1), cols = which == MATMUL ? N : K;
         NOT_USUAL(depth != (which == MATMUL ? K : N));
         NOT_USUAL(groups ? !dense(bs, p, at::kFloat, {groups, blocks(N), blocks(K)}) : !dense(bs, p, at::kFloat, {blocks(N), blocks(K)}));
@@ -185,7 +193,7 @@ PyObject* grad_weight(PyObject*, PyObject* const* args, Py_ssize_t n)
         const int accumulate = PyObject_IsTrue(args[7]);
         const int64_t groups = groups_of(args[4], p, c.offsets), M = dy->size(0), N = dy->size(1), K = x->size(1);
         NOT_USUAL(accumulate < 0 || (accumulate && args[6] == Py_None) || groups < 0 || M == 0 || M % 128 || N == 0 || K == 0 || !matrix(dy, p, CODES, M, N, 16, c.lda) ||
-                  !matrix(x, p, CODES, M, K, 16, c.ldb) || !matrix(dys, p, at::kFloat, M / 128, N, 4, c.lda_scales) || !matrix(xs, p, at::kFloat, M / 128, K, 4, c.ldb_scales));
+                  !matrix(x, p, CODES, M, K, 16, c.ldb) || !scales_of(dys, p, M / 128, N, c.lda_scales, c.loose) || !scales_of(xs, p, M / 128, K, c.ldb_scales, c.loose));
         at::Tensor out;
         int type;
         const int64_t shape[3] = {groups, N, K};

@@ -38,6 +38,7 @@ struct ProductParams {
     void* out; long long ldo, step_out;
     int out_type, accumulate;
     int by_tma;                     // the output's rows can be written by TMA
+    int loose;                      // scales along rows and columns that TMA cannot load
     int shares;                     // CTAs (a cluster, single CTAs only) that share a tile's contraction; more than one: a tile to a cluster
     Int8Ranges ranges;
 };
@@ -283,7 +284,8 @@ __device__ __forceinline__ void put_tile(const ProductParams& p, const CUtensorM
 // does, so it has one barrier to wait for and one to signal for a block: `full` counts the operands of a stage and the warps that have taken the sums
 // of an earlier block out of the accumulator that this one will take; `done` says to those warps that their sums are complete and to the producer that
 // the stage is free.  A block's scales, which those warps read and the MMAs do not, have a slot of their own and a barrier of the CTA that reads them.
-//   warp 0 TMA producer, warp 1 MMA issuer, warp 2 finds the tiles, warps 4 .. 11 sums and output: a TMEM lane quadrant and half of the columns each
+//   warp 0 TMA producer, warp 1 MMA issuer, warp 2 finds the tiles, warp 3 loads scales that TMA cannot, warps 4 .. 11 sums and output: a TMEM lane
+//   quadrant and half of the columns each
 template <int KIND, int NCTA, int TN> struct Cfg {
     static constexpr int TM = 128 * NCTA, A_BYTES = 128 * 128, B_ROWS = TN / NCTA, B_BYTES = B_MN<KIND> ? BOX : B_ROWS * 128, STAGE_BYTES = A_BYTES + B_BYTES;
     static_assert(!B_MN<KIND> || B_ROWS == 128, "an MN-major box is 128 elements wide");
@@ -334,10 +336,10 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const bool leader = rank == 0;
     if (warp == 2 && elect_one()) { prefetch_map(&tmA); prefetch_map(&tmB); }
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1 + NCTA * C::OUT_WARPS); mbar_init(bar_done(s), 1); }
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1 + NCTA * (C::OUT_WARPS + (p.loose ? 1 : 0))); mbar_init(bar_done(s), 1); }
         for (int s = 0; s < C::SLOTS; ++s) mbar_init(bar_scales(s), 1);
-        // the output warps, the producer, the issuer
-        for (int i = 0; i < TILE_RING; ++i) { mbar_init(bar_ring + 8u * i, 1); mbar_init(bar_ring + 8u * (TILE_RING + i), C::OUT_WARPS + 1 + leader); }
+        // the output warps, the producer, the issuer, the warp that loads loose scales
+        for (int i = 0; i < TILE_RING; ++i) { mbar_init(bar_ring + 8u * i, 1); mbar_init(bar_ring + 8u * (TILE_RING + i), C::OUT_WARPS + 1 + leader + (p.loose ? 1 : 0)); }
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -372,9 +374,11 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                     tma_load_2d<NCTA>(s, &tmA, A_MN<KIND> ? row : kb * 128, A_MN<KIND> ? kb * 128 : row, fb);
                     tma_load_3d<NCTA>(s + C::A_BYTES, &tmB, B_MN<KIND> ? col : kb * 128, B_MN<KIND> ? kb * 128 : col, KIND == GRAD_W ? 0 : t.group, fb);
                     const uint32_t scales = base + C::OFF_SCALES + slot * C::SLOT;
-                    mbar_expect_tx(bar_scales(slot), C::SCALE_BYTES);
-                    tma_load_2d<1>(scales, &tmRowScales, row & ~3, kb, bar_scales(slot));
-                    if (KIND == GRAD_W) tma_load_2d<1>(scales + 640, &tmColScales, t.col0, kb, bar_scales(slot));
+                    if (!p.loose) {
+                        mbar_expect_tx(bar_scales(slot), C::SCALE_BYTES);
+                        tma_load_2d<1>(scales, &tmRowScales, row & ~3, kb, bar_scales(slot));
+                        if (KIND == GRAD_W) tma_load_2d<1>(scales + 640, &tmColScales, t.col0, kb, bar_scales(slot));
+                    }
                 }
                 if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
                 if (++slot == C::SLOTS) slot = 0;
@@ -413,6 +417,41 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 t.kbs = to - from;
             }
             if (!ring.put(t, ctl) || t.group < 0) break;
+        }
+    } else if (p.loose) {
+        // Scales that TMA cannot load come by way of this warp's registers (4096 cubed 71 to 75 us, by TMA 71; 8192 cubed 535 of 495, weight gradient 717 of
+        // 679).  The MMAs wait for it too, so that it falls no round of stages behind.  Beyond the last row or column: 0, as by TMA.
+        int stage = 0, slot = 0; uint32_t phase = 0;
+        bool ok = true;
+        while (ok) {
+            const Tile t = ring.get(ctl);
+            if (t.group < 0) break;
+            const int row = t.row0 + rank * 128;
+            for (int kb = t.kb0; kb < t.kb0 + t.kbs; ++kb) {
+                const float *rows_from = p.a_scales + kb * p.lda_scales + row + lane, *cols_from = p.b_scales + kb * p.ldb_scales + t.col0 + lane;
+                float r[4] = {}, c[TN / 32] = {};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (row + 32 * i + lane < p.rows) r[i] = __ldg(rows_from + 32 * i);
+                if (KIND == GRAD_W) {
+#pragma unroll
+                    for (int i = 0; i < TN / 32; ++i) if (t.col0 + 32 * i + lane < p.cols) c[i] = __ldg(cols_from + 32 * i);
+                }
+                if (!mbar_wait_warp(bar_done(stage), phase ^ 1u, ctl, 2617)) { ok = false; break; }
+                const uint32_t to = base + C::OFF_SCALES + slot * C::SLOT + 4 * lane;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sts32f(to + ((row & 3) + 32 * i) * 4, r[i]);
+                if (KIND == GRAD_W) {
+#pragma unroll
+                    for (int i = 0; i < TN / 32; ++i) sts32f(to + 640 + 128 * i, c[i]);
+                }
+                __syncwarp();
+                if (elect_one()) {
+                    mbar_arrive(bar_scales(slot));
+                    if (NCTA == 2) mbar_arrive_cluster(bar_full(stage) & PEER_BIT_MASK); else mbar_arrive(bar_full(stage));
+                }
+                if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                if (++slot == C::SLOTS) slot = 0;
+            }
         }
     }
     if (NCTA == 1 && shares > 1) { __syncwarp(); cluster_sync(); cluster_sync(); }        // as the output warps below
@@ -747,9 +786,11 @@ template <int KIND, int NCTA, int TN> fmm_status_t launch_tiles(ProductParams p,
     const int64_t b_x = KIND == MATMUL ? p.depth : p.cols, b_y = KIND == MATMUL ? p.cols : p.depth;
     bool ok = make_map_2d(&tmA, codes, 1, p.a, (uint64_t)a_x, (uint64_t)a_y, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B, (uint64_t)p.lda) &&
               make_map_3d(&tmB, codes, 1, p.b, b_x, b_y, KIND == GRAD_W ? 1 : groups, p.ldb, p.step_b, 128, B_MN<KIND> ? 128 : C::B_ROWS) &&
-              make_map_2d(&tmRowScales, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, p.a_scales, (uint64_t)p.rows, (uint64_t)ceil_div(p.depth, 128), 132, 1, CU_TENSOR_MAP_SWIZZLE_NONE, (uint64_t)p.lda_scales) &&
               raise_smem(fp8_product_kernel<KIND, NCTA, TN>, C::SMEM_BYTES, done);
-    if (KIND == GRAD_W)
+    if (!p.loose)
+        ok = ok && make_map_2d(&tmRowScales, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, p.a_scales, (uint64_t)p.rows, (uint64_t)ceil_div(p.depth, 128), 132, 1, CU_TENSOR_MAP_SWIZZLE_NONE, (uint64_t)p.lda_scales);
+    else memset(&tmRowScales, 0, sizeof(tmRowScales));
+    if (KIND == GRAD_W && !p.loose)
         ok = ok && make_map_2d(&tmColScales, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, p.b_scales, (uint64_t)p.cols, (uint64_t)ceil_div(p.depth, 128), TN, 1, CU_TENSOR_MAP_SWIZZLE_NONE, (uint64_t)p.ldb_scales);
     else memset(&tmColScales, 0, sizeof(tmColScales));
     p.by_tma = !p.accumulate && int8_aligned(p.out, p.ldo * e, 16) && ((p.step_out * e) & 15) == 0;
@@ -872,8 +913,8 @@ template <int KIND> fmm_status_t product(const fmm_fp8_product_t* a, void* strea
     if (depth) {
         const int64_t a_cols = KIND == MATMUL ? K : N, b_rows = KIND == GRAD_W ? M : N;
         if (!a->a || a->lda < a_cols || !int8_aligned(a->a, a->lda, 16) || !a->b || a->ldb < K || !int8_aligned(a->b, a->ldb, 16) || !a->a_scales || !a->b_scales ||
-            a->lda_scales < (KIND == GRAD_W ? N : M) || !int8_aligned(a->a_scales, a->lda_scales * 4, 16)) return FMM_ERR_INVALID_ARG;
-        if (KIND == GRAD_W ? a->ldb_scales < K || !int8_aligned(a->b_scales, a->ldb_scales * 4, 16) : ((uintptr_t)a->b_scales & 3) != 0) return FMM_ERR_INVALID_ARG;
+            a->lda_scales < (KIND == GRAD_W ? N : M) || !int8_aligned(a->a_scales, a->lda_scales * 4, a->loose ? 4 : 16)) return FMM_ERR_INVALID_ARG;
+        if (KIND == GRAD_W ? a->ldb_scales < K || !int8_aligned(a->b_scales, a->ldb_scales * 4, a->loose ? 4 : 16) : ((uintptr_t)a->b_scales & 3) != 0) return FMM_ERR_INVALID_ARG;
         if (KIND != GRAD_W && count > 1 && (a->step_b < (b_rows - 1) * a->ldb + K || (a->step_b & 15))) return FMM_ERR_INVALID_ARG;
     }
     ProductParams p = {};
@@ -882,7 +923,7 @@ template <int KIND> fmm_status_t product(const fmm_fp8_product_t* a, void* strea
     p.a = a->a; p.lda = a->lda; p.a_scales = a->a_scales; p.lda_scales = a->lda_scales;
     p.b = a->b; p.ldb = a->ldb; p.step_b = KIND != GRAD_W && count > 1 ? a->step_b : 0; p.b_scales = a->b_scales; p.ldb_scales = a->ldb_scales;
     p.bias = a->bias; p.out = a->out; p.ldo = a->ldo; p.step_out = KIND == GRAD_W && count > 1 ? a->step_out : 0;
-    p.out_type = a->type; p.accumulate = a->accumulate != 0;
+    p.out_type = a->type; p.accumulate = a->accumulate != 0; p.loose = a->loose != 0;
     if (KIND == GRAD_W) int8_add_range(p.ranges, a->out, 1, (count - 1) * p.step_out + (rows - 1) * a->ldo + cols, 0, e);
     else int8_add_range(p.ranges, a->out, rows, cols, a->ldo, e);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

@@ -320,9 +320,10 @@ fmm_status_t fmm_fp8_quantize(const fmm_fp8_quantize_t* a, void* stream)
     if (!a->codes && !a->column_codes) return FMM_ERR_INVALID_ARG;
     if (rows == 0 || cols == 0) return FMM_OK;
     if (!a->x || ((uintptr_t)a->x & (e - 1)) || a->ldx < cols || (a->groups && (!a->offsets || ((uintptr_t)a->offsets & 3)))) return FMM_ERR_INVALID_ARG;
-    if (a->codes && (a->ldc < cols || !int8_aligned(a->codes, a->ldc, 16) || !a->scales || a->lds < rows || !int8_aligned(a->scales, a->lds * 4, 16))) return FMM_ERR_INVALID_ARG;
+    const unsigned step = a->loose ? 4 : 16;
+    if (a->codes && (a->ldc < cols || !int8_aligned(a->codes, a->ldc, 16) || !a->scales || a->lds < rows || !int8_aligned(a->scales, a->lds * 4, step))) return FMM_ERR_INVALID_ARG;
     if (a->column_codes && (a->ldcc < cols || !int8_aligned(a->column_codes, a->ldcc, 16) || !a->column_scales || a->ldcs < cols ||
-                            !int8_aligned(a->column_scales, a->ldcs * 4, 16))) return FMM_ERR_INVALID_ARG;
+                            !int8_aligned(a->column_scales, a->ldcs * 4, step))) return FMM_ERR_INVALID_ARG;
     QuantizeParams p = {};
     p.rows = (int)rows; p.cols = (int)cols; p.column_blocks = (int)ceil_div(cols, 128);
     p.groups = (int)a->groups; p.offsets = a->offsets; p.pow2 = a->scale_mode == FMM_FP8_SCALE_POW2;

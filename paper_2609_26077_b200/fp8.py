@@ -25,9 +25,9 @@ Codes are torch.float8_e4m3fn, a code times its scale being the number.  Scales:
 each 128 rows x K, of tiles ceil(N / 128) x ceil(K / 128).  The form along the columns has `column_rows` rows, of which a group takes the next
 multiple of 128; what is behind the last group in use is not written.  Rows of a grouped call that belong to no group take no part and are not written.
 
-Matrices are 2-D CUDA tensors whose columns are contiguous (rows may lie any distance apart; those of codes and of scales along rows or columns
-start on 16-byte boundaries, as the ones that are allocated here do).  All tensors of a call are on one device, on whose current stream the
-work is enqueued, or on `stream`; nothing is synchronised, and calls may be captured into CUDA graphs.  Outputs are allocated unless they are
+Matrices are 2-D CUDA tensors whose columns are contiguous (rows may lie any distance apart; those of codes start on 16-byte boundaries, as the ones
+that are allocated here do, and so may those of scales along rows or columns: where they do not, large products take up to a twelfth longer).  All tensors of
+a call are on one device, on whose current stream the work is enqueued, or on `stream`; nothing is synchronised, and calls may be captured into CUDA graphs.  Outputs are allocated unless they are
 given; a given one may not overlap an input or another output.  Unsuitable arguments raise TypeError (types, devices) or ValueError (shapes,
 strides), anything that the library refuses raises fmm.FmmError.  Nothing is recorded for autograd: the gradients are calls of their own.
 """
@@ -53,7 +53,7 @@ class QuantizeArgs(C.Structure):
     """fmm_fp8_quantize_t"""
     _fields_ = [("type", C.c_int), ("scale_mode", C.c_int), ("rows", C.c_int64), ("cols", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
                 ("groups", C.c_int64), ("offsets", C.c_void_p), ("codes", C.c_void_p), ("ldc", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64),
-                ("column_codes", C.c_void_p), ("ldcc", C.c_int64), ("column_scales", C.c_void_p), ("ldcs", C.c_int64)]
+                ("column_codes", C.c_void_p), ("ldcc", C.c_int64), ("column_scales", C.c_void_p), ("ldcs", C.c_int64), ("loose", C.c_int64)]
 
 
 class QuantizeWeightArgs(C.Structure):
@@ -67,7 +67,7 @@ class ProductArgs(C.Structure):
     _fields_ = [("type", C.c_int), ("accumulate", C.c_int), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("groups", C.c_int64),
                 ("offsets", C.c_void_p), ("a", C.c_void_p), ("lda", C.c_int64), ("a_scales", C.c_void_p), ("lda_scales", C.c_int64),
                 ("b", C.c_void_p), ("ldb", C.c_int64), ("step_b", C.c_int64), ("b_scales", C.c_void_p), ("ldb_scales", C.c_int64),
-                ("bias", C.c_void_p), ("out", C.c_void_p), ("ldo", C.c_int64), ("step_out", C.c_int64)]
+                ("bias", C.c_void_p), ("out", C.c_void_p), ("ldo", C.c_int64), ("step_out", C.c_int64), ("loose", C.c_int64)]
 
 
 _quantize_args, _weight_args, _product_args = _packer(QuantizeArgs), _packer(QuantizeWeightArgs), _packer(ProductArgs)
@@ -107,6 +107,14 @@ def _spaced(t, name, dtype, device, shape, step):
     if (ld % step or t.data_ptr() & 15) and rows and cols:
         raise ValueError(f"{name}: rows have to start on 16-byte boundaries (as those that this module allocates do)")
     return ld
+
+
+def _scales(t, name, device, shape):
+    """Scales along rows or columns: the distance of their rows, and whether these start anywhere but on 16-byte boundaries."""
+    ld = _matrix(t, name, torch.float32, device, shape)
+    if shape[0] <= 1:
+        ld = (shape[1] + 3) // 4 * 4 or 4
+    return ld, bool(ld % 4 or t.data_ptr() & 15)
 
 
 def _stack(t, name, dtype, device, groups=None):
@@ -168,15 +176,16 @@ def _quantize(x, device, pow2, offsets, codes, scales, column_codes, column_scal
     ldx = _matrix(x, "x", x.dtype, device)
     rows, cols = x.shape
     groups, at_offsets = (0, 0) if offsets is None else (_groups(offsets, device), offsets.data_ptr())
-    p = [0] * 8
+    p, loose = [0] * 8, False
     if codes is not None:
-        p[:4] = (codes.data_ptr(), _spaced(codes, "codes", CODES, device, (rows, cols), 16), scales.data_ptr(),
-                 _spaced(scales, "scales", torch.float32, device, (_blocks(cols), rows), 4))
+        lds, loose = _scales(scales, "scales", device, (_blocks(cols), rows))
+        p[:4] = codes.data_ptr(), _spaced(codes, "codes", CODES, device, (rows, cols), 16), scales.data_ptr(), lds
     if column_codes is not None:
         padded = column_rows(rows, offsets)
-        p[4:] = (column_codes.data_ptr(), _spaced(column_codes, "column_codes", CODES, device, (padded, cols), 16), column_scales.data_ptr(),
-                 _spaced(column_scales, "column_scales", torch.float32, device, (padded // 128, cols), 4))
-    a = _quantize_args(kind, 1 if pow2 else 0, rows, cols, x.data_ptr(), ldx, groups, at_offsets, *p)
+        ldcs, also = _scales(column_scales, "column_scales", device, (padded // 128, cols))
+        loose |= also
+        p[4:] = column_codes.data_ptr(), _spaced(column_codes, "column_codes", CODES, device, (padded, cols), 16), column_scales.data_ptr(), ldcs
+    a = _quantize_args(kind, 1 if pow2 else 0, rows, cols, x.data_ptr(), ldx, groups, at_offsets, *p, loose)
     if rows and cols:
         _call((_lib or lib()).fmm_fp8_quantize(a, _stream(device)), "fmm_fp8_quantize")
 
@@ -315,7 +324,7 @@ def _product(which, a, a_scales, b, b_scales, offsets, bias, dtype, out, accumul
     M, depth = a.shape
     N, K = b.shape[-2:]
     lda = _spaced(a, "a", CODES, device, None, 16)
-    lds = _spaced(a_scales, "a_scales", torch.float32, device, (_blocks(depth), M), 4)
+    lds, loose = _scales(a_scales, "a_scales", device, (_blocks(depth), M))
     ldb, step_b = _weight(b, "b", device, groups)
     tiles = (_blocks(N), _blocks(K))
     _vector(b_scales, "b_scales", torch.float32, device, tiles if groups is None else (groups, *tiles))
@@ -331,7 +340,7 @@ def _product(which, a, a_scales, b, b_scales, offsets, bias, dtype, out, accumul
     if bias is not None:
         _vector(bias, "bias", out.dtype, device, (N,) if groups is None else (groups, N))
     p = _product_args(kind, bool(accumulate), M, N, K, groups or 0, 0 if offsets is None else offsets.data_ptr(), a.data_ptr(), lda, a_scales.data_ptr(), lds,
-                      b.data_ptr(), ldb, step_b, b_scales.data_ptr(), 0, 0 if bias is None else bias.data_ptr(), out.data_ptr(), ldo, 0)
+                      b.data_ptr(), ldb, step_b, b_scales.data_ptr(), 0, 0 if bias is None else bias.data_ptr(), out.data_ptr(), ldo, 0, loose)
     if M and shape[1]:
         _call(getattr(_lib or lib(), which)(p, _stream(device)), which)
     return out
@@ -405,12 +414,12 @@ def _grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate, de
     M, N = dy.shape
     K = x.shape[1]
     ldy, ldx = _spaced(dy, "dy", CODES, device, None, 16), _spaced(x, "x", CODES, device, None, 16)
-    ldys = _spaced(dy_scales, "dy_scales", torch.float32, device, (M // 128, N), 4)
-    ldxs = _spaced(x_scales, "x_scales", torch.float32, device, (M // 128, K), 4)
+    ldys, loose = _scales(dy_scales, "dy_scales", device, (M // 128, N))
+    ldxs, also = _scales(x_scales, "x_scales", device, (M // 128, K))
     shape = (N, K) if groups is None else (groups, N, K)
     kind, out, ldo, step = _output(out, dtype, shape, device, dy, groups, accumulate)
     p = _product_args(kind, bool(accumulate), M, N, K, groups or 0, 0 if offsets is None else offsets.data_ptr(), dy.data_ptr(), ldy, dy_scales.data_ptr(), ldys,
-                      x.data_ptr(), ldx, 0, x_scales.data_ptr(), ldxs, 0, out.data_ptr(), ldo, step)
+                      x.data_ptr(), ldx, 0, x_scales.data_ptr(), ldxs, 0, out.data_ptr(), ldo, step, loose or also)
     if N and K:
         _call((_lib or lib()).fmm_fp8_grad_weight(p, _stream(device)), "fmm_fp8_grad_weight")
     return out
