@@ -169,7 +169,7 @@ def prepare(case, seed):
     else:
         # the activations as the forward pass kept them
         codes, scales = _quantize_columns(_activations(M, K, torch.float32, gen), s.get("offsets"), pow2)
-        s["x"], s["xscales"] = _held(codes), _held_scales(scales)
+        s["x"], s["xscales"] = _held(codes), scales
         s["dy"] = torch.randn(M, N, device="cuda", generator=gen).to(dtype)
     return s
 
