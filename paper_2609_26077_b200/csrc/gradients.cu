@@ -160,7 +160,7 @@ template <int CAP> __global__ void __launch_bounds__(THREADS, 4) gradient_scale_
     for (uint32_t b = blockIdx.x; b < l.chunks; b += gridDim.x) {
         const uint32_t c = l.chunks - 1 - b;
         const Entry& e = l.e[find_entry(l, c)];
-        if (f.rest == 1.0f && e.out == e.x) continue;
+        if (f.power == 1.0f && f.rest == 1.0f && e.out == e.x) continue;      // (a factor just below 2^-64 has 2^-64 and 1)
         const long long at = (long long)(c - e.first) * l.chunk;
         const int n = (int)min((long long)l.chunk, e.size - at);
         if (e.type == FMM_TYPE_F32) chunk_scale(static_cast<const float*>(e.x) + at, static_cast<float*>(e.out) + at, n, f);
