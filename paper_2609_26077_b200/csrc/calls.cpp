@@ -86,23 +86,31 @@ at::Tensor spaced(int64_t rows, int64_t cols, int64_t step, at::ScalarType type,
     if (cols % step == 0) return empty({rows, cols}, type, p);
     return at::empty_strided({rows, cols}, {up(cols, step), 1}, at::TensorOptions().dtype(type).device(at::kCUDA, (c10::DeviceIndex)p.device));
 }
-bool output(PyObject* out, PyObject* dtype, at::IntArrayRef shape, const Place& p, at::Tensor& t, int& type, int64_t& ld, int64_t& step)
+// An output: the one that is given, in `t`, or of which type one has to be allocated (t undefined), dense
+bool output(PyObject* out, PyObject* dtype, at::IntArrayRef shape, const Place& p, at::Tensor& t, at::ScalarType& type, int64_t& ld, int64_t& step)
 {
     if (out == Py_None) {
         if (!THPDtype_Check(dtype)) return false;
-        const at::ScalarType st = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
-        if ((type = type_of(st)) < 0) return false;
-        t = empty(shape, st, p);
-    } else {
-        const at::Tensor* o = tensor(out);
-        if (!o || (type = type_of(o->scalar_type())) < 0 || !here(o, p, o->scalar_type()) || o->sizes() != shape) return false;
-        t = *o;
+        type = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
+        ld = shape.back();
+        step = shape.size() == 3 && shape[0] > 1 ? shape[1] * shape[2] : 0;
+        return type_of(type) >= 0;
     }
+    const at::Tensor* o = tensor(out);
+    if (!o || type_of(type = o->scalar_type()) < 0 || !here(o, p, type) || o->sizes() != shape) return false;
+    t = *o;
     const int64_t d = (int64_t)shape.size() - 2, rows = shape[d], cols = shape[d + 1];
     ld = t.stride(d);
     step = d && shape[0] > 1 ? t.stride(0) : 0;
     return t.stride(d + 1) == 1 && ld >= cols && (!step || step >= (rows - 1) * ld + cols);
 }
+
+// While one lives, other Python threads run: an allocation may wait for the device, a launch for its queue, and what the device waits for may be another
+// thread's to do.  Nothing of Python is touched meanwhile; the tensors are those of the caller's frame (lists: its own), which holds on to them.
+struct OthersRun {
+    PyThreadState* state = PyEval_SaveThread();
+    ~OthersRun() { PyEval_RestoreThread(state); }
+};
 
 #define NOT_USUAL(condition) if (condition) { PyErr_Clear(); Py_RETURN_NONE; }
 
@@ -124,20 +132,25 @@ PyObject* quantize(PyObject*, PyObject* const* args, Py_ssize_t n)
         a.type = (fmm_type_t)type; a.scale_mode = pow2 ? FMM_FP8_SCALE_POW2 : FMM_FP8_SCALE_AMAX_DIV_448;
         a.rows = rows; a.cols = cols; a.x = x->data_ptr(); a.ldx = ldx; a.groups = groups; a.offsets = offsets;
         at::Tensor out[4];
-        if (forms & 1) {
-            out[0] = spaced(rows, cols, 16, CODES, p);
-            out[1] = spaced(blocks(cols), rows, 4, at::kFloat, p);
-            a.codes = static_cast<uint8_t*>(out[0].data_ptr()); a.ldc = out[0].stride(0);
-            a.scales = static_cast<float*>(out[1].data_ptr()); a.lds = out[1].stride(0);
+        fmm_status_t status;
+        {
+            const OthersRun others;
+            if (forms & 1) {
+                out[0] = spaced(rows, cols, 16, CODES, p);
+                out[1] = spaced(blocks(cols), rows, 4, at::kFloat, p);
+                a.codes = static_cast<uint8_t*>(out[0].data_ptr()); a.ldc = out[0].stride(0);
+                a.scales = static_cast<float*>(out[1].data_ptr()); a.lds = out[1].stride(0);
+            }
+            if (forms & 2) {
+                const int64_t padded = (rows + 127 * std::max<int64_t>(groups, 1)) / 128 * 128;
+                out[2] = spaced(padded, cols, 16, CODES, p);
+                out[3] = spaced(padded / 128, cols, 4, at::kFloat, p);
+                a.column_codes = static_cast<uint8_t*>(out[2].data_ptr()); a.ldcc = out[2].stride(0);
+                a.column_scales = static_cast<float*>(out[3].data_ptr()); a.ldcs = out[3].stride(0);
+            }
+            status = reinterpret_cast<Quantize>(entry[QUANTIZE])(&a, p.stream);
         }
-        if (forms & 2) {
-            const int64_t padded = (rows + 127 * std::max<int64_t>(groups, 1)) / 128 * 128;
-            out[2] = spaced(padded, cols, 16, CODES, p);
-            out[3] = spaced(padded / 128, cols, 4, at::kFloat, p);
-            a.column_codes = static_cast<uint8_t*>(out[2].data_ptr()); a.ldcc = out[2].stride(0);
-            a.column_scales = static_cast<float*>(out[3].data_ptr()); a.ldcs = out[3].stride(0);
-        }
-        NOT_USUAL(reinterpret_cast<Quantize>(entry[QUANTIZE])(&a, p.stream) != FMM_OK);
+        NOT_USUAL(status != FMM_OK);
         const int first = forms & 1 ? 0 : 2, count = forms == 3 ? 4 : 2;
         PyObject* r = PyTuple_New(count);
         if (r) for (int i = 0; i < count; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(std::move(out[first + i])));
@@ -163,19 +176,25 @@ PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t n)
         NOT_USUAL(depth != (which == MATMUL ? K : N));
         NOT_USUAL(groups ? !dense(bs, p, at::kFloat, {groups, blocks(N), blocks(K)}) : !dense(bs, p, at::kFloat, {blocks(N), blocks(K)}));
         at::Tensor out;
-        int type;
+        at::ScalarType type;
         int64_t step;
         NOT_USUAL(!output(args[8], args[7], {M, cols}, p, out, type, c.ldo, step));
         if (args[6] != Py_None) {
             const at::Tensor* bias = tensor(args[6]);
-            NOT_USUAL(which != MATMUL || (groups ? !dense(bias, p, out.scalar_type(), {groups, N}) : !dense(bias, p, out.scalar_type(), {N})));
+            NOT_USUAL(which != MATMUL || (groups ? !dense(bias, p, type, {groups, N}) : !dense(bias, p, type, {N})));
             c.bias = bias->data_ptr();
         }
-        c.type = (fmm_type_t)type; c.accumulate = accumulate; c.M = M; c.N = N; c.K = K; c.groups = groups;
+        c.type = (fmm_type_t)type_of(type); c.accumulate = accumulate; c.M = M; c.N = N; c.K = K; c.groups = groups;
         c.a = static_cast<const uint8_t*>(a->data_ptr()); c.a_scales = static_cast<const float*>(as->data_ptr());
         c.b = static_cast<const uint8_t*>(b->data_ptr()); c.b_scales = static_cast<const float*>(bs->data_ptr());
-        c.out = out.data_ptr();
-        NOT_USUAL(reinterpret_cast<Product>(entry[which])(&c, p.stream) != FMM_OK);
+        fmm_status_t status;
+        {
+            const OthersRun others;
+            if (!out.defined()) out = empty({M, cols}, type, p);
+            c.out = out.data_ptr();
+            status = reinterpret_cast<Product>(entry[which])(&c, p.stream);
+        }
+        NOT_USUAL(status != FMM_OK);
         if (args[8] != Py_None) { Py_INCREF(args[8]); return args[8]; }
         return THPVariable_Wrap(std::move(out));
     } catch (...) { PyErr_Clear(); Py_RETURN_NONE; }
@@ -195,14 +214,21 @@ PyObject* grad_weight(PyObject*, PyObject* const* args, Py_ssize_t n)
         NOT_USUAL(accumulate < 0 || (accumulate && args[6] == Py_None) || groups < 0 || M == 0 || M % 128 || N == 0 || K == 0 || !matrix(dy, p, CODES, M, N, 16, c.lda) ||
                   !matrix(x, p, CODES, M, K, 16, c.ldb) || !scales_of(dys, p, M / 128, N, c.lda_scales, c.loose) || !scales_of(xs, p, M / 128, K, c.ldb_scales, c.loose));
         at::Tensor out;
-        int type;
-        const int64_t shape[3] = {groups, N, K};
-        NOT_USUAL(!output(args[6], args[5], groups ? at::IntArrayRef(shape, 3) : at::IntArrayRef(shape + 1, 2), p, out, type, c.ldo, c.step_out));
-        c.type = (fmm_type_t)type; c.accumulate = accumulate; c.M = M; c.N = N; c.K = K; c.groups = groups;
+        at::ScalarType type;
+        const int64_t dims[3] = {groups, N, K};
+        const at::IntArrayRef shape = groups ? at::IntArrayRef(dims, 3) : at::IntArrayRef(dims + 1, 2);
+        NOT_USUAL(!output(args[6], args[5], shape, p, out, type, c.ldo, c.step_out));
+        c.type = (fmm_type_t)type_of(type); c.accumulate = accumulate; c.M = M; c.N = N; c.K = K; c.groups = groups;
         c.a = static_cast<const uint8_t*>(dy->data_ptr()); c.a_scales = static_cast<const float*>(dys->data_ptr());
         c.b = static_cast<const uint8_t*>(x->data_ptr()); c.b_scales = static_cast<const float*>(xs->data_ptr());
-        c.out = out.data_ptr();
-        NOT_USUAL(reinterpret_cast<Product>(entry[GRAD_WEIGHT])(&c, p.stream) != FMM_OK);
+        fmm_status_t status;
+        {
+            const OthersRun others;
+            if (!out.defined()) out = empty(shape, type, p);
+            c.out = out.data_ptr();
+            status = reinterpret_cast<Product>(entry[GRAD_WEIGHT])(&c, p.stream);
+        }
+        NOT_USUAL(status != FMM_OK);
         if (args[6] != Py_None) { Py_INCREF(args[6]); return args[6]; }
         return THPVariable_Wrap(std::move(out));
     } catch (...) { PyErr_Clear(); Py_RETURN_NONE; }
@@ -237,11 +263,18 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
         }
         size_t need = 0;
         NOT_USUAL(reinterpret_cast<WorkspaceBytes>(entry[WORKSPACE_BYTES])(count, &need) != FMM_OK);
-        at::Tensor norm = empty({}, at::kFloat, p), workspace = empty({(int64_t)need}, at::kByte, p);
         const fmm_gradients_t g = {count, x.data(), out.empty() ? nullptr : out.data(), sizes.data(), types.data()};
-        float* to = static_cast<float*>(norm.data_ptr());
-        NOT_USUAL((only_norm ? reinterpret_cast<Norm>(entry[NORM])(&g, to, workspace.data_ptr(), need, p.stream)
-                             : reinterpret_cast<Clip>(entry[CLIP])(&g, max_norm, to, workspace.data_ptr(), need, p.stream)) != FMM_OK);
+        at::Tensor norm;
+        fmm_status_t status;
+        {
+            const OthersRun others;
+            norm = empty({}, at::kFloat, p);
+            const at::Tensor workspace = empty({(int64_t)need}, at::kByte, p);
+            float* to = static_cast<float*>(norm.data_ptr());
+            status = only_norm ? reinterpret_cast<Norm>(entry[NORM])(&g, to, workspace.data_ptr(), need, p.stream)
+                               : reinterpret_cast<Clip>(entry[CLIP])(&g, max_norm, to, workspace.data_ptr(), need, p.stream);
+        }
+        NOT_USUAL(status != FMM_OK);
         return THPVariable_Wrap(std::move(norm));
     } catch (...) { PyErr_Clear(); Py_RETURN_NONE; }
 }
