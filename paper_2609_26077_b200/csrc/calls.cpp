@@ -3,7 +3,8 @@
 // 45 ns for each property of each tensor of a list).
 //
 // Every function returns None where anything about its arguments is not as it expects (types, devices, strides, a refusal by the library), without having
-// done anything; the caller then goes the general way, which says what is wrong or does what is unusual.
+// enqueued anything but what a refused call may have left in its own workspace; the caller then goes the general way, which says what is wrong or does what
+// is unusual.  Any other failure of the library's is raised here: its work may have been enqueued, and must not be a second time.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <torch/csrc/Dtype.h>
@@ -114,9 +115,29 @@ struct OthersRun {
 
 #define NOT_USUAL(condition) if (condition) { PyErr_Clear(); Py_RETURN_NONE; }
 
+// What a function returns for a status that is not FMM_OK
+PyObject* failed(fmm_status_t status, const char* what)
+{
+    NOT_USUAL(status == FMM_ERR_INVALID_ARG || status == FMM_ERR_SHAPE || status == FMM_ERR_WORKSPACE);
+    PyErr_Clear();
+    PyObject* fmm = PyImport_ImportModule("paper_2609_26077_b200.fmm");
+    PyObject* r = fmm ? PyObject_CallMethod(fmm, "_check", "is", (int)status, what) : nullptr;      // raises FmmError
+    Py_XDECREF(fmm);
+    Py_XDECREF(r);
+    return nullptr;
+}
+// What it returns for a C++ exception, before or after the library has been called
+PyObject* thrown(bool called)
+{
+    NOT_USUAL(!called);
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "the call was made, its result could not be handed over");
+    return nullptr;
+}
+
 // quantize(x, offsets or None, pow2, forms): forms 1: along the rows, 2: along the columns, 3: both
 PyObject* quantize(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
+    bool called = false;
     try {
         NOT_USUAL(n != 4 || !entry[QUANTIZE]);
         const at::Tensor* x = tensor(args[0]);
@@ -148,19 +169,21 @@ PyObject* quantize(PyObject*, PyObject* const* args, Py_ssize_t n)
                 a.column_codes = static_cast<uint8_t*>(out[2].data_ptr()); a.ldcc = out[2].stride(0);
                 a.column_scales = static_cast<float*>(out[3].data_ptr()); a.ldcs = out[3].stride(0);
             }
+            called = true;
             status = reinterpret_cast<Quantize>(entry[QUANTIZE])(&a, p.stream);
         }
-        NOT_USUAL(status != FMM_OK);
+        if (status != FMM_OK) return failed(status, "fmm_fp8_quantize");
         const int first = forms & 1 ? 0 : 2, count = forms == 3 ? 4 : 2;
         PyObject* r = PyTuple_New(count);
         if (r) for (int i = 0; i < count; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(std::move(out[first + i])));
         return r;
-    } catch (...) { PyErr_Clear(); Py_RETURN_NONE; }
+    } catch (...) { return thrown(called); }
 }
 
 // product(which, a, a_scales, b, b_scales, offsets or None, bias or None, dtype, out or None, accumulate): which 1: matmul, 2: grad_input
 PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
+    bool called = false;
     try {
         NOT_USUAL(n != 10);
         const long which = PyLong_AsLong(args[0]);
@@ -192,17 +215,19 @@ PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t n)
             const OthersRun others;
             if (!out.defined()) out = empty({M, cols}, type, p);
             c.out = out.data_ptr();
+            called = true;
             status = reinterpret_cast<Product>(entry[which])(&c, p.stream);
         }
-        NOT_USUAL(status != FMM_OK);
+        if (status != FMM_OK) return failed(status, which == MATMUL ? "fmm_fp8_matmul" : "fmm_fp8_grad_input");
         if (args[8] != Py_None) { Py_INCREF(args[8]); return args[8]; }
         return THPVariable_Wrap(std::move(out));
-    } catch (...) { PyErr_Clear(); Py_RETURN_NONE; }
+    } catch (...) { return thrown(called); }
 }
 
 // grad_weight(dy, dy_scales, x, x_scales, offsets or None, dtype, out or None, accumulate)
 PyObject* grad_weight(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
+    bool called = false;
     try {
         NOT_USUAL(n != 8 || !entry[GRAD_WEIGHT]);
         const at::Tensor *dy = tensor(args[0]), *dys = tensor(args[1]), *x = tensor(args[2]), *xs = tensor(args[3]);
@@ -226,17 +251,19 @@ PyObject* grad_weight(PyObject*, PyObject* const* args, Py_ssize_t n)
             const OthersRun others;
             if (!out.defined()) out = empty(shape, type, p);
             c.out = out.data_ptr();
+            called = true;
             status = reinterpret_cast<Product>(entry[GRAD_WEIGHT])(&c, p.stream);
         }
-        NOT_USUAL(status != FMM_OK);
+        if (status != FMM_OK) return failed(status, "fmm_fp8_grad_weight");
         if (args[6] != Py_None) { Py_INCREF(args[6]); return args[6]; }
         return THPVariable_Wrap(std::move(out));
-    } catch (...) { PyErr_Clear(); Py_RETURN_NONE; }
+    } catch (...) { return thrown(called); }
 }
 
 // clip(list of tensors, max_norm, list of outputs or None), and the norm alone with max_norm None; the norm
 PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
+    bool called = false;
     try {
         NOT_USUAL(n != 3 || !PyList_Check(args[0]) || (args[2] != Py_None && !PyList_Check(args[2])) || !entry[WORKSPACE_BYTES] || !entry[NORM] || !entry[CLIP]);
         const bool only_norm = args[1] == Py_None;
@@ -271,12 +298,13 @@ PyObject* clip(PyObject*, PyObject* const* args, Py_ssize_t n)
             norm = empty({}, at::kFloat, p);
             const at::Tensor workspace = empty({(int64_t)need}, at::kByte, p);
             float* to = static_cast<float*>(norm.data_ptr());
+            called = true;
             status = only_norm ? reinterpret_cast<Norm>(entry[NORM])(&g, to, workspace.data_ptr(), need, p.stream)
                                : reinterpret_cast<Clip>(entry[CLIP])(&g, max_norm, to, workspace.data_ptr(), need, p.stream);
         }
-        NOT_USUAL(status != FMM_OK);
+        if (status != FMM_OK) return failed(status, only_norm ? "fmm_gradient_norm" : "fmm_gradient_clip");
         return THPVariable_Wrap(std::move(norm));
-    } catch (...) { PyErr_Clear(); Py_RETURN_NONE; }
+    } catch (...) { return thrown(called); }
 }
 
 // bind(addresses of the library's entry points, in the order of the list at the top)

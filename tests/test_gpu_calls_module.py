@@ -1,4 +1,4 @@
-"""What the module _calls does around the library's entry points: other Python threads run meanwhile."""
+"""What the module _calls does around the library's entry points: other Python threads run meanwhile, and a call that failed is not made again."""
 import ctypes as C
 import subprocess
 import threading
@@ -12,12 +12,14 @@ from paper_2609_26077_b200 import fmm, fp8, gradients
 pytestmark = pytest.mark.gpu
 
 ENTRIES = ["fmm_fp8_quantize", "fmm_fp8_matmul", "fmm_fp8_grad_input", "fmm_fp8_grad_weight", "fmm_gradient_workspace_bytes", "fmm_gradient_norm", "fmm_gradient_clip"]
+CUDA_ERROR = 6
 
 SOURCE = r"""
 #include <unistd.h>
 int calls = 0;
 int slow(void) { ++calls; usleep(400000); return 1; }        /* an argument that the library refuses, after a while */
-"""
+int fails(void) { ++calls; return %d; }                      /* an error of the device, after whatever was enqueued */
+""" % CUDA_ERROR
 
 
 @pytest.fixture
@@ -73,6 +75,18 @@ def test_other_threads_run_meanwhile(bound):
         assert count.value == 1
         # (a thread that holds on to the interpreter for the whole of the 0.4 s leaves none)
         assert len([t for t in ticks if start + 0.05 < t < start + 0.35]) >= 10
+
+
+def test_a_call_that_failed_is_not_made_again(bound):
+    """Its work may have been enqueued: once more would add or scale twice."""
+    calls = usual_calls()
+    for call, out in calls:
+        before = None if out is None else out.clone()
+        count = bound("fails")
+        with pytest.raises(fmm.FmmError):
+            call()
+        assert count.value == 1
+        assert out is None or torch.equal(out, before)
 
 
 def test_refusals_still_go_the_general_way():
