@@ -46,8 +46,17 @@ def build_calls(force: bool = False) -> str:
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
+    """The library, which needs nvcc alone, and the module, where torch and a compiler for it are there."""
+    out = build_library(force, verbose, debug)
+    try:
+        build_calls(force)
+    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+        print(f"{os.path.basename(CALLS_OUT)} is not built: {e}", file=sys.stderr)
+    return out
+
+
+def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     out = OUT_DEBUG if debug else OUT
-    build_calls(force)
     if not force and not _stale(out):
         return out
     objs = []
