@@ -1,5 +1,5 @@
-"""Build the CUDA library in-tree: paper_2609_26077_b200/libfmm_b200.so (sm_100a only), the Python module _calls.so that calls it for the usual
-arguments (csrc/calls.cpp, against the installed torch), and on request the library's checked twin libfmm_b200_debug.so (-DFMM_DEBUG: every global store of every kernel is range-checked)."""
+"""Build the CUDA library in-tree: paper_2609_26077_b200/libfmm_b200.so (sm_100a only), the Python module _calls that calls it for the usual
+arguments (csrc/calls.cpp, against the installed torch, which its file name tells), and on request the library's checked twin libfmm_b200_debug.so (-DFMM_DEBUG: every global store of every kernel is range-checked)."""
 import os
 import subprocess
 import sys
@@ -19,7 +19,7 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std
          "-Xcompiler", "-fPIC", "-cudart", "static"]
 
 
-CALLS_SOURCE, CALLS_OUT = os.path.join(CSRC, "calls.cpp"), os.path.join(HERE, "_calls.so")
+CALLS_SOURCE = os.path.join(CSRC, "calls.cpp")
 OUT_DEBUG = os.path.join(HERE, "libfmm_b200_debug.so")
 
 
@@ -31,18 +31,33 @@ def _stale(out):
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def calls_path() -> str:
+    """The module for the installed torch and this Python.  It knows how their objects lie in memory, so its name says which ones it was built against: that of
+    another torch is another file, and is not loaded."""
+    import torch
+    version = f"{torch.__version__}-{(torch.version.git_version or '')[:8]}-abi{int(torch._C._GLIBCXX_USE_CXX11_ABI)}"
+    return os.path.join(HERE, f"_calls.torch-{version}{sysconfig.get_config_var('EXT_SUFFIX')}")
+
+
 def build_calls(force: bool = False) -> str:
+    out = calls_path()
     headers = [h for h in HEADERS if h.endswith(("fmm.h", "fmm_int8.h", "fmm_fp8.h", "fmm_gradients.h"))]
-    if not force and os.path.exists(CALLS_OUT) and all(os.path.getmtime(d) <= os.path.getmtime(CALLS_OUT) for d in [CALLS_SOURCE] + headers):
-        return CALLS_OUT
+    if not force and os.path.exists(out) and all(os.path.getmtime(d) <= os.path.getmtime(out) for d in [CALLS_SOURCE] + headers):
+        return out
     import torch
     at = os.path.dirname(torch.__file__)
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
     for include in (os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
                     os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include")):
         cmd += ["-isystem", include]
-    subprocess.check_call(cmd + [CALLS_SOURCE, "-o", CALLS_OUT, "-L" + os.path.join(at, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python"])
-    return CALLS_OUT
+    part = f"{out}.{os.getpid()}.so"                          # (a process that loads the module meanwhile sees the old one or the new one)
+    try:
+        subprocess.check_call(cmd + [CALLS_SOURCE, "-o", part, "-L" + os.path.join(at, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python"])
+        os.replace(part, out)
+    finally:
+        if os.path.exists(part):
+            os.remove(part)
+    return out
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
@@ -51,7 +66,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     try:
         build_calls(force)
     except (ImportError, OSError, subprocess.CalledProcessError) as e:
-        print(f"{os.path.basename(CALLS_OUT)} is not built: {e}", file=sys.stderr)
+        print(f"the module for the usual calls is not built: {e}", file=sys.stderr)
     return out
 
 

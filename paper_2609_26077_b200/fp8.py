@@ -35,10 +35,13 @@ from __future__ import annotations
 
 import collections
 import ctypes as C
+import importlib.util
+import types
+import warnings
 
 import torch
 
-from . import fmm, int8
+from . import build, fmm, int8
 from .int8 import _call, _device, _elsewhere, _float_type, _matrix, _packer, _stream, _suits, _vector
 
 BLOCK = 128
@@ -72,7 +75,7 @@ class ProductArgs(C.Structure):
 
 _quantize_args, _weight_args, _product_args = _packer(QuantizeArgs), _packer(QuantizeWeightArgs), _packer(ProductArgs)
 _lib = None
-_calls = None               # the module of that name, once lib() has run
+_calls = None               # the module of that name, or what stands in for it, once lib() has run
 
 
 def lib():
@@ -84,11 +87,24 @@ def lib():
         L.fmm_fp8_column_rows.argtypes = [C.c_int64, C.c_int64, C.c_void_p]
         L.fmm_fp8_status.argtypes = [C.c_void_p]
         L.fmm_fp8_selftest_bounded_wait.argtypes = [C.c_int64, C.c_void_p]
-        from . import _calls as module
-        module.bind(*(C.cast(getattr(L, name), C.c_void_p).value for name in (
-            "fmm_fp8_quantize", "fmm_fp8_matmul", "fmm_fp8_grad_input", "fmm_fp8_grad_weight", "fmm_gradient_workspace_bytes", "fmm_gradient_norm", "fmm_gradient_clip")))
-        _calls, _lib = module, L
+        _calls, _lib = _load_calls(L), L
     return _lib
+
+
+def _load_calls(L):
+    """The module that makes the usual calls, or, where there is none for this torch and Python, one that leaves them all to the general way."""
+    spec = importlib.util.spec_from_file_location(__package__ + "._calls", build.calls_path())
+    try:
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError as e:
+        warnings.warn(f"calls go through ctypes, which takes the host some microseconds more, as there is no module for torch {torch.__version__} ({e}): "
+                      f"`python -m {__package__}.build` makes it", RuntimeWarning, stacklevel=4)
+        declines = lambda *a: None
+        return types.SimpleNamespace(quantize=declines, product=declines, grad_weight=declines, clip=declines)
+    module.bind(*(C.cast(getattr(L, name), C.c_void_p).value for name in (
+        "fmm_fp8_quantize", "fmm_fp8_matmul", "fmm_fp8_grad_input", "fmm_fp8_grad_weight", "fmm_gradient_workspace_bytes", "fmm_gradient_norm", "fmm_gradient_clip")))
+    return module
 
 
 def _usual():

@@ -94,3 +94,16 @@ def test_refusals_still_go_the_general_way():
     with pytest.raises(fmm.FmmError, match="fmm_gradient_clip"):
         gradients.clip([t, t], 1.0)
     assert (t == 1).all()
+
+
+def test_without_the_module_the_general_way_does_it(monkeypatch, tmp_path):
+    x, w = torch.randn(40, 200, device="cuda"), fp8.quantize_weight(torch.randn(72, 200, device="cuda"))
+    step = lambda: (*(t.view(torch.uint8) for t in fp8.quantize(x)), fp8.matmul(*fp8.quantize(x), *w), gradients.norm([x]), gradients.clip([x], 1.0, out=[torch.empty_like(x)]))
+    want = step()
+    monkeypatch.setattr(fp8.build, "calls_path", lambda: str(tmp_path / "_calls.so"))
+    monkeypatch.setattr(fp8, "_lib", None)
+    monkeypatch.setattr(fp8, "_calls", None)
+    with pytest.warns(RuntimeWarning, match="through ctypes"):
+        got = step()
+    assert fp8._usual().quantize(x, None, False, 1) is None
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
