@@ -84,8 +84,9 @@ fmm_status_t fmm_fp8_quantize_weight(const fmm_fp8_quantize_weight_t* p, void* c
  *     fmm_fp8_matmul       out[i][j]    (+)= sum_k a[i][k] b_g[j][k] + bias_g[j]    a: M x K along its rows,   b_g: N x K in tiles, out M x N
  *     fmm_fp8_grad_input   out[i][k]    (+)= sum_j a[i][j] b_g[j][k]                a: M x N (dy), its rows,   b_g: N x K in tiles, out M x K
  *     fmm_fp8_grad_weight  out_g[j][k]  (+)= sum_i a[i][j] b[i][k]                  a: M x N (dy) and b: M x K along their columns, out_g N x K
- *   M: tokens; grad_weight: rows of the form along the columns, a multiple of 128 (FMM_ERR_SHAPE).  It does not know the number of tokens, so
- *   that offsets beyond that are not cut to it there as elsewhere: nothing is read outside of the M rows, but that group's gradient is not specified.
+ *   M: tokens; grad_weight: rows of the form along the columns, a multiple of 128 (FMM_ERR_SHAPE).  tokens: of a grouped grad_weight only, the number of
+ *   tokens (from 1 to M, else FMM_ERR_SHAPE), to which offsets are cut as elsewhere; 0: it is not known, and with offsets beyond it nothing is read outside of the
+ *   M rows, but the gradients of groups that end there are not specified.
  *   a, lda, a_scales, lda_scales; b, ldb, b_scales as the forms have them, ldb_scales: of grad_weight's b only.  loose != 0: scales along rows and
  *   columns as any fp32 numbers.  step_b: codes from one group's weight to the next (a multiple of 16), whose scales are dense.  bias: groups x N of `type`, dense, or NULL (gradients: NULL).
  *   out: of `type`; step_out: elements from one group's weight gradient to the next.  accumulate != 0 adds to what it holds; without, a group
@@ -103,7 +104,7 @@ typedef struct {
     const float* b_scales;  int64_t ldb_scales;
     const void* bias;
     void* out;              int64_t ldo, step_out;
-    int64_t loose;
+    int64_t loose, tokens;
 } fmm_fp8_product_t;
 fmm_status_t fmm_fp8_matmul(const fmm_fp8_product_t* p, void* cuda_stream);
 fmm_status_t fmm_fp8_grad_input(const fmm_fp8_product_t* p, void* cuda_stream);

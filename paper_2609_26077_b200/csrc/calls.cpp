@@ -224,17 +224,21 @@ PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t n)
     } catch (...) { return thrown(called); }
 }
 
-// grad_weight(dy, dy_scales, x, x_scales, offsets or None, dtype, out or None, accumulate)
+// grad_weight(dy, dy_scales, x, x_scales, offsets or None, dtype, out or None, accumulate[, tokens or None])
 PyObject* grad_weight(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
     bool called = false;
     try {
-        NOT_USUAL(n != 8 || !entry[GRAD_WEIGHT]);
+        NOT_USUAL((n != 8 && n != 9) || !entry[GRAD_WEIGHT]);
         const at::Tensor *dy = tensor(args[0]), *dys = tensor(args[1]), *x = tensor(args[2]), *xs = tensor(args[3]);
         Place p;
         NOT_USUAL(!place_of(dy, p) || dy->dim() != 2 || !x || x->dim() != 2);
         fmm_fp8_product_t c = {};
         const int accumulate = PyObject_IsTrue(args[7]);
+        if (n == 9 && args[8] != Py_None) {
+            c.tokens = PyLong_AsLongLong(args[8]);
+            NOT_USUAL(c.tokens <= 0);                        // (none: the general way; -1 also where it is no number)
+        }
         const int64_t groups = groups_of(args[4], p, c.offsets), M = dy->size(0), N = dy->size(1), K = x->size(1);
         NOT_USUAL(accumulate < 0 || (accumulate && args[6] == Py_None) || groups < 0 || M == 0 || M % 128 || N == 0 || K == 0 || !matrix(dy, p, CODES, M, N, 16, c.lda) ||
                   !matrix(x, p, CODES, M, K, 16, c.ldb) || !scales_of(dys, p, M / 128, N, c.lda_scales, c.loose) || !scales_of(xs, p, M / 128, K, c.ldb_scales, c.loose));

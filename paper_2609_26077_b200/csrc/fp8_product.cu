@@ -904,6 +904,7 @@ template <int KIND> fmm_status_t product(const fmm_fp8_product_t* a, void* strea
     if (!a || !int8_type_ok(a->type)) return FMM_ERR_INVALID_ARG;
     const int64_t M = a->M, N = a->N, K = a->K, groups = a->groups, count = groups ? groups : 1;
     if (!dim_ok(M) || !dim_ok(N) || !dim_ok(K) || groups < 0 || groups > FMM_FP8_MAX_GROUPS || (KIND == GRAD_W && M % 128)) return FMM_ERR_SHAPE;
+    if (KIND == GRAD_W && groups && (a->tokens < 0 || a->tokens > M)) return FMM_ERR_SHAPE;
     const int64_t rows = KIND == GRAD_W ? N : M, cols = KIND == MATMUL ? N : K, depth = KIND == MATMUL ? K : KIND == GRAD_X ? N : M;
     if (rows == 0 || cols == 0) return FMM_OK;
     const int64_t e = int8_type_bytes(a->type);
@@ -919,7 +920,7 @@ template <int KIND> fmm_status_t product(const fmm_fp8_product_t* a, void* strea
     }
     ProductParams p = {};
     p.rows = (int)rows; p.cols = (int)cols; p.depth = (int)depth;
-    p.groups = (int)groups; p.offsets = a->offsets; p.tokens = (int)M;
+    p.groups = (int)groups; p.offsets = a->offsets; p.tokens = (int)(KIND == GRAD_W && a->tokens ? a->tokens : M);
     p.a = a->a; p.lda = a->lda; p.a_scales = a->a_scales; p.lda_scales = a->lda_scales;
     p.b = a->b; p.ldb = a->ldb; p.step_b = KIND != GRAD_W && count > 1 ? a->step_b : 0; p.b_scales = a->b_scales; p.ldb_scales = a->ldb_scales;
     p.bias = a->bias; p.out = a->out; p.ldo = a->ldo; p.step_out = KIND == GRAD_W && count > 1 ? a->step_out : 0;

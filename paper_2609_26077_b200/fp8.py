@@ -36,6 +36,7 @@ from __future__ import annotations
 import collections
 import ctypes as C
 import importlib.util
+import operator
 import types
 import warnings
 
@@ -70,7 +71,7 @@ class ProductArgs(C.Structure):
     _fields_ = [("type", C.c_int), ("accumulate", C.c_int), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("groups", C.c_int64),
                 ("offsets", C.c_void_p), ("a", C.c_void_p), ("lda", C.c_int64), ("a_scales", C.c_void_p), ("lda_scales", C.c_int64),
                 ("b", C.c_void_p), ("ldb", C.c_int64), ("step_b", C.c_int64), ("b_scales", C.c_void_p), ("ldb_scales", C.c_int64),
-                ("bias", C.c_void_p), ("out", C.c_void_p), ("ldo", C.c_int64), ("step_out", C.c_int64), ("loose", C.c_int64)]
+                ("bias", C.c_void_p), ("out", C.c_void_p), ("ldo", C.c_int64), ("step_out", C.c_int64), ("loose", C.c_int64), ("tokens", C.c_int64)]
 
 
 _quantize_args, _weight_args, _product_args = _packer(QuantizeArgs), _packer(QuantizeWeightArgs), _packer(ProductArgs)
@@ -356,7 +357,7 @@ def _product(which, a, a_scales, b, b_scales, offsets, bias, dtype, out, accumul
     if bias is not None:
         _vector(bias, "bias", out.dtype, device, (N,) if groups is None else (groups, N))
     p = _product_args(kind, bool(accumulate), M, N, K, groups or 0, 0 if offsets is None else offsets.data_ptr(), a.data_ptr(), lda, a_scales.data_ptr(), lds,
-                      b.data_ptr(), ldb, step_b, b_scales.data_ptr(), 0, 0 if bias is None else bias.data_ptr(), out.data_ptr(), ldo, 0, loose)
+                      b.data_ptr(), ldb, step_b, b_scales.data_ptr(), 0, 0 if bias is None else bias.data_ptr(), out.data_ptr(), ldo, 0, loose, 0)
     if M and shape[1]:
         _call(getattr(_lib or lib(), which)(p, _stream(device)), which)
     return out
@@ -421,7 +422,7 @@ def grouped_grad_input(dy, dy_scales, b, b_scales, offsets, dtype=torch.bfloat16
     return _product("fmm_fp8_grad_input", dy, dy_scales, b, b_scales, offsets, None, dtype, out, accumulate, device)
 
 
-def _grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate, device):
+def _grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate, tokens, device):
     groups = None if offsets is None else _groups(offsets, device)
     _suits(dy, "dy", CODES, device)
     _suits(x, "x", CODES, device)
@@ -432,10 +433,16 @@ def _grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate, de
     ldy, ldx = _spaced(dy, "dy", CODES, device, None, 16), _spaced(x, "x", CODES, device, None, 16)
     ldys, loose = _scales(dy_scales, "dy_scales", device, (M // 128, N))
     ldxs, also = _scales(x_scales, "x_scales", device, (M // 128, K))
+    if tokens is not None:
+        tokens = operator.index(tokens)
+        if not 0 <= tokens <= M:
+            raise ValueError(f"tokens: {tokens}, 0 to {M} is needed")
+        if tokens == 0:                                      # no group has any, whatever the offsets say
+            M = 0
     shape = (N, K) if groups is None else (groups, N, K)
     kind, out, ldo, step = _output(out, dtype, shape, device, dy, groups, accumulate)
     p = _product_args(kind, bool(accumulate), M, N, K, groups or 0, 0 if offsets is None else offsets.data_ptr(), dy.data_ptr(), ldy, dy_scales.data_ptr(), ldys,
-                      x.data_ptr(), ldx, 0, x_scales.data_ptr(), ldxs, 0, out.data_ptr(), ldo, step, loose or also)
+                      x.data_ptr(), ldx, 0, x_scales.data_ptr(), ldxs, 0, out.data_ptr(), ldo, step, loose or also, tokens or 0)
     if N and K:
         _call((_lib or lib()).fmm_fp8_grad_weight(p, _stream(device)), "fmm_fp8_grad_weight")
     return out
@@ -453,13 +460,14 @@ def grad_weight(dy, dy_scales, x, x_scales, dtype=torch.float32, out=None, accum
     if where is not None:
         with where:
             return grad_weight(dy, dy_scales, x, x_scales, dtype, out, accumulate)
-    return _grad_weight(dy, dy_scales, x, x_scales, None, dtype, out, accumulate, device)
+    return _grad_weight(dy, dy_scales, x, x_scales, None, dtype, out, accumulate, None, device)
 
 
-def grouped_grad_weight(dy, dy_scales, x, x_scales, offsets, dtype=torch.float32, out=None, accumulate=False, stream=None):
-    """grad_weight for each group of rows: E x N x K, zeros (or nothing added) where a group has no rows."""
+def grouped_grad_weight(dy, dy_scales, x, x_scales, offsets, dtype=torch.float32, out=None, accumulate=False, stream=None, tokens=None):
+    """grad_weight for each group of rows: E x N x K, zeros (or nothing added) where a group has no rows.  tokens: their number, which the forms along the
+    columns do not tell, to which offsets beyond it are cut, as the other calls do; without it there must be none."""
     if stream is None and offsets is not None:
-        r = (_calls or _usual()).grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate)
+        r = (_calls or _usual()).grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate, tokens)
         if r is not None:
             return r
     device = _device(dy)
@@ -467,8 +475,8 @@ def grouped_grad_weight(dy, dy_scales, x, x_scales, offsets, dtype=torch.float32
     where = _elsewhere(device, stream)
     if where is not None:
         with where:
-            return grouped_grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate)
-    return _grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate, device)
+            return grouped_grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate, tokens=tokens)
+    return _grad_weight(dy, dy_scales, x, x_scales, offsets, dtype, out, accumulate, tokens, device)
 
 
 def force_tile(columns=0, shares=1):

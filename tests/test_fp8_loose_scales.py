@@ -1,4 +1,4 @@
-"""CPU checks of scales that lie as any fp32 numbers do: what is refused all the same."""
+"""CPU checks of scales that lie as any fp32 numbers do, and of a number of tokens that is told: what is refused all the same."""
 import ctypes as C
 
 import pytest
@@ -6,7 +6,7 @@ import pytest
 from paper_2609_26077_b200 import build as fmm_build
 from paper_2609_26077_b200 import fp8
 
-OK, INVALID = 0, 1
+OK, INVALID, SHAPE = 0, 1, 2
 P = 4096                    # an address that is never followed: every call here is refused, or has nothing to do
 
 
@@ -44,3 +44,12 @@ def test_products(lib, which):
             (dict(lda_scales=64), dict(ldb_scales=32)) if which == "grad_weight" else ()):
         assert call(loose=1, **bad) == INVALID, bad
     assert call(loose=1, **dict(matmul=dict(N=0), grad_input=dict(K=0), grad_weight=dict(N=0))[which]) == OK
+
+
+def test_tokens(lib):
+    """The number of tokens that a grouped weight gradient's offsets are cut to."""
+    base = dict(type=0, M=256, N=64, K=32, groups=2, offsets=P, a=P, lda=64, a_scales=P, lda_scales=64, b=P, ldb=32, b_scales=P, ldb_scales=32, out=P, ldo=32, step_out=2048)
+    call = lambda **kw: lib.fmm_fp8_grad_weight(filled(fp8.ProductArgs, base, kw), None)
+    for bad in (-1, 257, 1 << 40):
+        assert call(tokens=bad) == SHAPE
+    assert call(tokens=200, N=0) == OK
