@@ -282,10 +282,11 @@ __device__ __forceinline__ void put_tile(const ProductParams& p, const CUtensorM
 // while another leaves TMEM.
 // Two TMEM accumulators (narrow tiles: four): a block is multiplied while the ones before it leave TMEM.  What issues the MMAs bounds the loop before the tensor pipe
 // does, so it has one barrier to wait for and one to signal for a block: `full` counts the operands of a stage and the warps that have taken the sums
-// of an earlier block out of the accumulator that this one will take; `done` says to those warps that their sums are complete and to the producer that
-// the stage is free.  A block's scales, which those warps read and the MMAs do not, have a slot of their own and a barrier of the CTA that reads them.
-//   warp 0 TMA producer, warp 1 MMA issuer, warp 2 finds the tiles, warp 3 loads scales that TMA cannot, warps 4 .. 11 sums and output: a TMEM lane
-//   quadrant and half of the columns each
+// of an earlier block out of the accumulator that this one will take; `done` says to those warps that their sums are complete and their scales are there, and
+// to the producer that the stage is free.  A block's scales, which those warps read and the MMAs do not, have a slot of their own, and a barrier of the CTA
+// that reads them.
+//   warp 0 TMA producer, warp 1 MMA issuer, warp 2 finds the tiles, warp 3 sees to the scales, warps 4 .. 11 sums and output: a TMEM lane quadrant and
+//   half of the columns each
 template <int KIND, int NCTA, int TN> struct Cfg {
     static constexpr int TM = 128 * NCTA, A_BYTES = 128 * 128, B_ROWS = TN / NCTA, B_BYTES = B_MN<KIND> ? BOX : B_ROWS * 128, STAGE_BYTES = A_BYTES + B_BYTES;
     static_assert(!B_MN<KIND> || B_ROWS == 128, "an MN-major box is 128 elements wide");
@@ -304,7 +305,7 @@ template <int KIND, int NCTA, int TN> struct Cfg {
     static constexpr int BUFS = TN == 256 ? 2 : 4, TMEM_COLS = BUFS * TN;
     static_assert(BUFS <= STAGES, "operands of the block that takes an accumulator next are counted by a barrier that has come round");
     // Block b is loaded when block b - STAGES has been multiplied, for which all warps have left the accumulator of block b - STAGES - BUFS; they may be
-    // at its last piece still.  So they have seen the slot's barrier come round, too, before it is armed again.
+    // at its last piece still.
     static_assert(SLOTS > STAGES + BUFS, "scales are not overwritten while they are read");
     static constexpr int REGS_AT_LAUNCH = 168, REGS_CTRL = 56, REGS_OUT = 224;
     static_assert(128 * REGS_CTRL + OUT_WARPS * 32 * REGS_OUT <= THREADS * REGS_AT_LAUNCH, "register pool");
@@ -336,10 +337,10 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const bool leader = rank == 0;
     if (warp == 2 && elect_one()) { prefetch_map(&tmA); prefetch_map(&tmB); }
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1 + NCTA * (C::OUT_WARPS + (p.loose ? 1 : 0))); mbar_init(bar_done(s), 1); }
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(bar_full(s), 1 + NCTA * C::OUT_WARPS); mbar_init(bar_done(s), 2); }
         for (int s = 0; s < C::SLOTS; ++s) mbar_init(bar_scales(s), 1);
-        // the output warps, the producer, the issuer, the warp that loads loose scales
-        for (int i = 0; i < TILE_RING; ++i) { mbar_init(bar_ring + 8u * i, 1); mbar_init(bar_ring + 8u * (TILE_RING + i), C::OUT_WARPS + 1 + leader + (p.loose ? 1 : 0)); }
+        // the output warps, the producer, the warp of the scales, the issuer
+        for (int i = 0; i < TILE_RING; ++i) { mbar_init(bar_ring + 8u * i, 1); mbar_init(bar_ring + 8u * (TILE_RING + i), C::OUT_WARPS + 2 + leader); }
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -418,39 +419,40 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             }
             if (!ring.put(t, ctl) || t.group < 0) break;
         }
-    } else if (p.loose) {
-        // Scales that TMA cannot load come by way of this warp's registers (4096 cubed 71 to 75 us, by TMA 71; 8192 cubed 535 of 495, weight gradient 717 of
-        // 679).  The MMAs wait for it too, so that it falls no round of stages behind.  Beyond the last row or column: 0, as by TMA.
-        int stage = 0, slot = 0; uint32_t phase = 0;
+    } else {
+        // A block's scales are there: said to the output warps by an arrival of this warp, which has seen it, beside that of the MMAs, which says nothing of
+        // what TMA has copied.  (A wait of each output warp for its scales costs a tenth of the time: 4096 cubed 70 to 76 us instead of 64 to 68.)  Scales
+        // that TMA cannot load come by way of this warp's registers (4096 cubed 71 us instead of 68, 8192 cubed 528 instead of 522, weight gradient 709
+        // instead of 672); beyond the last row or column: 0, as by TMA.
+        int stage = 0, slot = 0; uint32_t phase = 0, slot_phase = 0;
         bool ok = true;
         while (ok) {
             const Tile t = ring.get(ctl);
             if (t.group < 0) break;
             const int row = t.row0 + rank * 128;
             for (int kb = t.kb0; kb < t.kb0 + t.kbs; ++kb) {
-                const float *rows_from = p.a_scales + kb * p.lda_scales + row + lane, *cols_from = p.b_scales + kb * p.ldb_scales + t.col0 + lane;
-                float r[4] = {}, c[TN / 32] = {};
+                if (p.loose) {
+                    const float *rows_from = p.a_scales + kb * p.lda_scales + row + lane, *cols_from = p.b_scales + kb * p.ldb_scales + t.col0 + lane;
+                    float r[4] = {}, c[TN / 32] = {};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) if (row + 32 * i + lane < p.rows) r[i] = __ldg(rows_from + 32 * i);
-                if (KIND == GRAD_W) {
+                    for (int i = 0; i < 4; ++i) if (row + 32 * i + lane < p.rows) r[i] = __ldg(rows_from + 32 * i);
+                    if (KIND == GRAD_W) {
 #pragma unroll
-                    for (int i = 0; i < TN / 32; ++i) if (t.col0 + 32 * i + lane < p.cols) c[i] = __ldg(cols_from + 32 * i);
-                }
-                if (!mbar_wait_warp(bar_done(stage), phase ^ 1u, ctl, 2617)) { ok = false; break; }
-                const uint32_t to = base + C::OFF_SCALES + slot * C::SLOT + 4 * lane;
+                        for (int i = 0; i < TN / 32; ++i) if (t.col0 + 32 * i + lane < p.cols) c[i] = __ldg(cols_from + 32 * i);
+                    }
+                    if (!mbar_wait_warp(bar_done(stage), phase ^ 1u, ctl, 2617)) { ok = false; break; }
+                    const uint32_t to = base + C::OFF_SCALES + slot * C::SLOT + 4 * lane;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sts32f(to + ((row & 3) + 32 * i) * 4, r[i]);
-                if (KIND == GRAD_W) {
+                    for (int i = 0; i < 4; ++i) sts32f(to + ((row & 3) + 32 * i) * 4, r[i]);
+                    if (KIND == GRAD_W) {
 #pragma unroll
-                    for (int i = 0; i < TN / 32; ++i) sts32f(to + 640 + 128 * i, c[i]);
-                }
-                __syncwarp();
-                if (elect_one()) {
-                    mbar_arrive(bar_scales(slot));
-                    if (NCTA == 2) mbar_arrive_cluster(bar_full(stage) & PEER_BIT_MASK); else mbar_arrive(bar_full(stage));
-                }
+                        for (int i = 0; i < TN / 32; ++i) sts32f(to + 640 + 128 * i, c[i]);
+                    }
+                    __syncwarp();
+                } else if (!mbar_wait_warp(bar_scales(slot), slot_phase, ctl, 2616)) { ok = false; break; }
+                if (elect_one()) mbar_arrive(bar_done(stage));
                 if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
-                if (++slot == C::SLOTS) slot = 0;
+                if (++slot == C::SLOTS) { slot = 0; slot_phase ^= 1u; }
             }
         }
     }
@@ -476,7 +478,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             const long long blocks_c = (p.cols + 127) / 128, c = min((t.col0 + half * COLS) / 128, (int)blocks_c - 1), all = (p.depth + 127) / 128, b = t.kb0 + kb + lane;
             return __ldg(p.b_scales + t.group * blocks_c * all + (KIND == MATMUL ? c * all + b : b * blocks_c + c));
         };
-        int slot = 0; uint32_t slot_phase = 0;
+        int slot = 0;
         Tile t = ring.get(ctl);
         scales_now = fetch(t, 0);
         float sum[COLS];
@@ -494,14 +496,8 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             auto arrived = [&](uint32_t (&r)[CH]) {
                 if constexpr (CH == 32) tmem_ld_wait32(r); else tmem_ld_wait16(r);
             };
-            // A block's scales and its sums.  (`done` says nothing of the scales: TMA copied them, which these warps see through a barrier that counts its
-            // bytes.  They are there long before the sums, so that their wait is part of that for these.)
-            auto wait_block = [&] {
-                const bool scales = mbar_wait(bar_scales(slot), slot_phase, ctl, 2616);
-                return __all_sync(0xffffffffu, scales && mbar_wait(bar_done(stage), phase, ctl, 2613));
-            };
             if (t.kbs > 0) {
-                if (!wait_block()) { ok = false; break; }
+                if (!mbar_wait_warp(bar_done(stage), phase, ctl, 2613)) { ok = false; break; }
                 tc_fence_after();
                 load(v[0], 0);
             }
@@ -513,7 +509,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                 const uint32_t cols_at = base + C::OFF_SCALES + slot * C::SLOT + 640 + half * COLS * 4;
                 const float row_scale = lds32f(base + C::OFF_SCALES + slot * C::SLOT + row_at);
                 const float factor = KIND == GRAD_W ? 0.0f : row_scale * __shfl_sync(0xffffffffu, scales_now, kb & 31);
-                if (++slot == C::SLOTS) { slot = 0; slot_phase ^= 1u; }
+                if (++slot == C::SLOTS) slot = 0;
 #pragma unroll
                 for (int i = 0; i < COLS / CH; ++i) {
                     uint32_t (&now)[CH] = v[i & 1], (&then)[CH] = v[(i + 1) & 1];
@@ -527,7 +523,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
                         if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
                         if (++buf == C::BUFS) buf = 0;
                         if (kb + 1 < t.kbs) {
-                            if (!wait_block()) { ok = false; break; }
+                            if (!mbar_wait_warp(bar_done(stage), phase, ctl, 2613)) { ok = false; break; }
                             tc_fence_after();
                             load(then, 0);
                         }

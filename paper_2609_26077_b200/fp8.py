@@ -26,7 +26,7 @@ each 128 rows x K, of tiles ceil(N / 128) x ceil(K / 128).  The form along the c
 multiple of 128; what is behind the last group in use is not written.  Rows of a grouped call that belong to no group take no part and are not written.
 
 Matrices are 2-D CUDA tensors whose columns are contiguous (rows may lie any distance apart; those of codes start on 16-byte boundaries, as the ones
-that are allocated here do, and so may those of scales along rows or columns: where they do not, large products take up to a twelfth longer).  All tensors of
+that are allocated here do, and so may those of scales along rows or columns: where they do not, large products take up to a twentieth longer).  All tensors of
 a call are on one device, on whose current stream the work is enqueued, or on `stream`; nothing is synchronised, and calls may be captured into CUDA graphs.  Outputs are allocated unless they are
 given; a given one may not overlap an input or another output.  Unsuitable arguments raise TypeError (types, devices) or ValueError (shapes,
 strides), anything that the library refuses raises fmm.FmmError.  Nothing is recorded for autograd: the gradients are calls of their own.
