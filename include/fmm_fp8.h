@@ -91,8 +91,9 @@ fmm_status_t fmm_fp8_quantize_weight(const fmm_fp8_quantize_weight_t* p, void* c
  *   columns as any fp32 numbers.  step_b: codes from one group's weight to the next (a multiple of 16), whose scales are dense.  bias: groups x N of `type`, dense, or NULL (gradients: NULL).
  *   out: of `type`; step_out: elements from one group's weight gradient to the next.  accumulate != 0 adds to what it holds; without, a group
  *   without rows has 0 as its weight gradient.
- *   Arithmetic: the products of a block of 128 are summed by the tensor cores in fp32, the blocks' sums, times their two scales (whose product
- *   is taken in fp32), in fp32 registers, rounded to nearest; the result is rounded once. */
+ *   Arithmetic: the products of a block of 128 are summed by the tensor cores in fp32, the blocks' sums, times their two scales, in fp32 registers,
+ *   rounded to nearest; the result is rounded once.  The two scales are multiplied first, in fp32 (grad_weight: the sum times b's scale, then a's), so that
+ *   scales whose product is beyond fp32 give infinities or NaN. */
 typedef struct {
     fmm_type_t type;
     int accumulate;

@@ -275,10 +275,15 @@ __device__ __forceinline__ void put_tile(const ProductParams& p, const CUtensorM
 
 // ------------------------------------------------------------------------------------------------ kernel
 // Persistent CTAs, or pairs of them (cta_group::2) that share a tile of 256 x 256: each loads its 128 rows and half of the columns.
-// Bound by the shared memory port and the power limit.  For a block of a pair's tile the tensor pipe takes 512 cycles; the MMAs read 48 KB from shared
-// memory and TMA writes 32 KB, 640 cycles at 128 bytes a clock; the loop takes about 675 (the weight gradient, whose output warps read 256 column
-// scales besides, 1050).  16384 x 8192 x 8192: 886 us in a single call (2.48 PFLOP/s, tensor pipe 73 % of the cycles), 1050 to 1110 in a long run at
-// 1.2 to 1.5 GHz; 8192 cubed 510 to 535, input gradient 490 to 515, weight gradient in fp32 630 to 680.  Larger tiles would not let a block be multiplied
+// Bound by the way of the sums through the output warps, then by the power limit.  Cycles for a block of a pair's tile, of which the tensor pipe takes 512
+// (8192 cubed, 64 blocks a tile, the tiles' output included; product, input gradient, weight gradient):
+//   as it is                                                 704    697    1028
+//   without the loads from TMEM                              681    696    1040
+//   without the multiply-adds                                636    638     698
+//   sums left in TMEM for a tile's 64 blocks                 610    609     660
+//   one read of the columns' scales a block instead of 32                   904
+// 16384 x 8192 x 8192: 880 us in a single call (2.50 PFLOP/s, tensor pipe 73 % of the cycles), 1040 to 1120 in a long run at
+// 1.2 to 1.5 GHz; 8192 cubed 506 to 539, input gradient 479 to 525, weight gradient in fp32 647 to 693.  Larger tiles would not let a block be multiplied
 // while another leaves TMEM.
 // Two TMEM accumulators (narrow tiles: four): a block is multiplied while the ones before it leave TMEM.  What issues the MMAs bounds the loop before the tensor pipe
 // does, so it has one barrier to wait for and one to signal for a block: `full` counts the operands of a stage and the warps that have taken the sums
@@ -604,7 +609,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // channels of a group, its warps share the blocks of K.  The weight goes from global memory straight into the A fragments of mma.m16n8k32, the
 // tokens into the B fragments: a lane loads 2 x 16 codes of channel lane / 4, of channel lane / 4 + 8 and of token lane / 4, all at the same places of
 // K, eight of each for one of the four instructions of a block - both sides number the contraction alike, so any numbering will do.
-// NT x 8 tokens at a time.  1 x 8192 x 8192 in 14.9 us (4.5 TB/s), 64 experts x 128 rows x 2048 x 4096 in 74 (6.0).  (The weight by way of
+// NT x 8 tokens at a time.  1 x 8192 x 8192 in 15.2 us (4.4 TB/s), 64 experts x 128 rows x 2048 x 4096 in 75 (5.9).  (The weight by way of
 // shared memory, three blocks ahead of each warp: 1.7 and 10 us more.)
 constexpr int FEW_CHANNELS = 16;
 
@@ -839,9 +844,9 @@ constexpr int FEW = 8, MOST_SHARES = 4;
 
 // Time of a tile shape in microseconds: the launch, and waves of tiles that take `stage` for each block of the contraction and what their output takes
 // beside the next tile's blocks: 16-bit numbers and fp32 ones that go out by TMA, and rows that it cannot write.  Fitted to 34000 calls (1 to 16384
-// tokens, 64 to 8192 channels, dense and of 2 to 64 groups, whose tiles are counted as if they were alike; weights that L2 does not hold).  The choice
-// takes 1.6 % (gradients 0.7 %) more time than the fastest of all shapes in the mean; pairs wherever their tiles fill a third of the device took
-// 5 to 8 % more, at worst 2.3 times.
+// tokens, 64 to 8192 channels, dense and of 2 to 64 groups, whose tiles are counted as if they were alike; weights that L2 does not hold), before the
+// scales had a warp of their own.  On 36000 other calls of each kind since then the choice takes 2.4 % (input gradient 1.2 %, weight gradient 1.3 %) more time
+// than the fastest of all shapes in the mean, at worst 2.1 times (1.6, 1.8); pairs wherever their tiles fill a third of the device took 5 to 8 % more.
 struct TileModel { int columns; float lat, stage, out[3]; };
 template <int KIND> constexpr TileModel TILES[3] = {};
 template <> constexpr TileModel TILES<MATMUL>[3] = {{256, 4.28f, 0.383f, {1.8f, 2.8f, 3.9f}}, {128, 3.68f, 0.271f, {1.1f, 1.5f, 2.05f}}, {64, 3.50f, 0.187f, {1.4f, 1.6f, 1.8f}}};
@@ -855,8 +860,10 @@ template <int KIND> Shape choose_shape(const ProductParams& p)
 {
     if (forced_shape.columns) return forced_shape;
     // The kernel for few tokens takes 0.5 to 0.75 of the best tiles' time with up to eight tokens, 0.65 with 16 (8192 x 8192: 23.6 us, by tiles 18.6), 0.9
-    // to 1.6 with 32; by group 0.6 to 0.9 with up to four to a group, with eight 0.75 to 0.9 for small weights (of many groups at worst 2.4) and
-    // 1.05 to 1.2 for large ones.
+    // to 1.6 with 32.  By group, where all have about as many rows: 0.6 to 0.9 with up to four to a group, with eight 0.75 to 0.9 for small weights (of many
+    // groups at worst 2.4, hence 16 of them at most) and 1.05 to 1.2 for large ones.  How the rows are distributed is known on the device alone.  A group's
+    // blocks walk over its rows eight at a time and read its weight again for each eight, so that rows which all go to one group take many times as long as
+    // by tiles: 64 groups of 2048 x 4096, 128 rows 74 us (by tiles 11), 256 rows 144 (11); 1024 groups of 512 x 512, 4096 rows 392 (22).
     const int64_t weights = (int64_t)std::max(p.groups, 1) * p.cols * p.depth;
     if (KIND == MATMUL && p.lda_scales <= 0x7FFFFFFF && (p.groups ? p.rows <= (weights <= 1 << 24 && p.groups <= 16 ? 8 : 4) * (int64_t)p.groups : p.rows <= 8 || (p.rows <= 16 && weights <= 1 << 25))) return {FEW, 1};
     const float groups = (float)std::max(p.groups, 1);

@@ -113,7 +113,8 @@ def norm(gradients, stream=None):
 
 def clip(gradients, max_norm, out=None, stream=None):
     """Scales the gradients by min(1, max_norm / norm), in place or into the tensors of `out`, and returns their norm from before (one float32
-    number on the device).  No output may share memory with another tensor of the list."""
+    number on the device).  Nothing is added to the norm, as torch.nn.utils.clip_grad_norm_ adds 1e-6: a norm of 0 leaves the gradients as they are.  No output may
+    share memory with another tensor of the list."""
     tensors, max_norm, out = _tensors(gradients, "gradients"), _number(max_norm, "max_norm"), None if out is None else list(out)
     if stream is None:
         r = _usual().clip(tensors, max_norm, out)
